@@ -1,0 +1,278 @@
+"""The operators that make and run the networks this library verifies, as they are measured: weights
+and rows held in microscaled 4-bit floating point (32 values with a common power of two), the
+products with them and their gradients, and the orthogonalised update of a layer's weights.
+
+A case is one call (or the two calls a program makes in a row) on inputs drawn from the seed.
+With `own` the calls go through `paper_2606_09377_amd.Ctx`; otherwise the same is computed by
+elementary torch operations in float32.
+"""
+import torch
+
+own = False
+
+A, B, C = 3.4445, -4.7750, 2.0315      # the quintic's coefficients
+EPS = 1e-7
+BLOCK, GROUP = 32, 128                 # values with one scale; rows are padded to groups of 4 blocks
+KINDS = ("quantize", "product", "linear", "grad", "orthogonalize")
+LARGEST = {"product": 4096 * 8192 * 8192, "linear": 2048 * 8192 * 8192, "grad": 4096 * 8192 * 8192}
+
+
+# ---- the cases ------------------------------------------------------------------------------
+def listed():
+    return [
+        # a hidden layer of the wide MLP stored in 4 bits and read back for the verifier
+        dict(name="quantize f32 8192x8192", kind="quantize", type="float32", rows=8192, cols=8192),
+        # a small batch of activations of no tile's size
+        dict(name="quantize bf16 777x1000", kind="quantize", type="bfloat16", rows=777, cols=1000),
+        # one query through a wide layer, everything in 4 bits
+        dict(name="product bf16 1x8192x8192", kind="product", type="bfloat16", rows=1, inner=8192, cols=8192,
+             relu=True),
+        # a large batch through it
+        dict(name="product bf16 4096x8192x8192", kind="product", type="bfloat16", rows=4096, inner=8192, cols=8192,
+             relu=True),
+        # one query on the widest layer (4096 inputs, 262144 neurons): the weights are read once
+        dict(name="linear f32 1x4096x262144", kind="linear", type="float32", rows=1, inner=4096, cols=262144,
+             relu=True),
+        # a serving batch on a wide layer
+        dict(name="linear bf16 256x8192x8192", kind="linear", type="bfloat16", rows=256, inner=8192, cols=8192,
+             relu=False),
+        # an evaluation batch on widths that are no multiple of a tile
+        dict(name="linear f32 2001x1000x1500", kind="linear", type="float32", rows=2001, inner=1000, cols=1500,
+             relu=True),
+        # a training batch on a layer of the 784-1024x6 MLP
+        dict(name="grad f32 64x1024x1024", kind="grad", type="float32", rows=64, inner=1024, cols=1024, relu=True),
+        # a training batch on a layer of the wide MLP
+        dict(name="grad bf16 4096x8192x8192", kind="grad", type="bfloat16", rows=4096, inner=8192, cols=8192,
+             relu=True),
+        # the update of one odd layer, added to its weights
+        dict(name="orthogonalize f32 777x1500", kind="orthogonalize", type="float32", count=1, rows=777, cols=1500,
+             steps=5, base=True),
+        # the updates of the 784-1024x6 MLP's hidden layers
+        dict(name="orthogonalize f32 5x1024x1024", kind="orthogonalize", type="float32", count=5, rows=1024,
+             cols=1024, steps=5, base=False),
+        # the update of a layer of the wide MLP
+        dict(name="orthogonalize bf16 8192x8192", kind="orthogonalize", type="bfloat16", count=1, rows=8192,
+             cols=8192, steps=5, base=False),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number between lo and hi, spread over its logarithm, of any remainder."""
+    return max(lo, min(hi, round(lo * (hi / lo) ** rng.random())))
+
+
+def draw(rng):
+    kind = rng.choice(KINDS)
+    case = dict(kind=kind, type=rng.choice(("float32", "bfloat16")))
+    if kind == "quantize":
+        return {**case, "rows": _log(rng, 1, 8192), "cols": _log(rng, 10, 8192)}
+    if kind == "orthogonalize":
+        case |= dict(count=rng.choice((1, 1, 2, 3, 5)), rows=_log(rng, 10, 4096), cols=_log(rng, 64, 8192), steps=5,
+                     base=rng.random() < 0.3)
+        if case["rows"] * case["cols"] > 2 ** 23:
+            case["count"] = 1
+        return case
+    case |= dict(rows=_log(rng, 1, 4096), inner=_log(rng, 64, 8192), cols=_log(rng, 10, 8192), relu=rng.random() < 0.5)
+    if case["rows"] * case["inner"] * case["cols"] > LARGEST[kind]:
+        case["rows"] = 2048
+    return case
+
+
+# ---- inputs ---------------------------------------------------------------------------------
+def prepare(case, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+    kind, dt = case["kind"], getattr(torch, case["type"])
+    s = {"case": case, "dtype": dt}
+    if kind == "quantize":
+        s["x"] = (normal(case["rows"], case["cols"]) * (2.0 / case["cols"]) ** 0.5).to(dt)
+        return s
+    if kind == "orthogonalize":
+        n, r, c = case["count"], case["rows"], case["cols"]
+        # a gradient averaged over a batch and over steps: a few strong directions and noise
+        k = min(r, c, 64)
+        strong = (normal(n, r, k) * torch.logspace(0, -2, k, device="cuda")) @ normal(n, k, c)
+        s["g"] = ((strong / k ** 0.5 + 0.3 * normal(n, r, c)) * 1e-3).to(dt)
+        if case["base"]:
+            s["w"] = normal(n, r, c) * (2.0 / c) ** 0.5
+        return s
+    m, k, n = case["rows"], case["inner"], case["cols"]
+    # a layer's stored weights: 4-bit codes (bit 3 the sign) and the blocks' powers of two; He-normal
+    # weights in blocks of 32 have exponents of a few neighbouring values
+    groups = -(-k // GROUP)
+    codes = torch.randint(0, 256, (n, GROUP // 2 * groups), generator=g, device="cuda", dtype=torch.uint8)
+    blocks = GROUP // BLOCK * groups
+    top = round(float(torch.log2(torch.tensor((2.0 / k) ** 0.5))))
+    scales = torch.randint(127 + top - 2, 127 + top + 1, (n, blocks), generator=g, device="cuda", dtype=torch.uint8)
+    if k % GROUP:   # the padding of a row holds zeros
+        codes[:, (k + 1) // 2:] = 0
+        if k % 2:
+            codes[:, k // 2] &= 15
+        scales[:, -(-k // BLOCK):] = 0
+    s |= {"codes": codes, "scales": scales, "bias": normal(n) * 0.01}
+    s["x"] = normal(m, k).relu_().to(dt)   # activations of the layer before
+    if kind == "grad":
+        s["dy"] = (normal(m, n) / m).to(dt)
+        s["y"] = normal(m, n).to(dt) if case["relu"] else None
+    return s
+
+
+# ---- the plain forms ------------------------------------------------------------------------
+def _quantized(x):
+    """The values that the 4-bit form of x stands for."""
+    rows, cols = x.shape
+    v = torch.nn.functional.pad(x.float(), (0, -cols % BLOCK)).view(rows, -1, BLOCK)
+    top = v.abs().amax(-1, keepdim=True)
+    e = (torch.frexp(top)[1] - 3).clamp(-127, 127)
+    a = torch.ldexp(v.abs(), -e)
+    code = ((a > 0.25).int() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0))
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=x.device)
+    q = torch.ldexp(grid[code] * torch.sign(v), e)
+    q = torch.where(torch.isfinite(top), q, torch.full_like(q, float("nan")))
+    return q.view(rows, -1)[:, :cols]
+
+
+def _stored(codes, scales, cols):
+    """The values that codes and scales stand for."""
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=codes.device)
+    grid = torch.cat([grid, -grid])
+    v = grid[torch.stack((codes & 15, codes >> 4), -1).int()].view(codes.shape[0], -1, BLOCK)
+    v = torch.ldexp(v, scales.int()[..., None] - 127)
+    return v.view(codes.shape[0], -1)[:, :cols]
+
+
+def _plain(s):
+    case, dt = s["case"], s["dtype"]
+    kind = case["kind"]
+    if kind == "quantize":
+        return _quantized(s["x"])
+    if kind == "orthogonalize":
+        tall = case["rows"] > case["cols"]
+        x = s["g"].float()
+        x = x.mT.contiguous() if tall else x
+        x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + EPS)
+        for _ in range(case["steps"]):
+            gram = x @ x.mT
+            x = A * x + (B * gram + C * (gram @ gram)) @ x
+        x = x.mT if tall else x
+        return (s["w"] - 0.2 * x) if case["base"] else x.to(dt)
+    w = _stored(s["codes"], s["scales"], case["inner"])
+    if kind == "grad":
+        g = s["dy"].float()
+        g = g * (s["y"].float() > 0) if case["relu"] else g
+        return {"dx": (g @ w).to(dt), "dw": g.T @ s["x"].float(), "db": g.sum(0)}
+    x = _quantized(s["x"]) if kind == "product" else s["x"].float()
+    y = x @ w.T + s["bias"]
+    return (y.relu() if case["relu"] else y).to(dt)
+
+
+# ---- the framework's calls ------------------------------------------------------------------
+_context = []
+
+
+def _ctx():
+    if not _context:
+        from paper_2606_09377_amd import Ctx
+        _context.append(Ctx(0))
+    return _context[0]
+
+
+def _own(s):
+    from paper_2606_09377_amd import MX
+    ctx, case = _ctx(), s["case"]
+    kind = case["kind"]
+    if kind == "quantize":
+        return ctx.mx_dequantize(ctx.mx_quantize(s["x"]))
+    if kind == "orthogonalize":
+        if case["base"]:
+            return ctx.orthogonalize(s["g"], steps=case["steps"], coefficients=(A, B, C), eps=EPS, gain=-0.2,
+                                     base=s["w"])
+        return ctx.orthogonalize(s["g"], steps=case["steps"], coefficients=(A, B, C), eps=EPS)
+    w = MX(s["codes"], s["scales"], case["inner"])
+    if kind == "grad":
+        dx, dw, db = ctx.mx_linear_grad(s["dy"], s["x"], w, y=s["y"])
+        return {"dx": dx, "dw": dw, "db": db}
+    if kind == "product":
+        return ctx.mx_product(ctx.mx_quantize(s["x"]), w, bias=s["bias"], relu=case["relu"], dtype=s["dtype"])
+    return ctx.mx_linear(s["x"], w, bias=s["bias"], relu=case["relu"])
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+# ---- floors and 64 bits ---------------------------------------------------------------------
+def work(case):
+    t = 4 if case["type"] == "float32" else 2
+    held = 0.5 + 1 / BLOCK   # bytes of a stored value
+    kind = case["kind"]
+    if kind == "quantize":
+        n = case["rows"] * case["cols"]
+        return {"bytes": n * (t + 4), "flops": 0}
+    if kind == "orthogonalize":
+        m, n = sorted((case["rows"], case["cols"]))
+        out = 8 if case["base"] else t
+        return {"bytes": case["count"] * m * n * (t + out),
+                "flops": case["count"] * case["steps"] * (m * m * n + m ** 3 + 2 * m * m * n)}
+    m, k, n = case["rows"], case["inner"], case["cols"]
+    if kind == "grad":
+        return {"bytes": m * n * t * (2 if case["relu"] else 1) + 2 * m * k * t + n * k * (held + 4) + 4 * n,
+                "flops": 4 * m * n * k}
+    return {"bytes": m * k * t + n * k * held + 4 * n + m * n * t, "flops": 2 * m * n * k}
+
+
+def exact(case, seed):
+    """run()'s outputs from the operators' definitions in 64 bits."""
+    s = prepare(case, seed)
+    kind = case["kind"]
+
+    def rounded(x):   # to 4 bits: the nearest of the 15 values, ties to the one with an even code
+        points = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=x.device)
+        out = torch.empty(x.shape, dtype=torch.float64, device=x.device)
+        for k0 in range(0, x.shape[1], BLOCK):
+            b = x[:, k0:k0 + BLOCK].double()
+            m = b.abs().max(1, keepdim=True).values
+            unit = torch.exp2((torch.log2(m.clamp_min(2.0 ** -140)).floor() - 2).clamp(-127, 127))
+            # log2 may round up to a whole number just below a power of two
+            unit = torch.where(m < 4 * unit, unit / 2, unit).clamp_min(2.0 ** -127)
+            v = (b.abs() / unit).clamp_max(6.0)
+            above = torch.searchsorted(points, v.contiguous()).clamp(1, 7)   # points[above - 1] < v <= points[above]
+            lo, hi = points[above - 1], points[above]
+            up = (hi - v < v - lo) | ((hi - v == v - lo) & (above % 2 == 0))
+            out[:, k0:k0 + BLOCK] = torch.where(up, hi, lo) * unit * torch.sign(b)
+        return out
+
+    def weights(rows):   # some of the stored weights
+        c = s["codes"][rows].long()
+        c = torch.stack((c % 16, c // 16), 2).flatten(1)
+        mag, sign = c % 8, 1.0 - 2.0 * (c // 8)
+        # exponent field 0: mantissa / 2, else 2^(field - 1) (1 + mantissa / 2)
+        field, man = (mag // 2).double(), (mag % 2).double()
+        v = torch.where(field == 0, man / 2, torch.exp2(field - 1) * (1 + man / 2)) * sign
+        return (v * torch.exp2(s["scales"][rows].double() - 127).repeat_interleave(BLOCK, 1))[:, :case["inner"]]
+
+    if kind == "quantize":
+        return rounded(s["x"])
+    if kind == "orthogonalize":
+        x = s["g"].double()
+        x = x / (torch.linalg.matrix_norm(x, keepdim=True) + EPS)
+        wide = case["rows"] <= case["cols"]
+        for _ in range(case["steps"]):
+            gram = torch.matmul(x, x.transpose(1, 2)) if wide else torch.matmul(x.transpose(1, 2).contiguous(), x)
+            poly = A * torch.eye(gram.shape[-1], dtype=x.dtype, device=x.device) + B * gram + C * torch.matmul(gram, gram)
+            x = torch.matmul(poly, x) if wide else torch.matmul(x, poly)
+        return s["w"].double() - 0.2 * x if case["base"] else x
+    step = 16384
+    parts = [slice(i, i + step) for i in range(0, case["cols"], step)]
+    x = s["x"].double()
+    if kind == "grad":
+        g = s["dy"].double()
+        if case["relu"]:
+            g = torch.where(s["y"] > 0, g, torch.zeros_like(g))
+        return {"dx": sum(torch.matmul(g[:, p], weights(p)) for p in parts),
+                "dw": torch.matmul(g.t().contiguous(), x), "db": g.sum(0)}
+    x = rounded(s["x"]) if kind == "product" else x
+    y = torch.cat([torch.matmul(x, weights(p).t()) for p in parts], 1) + s["bias"].double()
+    return y.clamp_min(0) if case["relu"] else y
