@@ -6,6 +6,8 @@ A case is one call (or the two calls a program makes in a row) on inputs drawn f
 With `own` the calls go through `paper_2606_09377_amd.Ctx`; otherwise the same is computed by
 elementary torch operations in float32.
 """
+import math
+
 import torch
 
 own = False
@@ -79,6 +81,16 @@ def draw(rng):
 
 
 # ---- inputs ---------------------------------------------------------------------------------
+def _laid_out(codes, scales):
+    """The weights as a program keeps them: laid out once in the order the matrix instructions read,
+    16 rows by 128 columns together (16 bytes of each row and block), the scales of 4 such groups side by side."""
+    n, groups = codes.shape[0], codes.shape[1] // (GROUP // 2)
+    fill = torch.nn.functional.pad
+    codes = fill(codes, (0, 0, 0, -n % 16)).view(-1, 16, groups, 4, 16).permute(0, 2, 3, 1, 4)
+    scales = fill(scales, (0, -groups % 4 * 4, 0, -n % 16)).view(-1, 16, -(-groups // 4), 4, 4).permute(0, 2, 4, 1, 3)
+    return codes.reshape(-1, groups, 64, 16), scales.reshape(-1, -(-groups // 4), 64, 4)
+
+
 def prepare(case, seed):
     g = torch.Generator("cuda").manual_seed(seed)
 
@@ -103,15 +115,17 @@ def prepare(case, seed):
     # weights in blocks of 32 have exponents of a few neighbouring values
     groups = -(-k // GROUP)
     codes = torch.randint(0, 256, (n, GROUP // 2 * groups), generator=g, device="cuda", dtype=torch.uint8)
-    blocks = GROUP // BLOCK * groups
-    top = round(float(torch.log2(torch.tensor((2.0 / k) ** 0.5))))
-    scales = torch.randint(127 + top - 2, 127 + top + 1, (n, blocks), generator=g, device="cuda", dtype=torch.uint8)
+    top = round(math.log2((2.0 / k) ** 0.5))
+    scales = torch.randint(127 + top - 2, 127 + top + 1, (n, 4 * groups), generator=g, device="cuda",
+                           dtype=torch.uint8)
     if k % GROUP:   # the padding of a row holds zeros
         codes[:, (k + 1) // 2:] = 0
         if k % 2:
             codes[:, k // 2] &= 15
         scales[:, -(-k // BLOCK):] = 0
-    s |= {"codes": codes, "scales": scales, "bias": normal(n) * 0.01}
+    s["codes"], s["scales"] = codes, scales
+    s["held"] = _laid_out(codes, scales)
+    s["bias"] = normal(n) * 0.01
     s["x"] = normal(m, k).relu_().to(dt)   # activations of the layer before
     if kind == "grad":
         s["dy"] = (normal(m, n) / m).to(dt)
@@ -190,7 +204,7 @@ def _own(s):
             return ctx.orthogonalize(s["g"], steps=case["steps"], coefficients=(A, B, C), eps=EPS, gain=-0.2,
                                      base=s["w"])
         return ctx.orthogonalize(s["g"], steps=case["steps"], coefficients=(A, B, C), eps=EPS)
-    w = MX(s["codes"], s["scales"], case["inner"])
+    w = MX(*s["held"], case["cols"], case["inner"])
     if kind == "grad":
         dx, dw, db = ctx.mx_linear_grad(s["dy"], s["x"], w, y=s["y"])
         return {"dx": dx, "dw": dw, "db": db}
