@@ -20,8 +20,8 @@
  *     input are bounded in one batched pass (Sec. 2.4, batch BaB).
  *
  * Conventions shared by every entry point:
- *   - All tensors are float32, dense, row-major (C order).  Device pointers must come from
- *     the context's device and be 16-byte aligned.
+ *   - All tensors are float32, dense, row-major (C order), unless given as vcr_mat or vcr_mx.  Device
+ *     pointers must come from the context's device and be 16-byte aligned (vcr_mat: element-aligned).
  *   - Work is queued on the context's stream (vcr_set_stream; default: the null stream).
  *     Entry points return once the work is queued; outputs are valid after the stream is
  *     synchronised.  Entry points that must read device results say "synchronises".
@@ -361,6 +361,88 @@ vcr_status vcr_get_layer_bounds(vcr_ctx *ctx, int32_t relu_id, float *l, float *
 
 /* Device bytes a bounds call of this size would hold (without a cap). */
 vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_domains, uint64_t *bytes);
+
+/* ---- Layers in 4 bits, and the update that trains them -----------------------------------------
+ * The network that answers is often not the one that was trained: its weights are held in
+ * microscaled 4-bit floating point.  These calls make such weights, multiply by them, give the
+ * gradients through them, and read them back, so that the bounds above are taken of the network as it
+ * is deployed (load the values of vcr_mx_dequantize); and they orthogonalise the update of a layer's
+ * weights, which keeps the spectral norms that bounds grow by in check.
+ *
+ * Matrices are given by vcr_mat: float32 or bf16, row-major, rows `ld` elements apart (>= cols), aligned to
+ * their element type (calls are faster where p and the rows are 16-byte aligned).  A matrix of no rows is
+ * allowed where rows are a batch, and queues nothing (or zeros, for sums over the batch).  Outputs
+ * must not overlap inputs unless stated.  These calls need no loaded network and leave it, its bounds
+ * and the other calls' workspace alone; they keep one workspace per stream, which grows as needed
+ * (VCR_ERR_OOM beyond VCR_OPT_WORKSPACE_CAP_BYTES).  A call may be recorded into a HIP graph by the
+ * caller once it has run with the same sizes on that stream (else VCR_ERR_STATE). */
+enum { VCR_F32 = 0, VCR_BF16 = 1 };
+
+typedef struct {
+  void *p;                  /* device */
+  int32_t type;             /* VCR_F32 or VCR_BF16 */
+  int64_t rows, cols, ld;
+} vcr_mat;
+
+/* A rows x cols matrix in microscaled 4-bit floating point (the OCP MX formats' MXFP4): 32 consecutive
+ * values of a row share a scale 2^(byte - 127) (byte 255: the block is NaN), each is one of +-{0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6} as 4 bits: sign, two bits of exponent, one of mantissa.  Laid out in the order the matrix
+ * instructions read, padded with zero codes to whole groups of 16 rows and 128 columns (and scales that
+ * are not 255):
+ *   codes  [ceil(rows/16)][ceil(cols/128)][64][16]  entry l = 16 g + r holds columns 32 g .. 32 g + 31 of the
+ *          group's row r, the even one of two columns in the low half of a byte;
+ *   scales [ceil(rows/16)][ceil(cols/512)][64][4]   entry [l][q]: the scale of that row and block in the
+ *          q-th group of 128 columns.
+ * Both 16-byte aligned; vcr_mx_bytes gives their sizes. */
+typedef struct {
+  uint8_t *codes, *scales;  /* device */
+  int64_t rows, cols;
+} vcr_mx;
+
+vcr_status vcr_mx_bytes(int64_t rows, int64_t cols, uint64_t *codes, uint64_t *scales);
+
+/* q = x in 4 bits: per block the exponent floor(log2 max|x|) - 2 within [-127, 127], values rounded to
+ * nearest, ties to the even code, above 6 to 6.  A block with an infinity or NaN becomes NaN. */
+vcr_status vcr_mx_quantize(vcr_ctx *ctx, const vcr_mat *x, const vcr_mx *q);
+
+/* y = the values q stands for (exact in either type; above 2^127 1.5 they are infinite). */
+vcr_status vcr_mx_dequantize(vcr_ctx *ctx, const vcr_mx *q, const vcr_mat *y);
+
+/* y = act(a w^T + bias), a (rows, k) and w (n, k) both in 4 bits, y (rows, n); bias device (n) or NULL;
+ * act = max(., 0) with relu, else nothing.  Products are exact, sums float32. */
+vcr_status vcr_mx_product(vcr_ctx *ctx, const vcr_mx *a, const vcr_mx *w, const float *bias, int32_t relu,
+                          const vcr_mat *y);
+
+/* y = act(x w^T + bias) with x (rows, k) as it is: the layer whose weights are the 4-bit ones, which
+ * is the one a verified network has.  float32 x is multiplied as three bf16 values, exactly but for what of x
+ * is below 2^-133 (as under "Arithmetic"), bf16 x exactly; sums are float32, their order depends on the sizes. */
+vcr_status vcr_mx_linear(vcr_ctx *ctx, const vcr_mat *x, const vcr_mx *w, const float *bias, int32_t relu,
+                         const vcr_mat *y);
+
+/* Gradients of vcr_mx_linear from dy (rows, n): with g = dy, or dy where y > 0 (y: the output of a call with
+ * relu, of dy's type; NULL: no relu),
+ *   dx (rows, k) = g w,   dw (n, k) = g^T x   (the gradient by the weights before their quantisation, which
+ *   passes it on as it is),   db (n) = sum of g over the rows, float32.
+ * Outputs may be NULL; x (of dy's type) is needed for dw, w for dx.  No rows: dw and db are zero. */
+vcr_status vcr_mx_linear_grad(vcr_ctx *ctx, const vcr_mat *dy, const vcr_mat *y, const vcr_mat *x, const vcr_mx *w,
+                              const vcr_mat *dx, const vcr_mat *dw, float *db);
+
+/* Newton-Schulz orthogonalisation: X = g / (|g|_F + eps), then `steps` times, with A = X X^T (X^T X for more
+ * rows than columns), X <- (a I + b A + c A A) X (from the right); out = gain X, or keep base + gain X.  With a =
+ * 3.4445, b = -4.7750, c = 2.0315 five steps bring singular values above about 2^-9 of the norm
+ * into [0.7, 1.2].  float32 g is multiplied to float32's accuracy, bf16 g with 16 bits of every factor. */
+typedef struct {
+  int32_t steps;            /* in [1, 100] */
+  float a, b, c;
+  float eps;                /* >= 0; without it a zero matrix gives NaN */
+  float gain;
+  float keep;               /* factor of base */
+} vcr_ns_opts;
+
+/* `count` matrices, the strides in elements between them (not read for count <= 1).  base may be NULL, and may be
+ * out itself; all of one shape, of any types. */
+vcr_status vcr_orthogonalize(vcr_ctx *ctx, const vcr_mat *g, int32_t count, int64_t g_stride, const vcr_ns_opts *opts,
+                             const vcr_mat *base, int64_t base_stride, const vcr_mat *out, int64_t out_stride);
 
 /* Statistics; synchronises the stream. */
 vcr_status vcr_get_stats(vcr_ctx *ctx, vcr_stats *out);

@@ -386,6 +386,10 @@ void vcr_destroy(vcr_ctx *c) {
     forget_split_operands(c);
     free_layers(c);
     free_ws(c);
+    if (!c->op_spaces.empty()) (void)hipDeviceSynchronize();   // calls on any stream may still use their room
+    for (auto &o : c->op_spaces)
+      if (o.w.base) (void)hipFree(o.w.base);
+    for (void *p : c->op_retired) (void)hipFree(p);
     if (c->d_counters) (void)hipFree(c->d_counters);
     if (c->bab_buf) (void)hipFree(c->bab_buf);
     if (c->root_cache) (void)hipFree(c->root_cache);
@@ -1740,6 +1744,7 @@ vcr_status vcr_get_stats(vcr_ctx *c, vcr_stats *out) {
   out->gemm_flops_last_call = c->flops_last;
   out->peak_workspace_bytes = c->peak_ws;
   out->workspace_bytes = c->ws.cap;
+  for (const auto &o : c->op_spaces) out->workspace_bytes += o.w.cap;
   out->n_chunks_last_call = c->chunks_last;
   out->n_relu = (int32_t)c->relu_n.size();
   out->net_bytes = c->net_bytes;

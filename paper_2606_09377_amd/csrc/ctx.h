@@ -45,6 +45,14 @@ struct Workspace {
   size_t cap = 0, used = 0;
 };
 
+// Room of the calls on layers' weights (layers.h) on one stream; held: a graph that the caller
+// recorded uses it, so it is kept when a larger one takes its place
+struct OpSpace {
+  hipStream_t stream = nullptr;
+  Workspace w;
+  bool held = false;
+};
+
 }  // namespace vcr_internal
 
 using vcr_internal::DenseLayer;
@@ -74,6 +82,8 @@ struct vcr_ctx {
   // workspace
   Workspace ws;
   uint64_t peak_ws = 0;
+  std::vector<vcr_internal::OpSpace> op_spaces;
+  std::vector<void *> op_retired;
   // split weight operands: what the loaded network would have split, and the one allocation that
   // holds them (null while there is none)
   std::vector<SplitItem> split_items;

@@ -1,0 +1,258 @@
+// Orthogonalised updates of layers' weights by Newton-Schulz products: vcr_orthogonalize of vcrown.h.
+//
+// With X = G / (|G| + eps) (Frobenius norm; G transposed where it is taller than wide, so X is m x n, m <= n),
+// every step is  A = X X^T,  Q = a I + b A + c A A,  X <- Q X,  which takes each singular value s of X to
+// s (a + b s^2 + c s^4) and so all of them towards 1.
+//
+// A and Q are symmetric: of their 16 x 16 blocks those on and below the diagonal are computed and
+// stored twice.  A step is 3 m^2 n + m^3 multiply-adds that way (of 4 m^2 n + 2 m^3).  All three products
+// contract the contiguous axes of operands in the layout of nt.h: X (rows m) and its transpose (rows
+// n) are both kept, written by the epilogue that makes them.  float32 updates take three bf16 parts
+// (float32's accuracy), bf16 ones two: a singular value of 2^-9 is raised by a^5 = 485 in five steps, and
+// the rounding of one part, 2^-9 of the largest, with it.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "layers.h"
+#include "planes.h"
+
+namespace vcr {
+
+constexpr int NORM_PARTS = 64;   // partial sums of a matrix's squares
+
+template <bool BF>
+__global__ __launch_bounds__(256) void k_ns_norm(DevMat g, double *part) {
+  __shared__ double sh[4];
+  const int64_t base = (int64_t)blockIdx.y * g.stride, total = g.rows * g.cols;
+  double s = 0.0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += NORM_PARTS * 256) {
+    const int64_t r = i / g.cols;
+    const float x = mat_at<BF>(g, base, r, i - r * g.cols);
+    s += (double)x * x;
+  }
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.y * NORM_PARTS + blockIdx.x] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
+}
+// 1 / (norm + eps), by every wave
+__device__ __forceinline__ float ns_scale(const double *part, int batch, float eps) {
+  double s = part[batch * NORM_PARTS + (threadIdx.x & 63)];
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  return (float)(1.0 / (sqrt(s) + (double)eps));
+}
+
+// X's parts from G: rows as they are, and transposed
+template <int P, bool BF>
+__global__ __launch_bounds__(256) void k_ns_rows(DevMat g, int vec, const double *part, float eps, int64_t row_blocks, int64_t chunks,
+                                                 uint8_t *out) {
+  const int lane = threadIdx.x & 63;
+  const float sc = ns_scale(part, blockIdx.y, eps);
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rb = id / chunks, ch = id - rb * chunks;
+  if (rb >= row_blocks) return;
+  float v[8];
+  mat_row8<BF>(g, (int64_t)blockIdx.y * g.stride, rb * 16 + (lane & 15), ch * 32 + (lane >> 4) * 8, vec, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= sc;
+  store_slot<P>(out + blockIdx.y * row_blocks * chunks * P * FRAG, id, lane, v);
+}
+template <int P, bool BF>
+__global__ __launch_bounds__(256) void k_ns_cols(DevMat g, const double *part, float eps, int64_t row_blocks, int64_t chunks,
+                                                 uint8_t *out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float sc = ns_scale(part, blockIdx.y, eps);
+  const int64_t nc = (row_blocks + 3) / 4, ch = blockIdx.x / nc, col = (blockIdx.x - ch * nc) * 64 + lane;
+  if (col >= row_blocks * 16) return;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = sc * mat_at<BF>(g, (int64_t)blockIdx.y * g.stride, ch * 32 + wave * 8 + i, col);
+  store_slot<P>(out + blockIdx.y * row_blocks * chunks * P * FRAG, (col >> 4) * chunks + ch, wave * 16 + (int)(col & 15), v);
+}
+
+enum NsMode : int32_t { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2, NS_OUT = 3 };
+
+// Epilogue of a step's three products; mp x np the padded sizes
+struct NsEpilogue {
+  int32_t mp, np;
+  uint8_t *dst, *dst_t;        // [mp][mp] (gram, poly); X [mp][np] and its transpose (update)
+  const uint8_t *gram;         // poly
+  float a, b, c;
+  // out = keep base + gain X, transposed back where the update is
+  DevMat base;
+  void *out;
+  int64_t out_rows, out_cols, out_ld, out_stride;
+  float keep, gain;
+  int32_t out_bf16, vec, transposed;
+};
+template <int P, int MODE>
+struct EpiNs : NsEpilogue {
+  __device__ __forceinline__ void store(int batch, int, int m, int n, f32v4 v, int lane) const {
+    const int bm = m >> 4, bn = n >> 4, r = lane & 15;
+    // after a transposition the lane holds row nt, columns mt .. mt + 3
+    const int nt = n + (r & 3), mt = (m & ~3);
+    if constexpr (MODE <= NS_POLY) {
+      if (bm * 16 >= mp || bn > bm) return;   // wave-uniform
+      const int64_t off = (int64_t)batch * (mp / 16) * (mp / 32) * P * FRAG;
+      if constexpr (MODE == NS_POLY) {
+        const f32v4 q = load_quad<P>(gram + off, m, n, mp / 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(c, v[i], fmaf(b, q[i], m == n + i ? a : 0.f));
+      }
+      store_quad<P>(dst + off, m, n, mp / 32, v);
+      if (bm != bn) store_quad<P>(dst + off, nt, mt, mp / 32, quad_transpose(v, lane));
+    } else if (bm * 16 >= mp || bn * 16 >= np) {
+      return;
+    } else if constexpr (MODE == NS_UPDATE) {
+      const int64_t off = (int64_t)batch * (mp / 16) * (np / 32) * P * FRAG;
+      store_quad<P>(dst + off, m, n, np / 32, v);
+      store_quad<P>(dst_t + off, nt, mt, mp / 32, quad_transpose(v, lane));
+    } else {
+      if (transposed) v = quad_transpose(v, lane);
+      const int64_t row = transposed ? nt : m, col = transposed ? mt : n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] *= gain;
+        if (base.p && row < out_rows && col + i < out_cols) {
+          const int64_t at = batch * base.stride + row * base.ld + col + i;
+          const float w = base.bf16 ? bf16_value(static_cast<const uint16_t *>(base.p)[at]) : static_cast<const float *>(base.p)[at];
+          v[i] = fmaf(keep, w, v[i]);
+        }
+      }
+      store_row4(static_cast<char *>(out) + batch * out_stride * (out_bf16 ? 2 : 4), out_bf16, out_ld, out_rows, out_cols, vec, row, col, v);
+    }
+  }
+};
+
+template <int P>
+struct NsTiles {
+  typedef std::conditional_t<P == 3, NtTile<4, 4, 4, 2, P, P, 1>, NtTile<8, 4, 2, 4, P, P, 1>> L;
+  typedef std::conditional_t<P == 3, NtTile<4, 2, 2, 4, P, P, 1>, NtTile<4, 4, 2, 2, P, P, 1>> M;
+  typedef NtTile<2, 2, 2, 2, P, P, 1> S;
+};
+template <int P, int MODE>
+static hipError_t ns_product(const NtArgs &g, int64_t M, int64_t N, int batch, const NsEpilogue &base, hipStream_t s) {
+  typedef NsTiles<P> TS;
+  const EpiNs<P, MODE> e{base};
+  auto tiles = [&](int bm, int bn) { return blocks_of(M, bm) * blocks_of(N, bn) * batch / (g.tri ? 2 : 1); };
+  if (tiles(TS::L::BM, TS::L::BN) >= 200) return launch_nt<typename TS::L>(g, M, N, batch, 1, e, s);
+  if (tiles(TS::M::BM, TS::M::BN) >= 200) return launch_nt<typename TS::M>(g, M, N, batch, 1, e, s);
+  return launch_nt<typename TS::S>(g, M, N, batch, 1, e, s);
+}
+
+struct NsSpace {
+  double *norm;
+  uint8_t *x, *xt, *x2, *xt2, *gram, *poly;
+};
+static NsSpace ns_carve(Workspace &w, int64_t mp, int64_t np, int batch, int P) {
+  NsSpace s;
+  const size_t bx = (size_t)batch * mp * np * 2 * P, bg = (size_t)batch * mp * mp * 2 * P;
+  s.norm = take<double>(w, (size_t)batch * NORM_PARTS);
+  s.x = take<uint8_t>(w, bx);
+  s.xt = take<uint8_t>(w, bx);
+  s.x2 = take<uint8_t>(w, bx);
+  s.xt2 = take<uint8_t>(w, bx);
+  s.gram = take<uint8_t>(w, bg);
+  s.poly = take<uint8_t>(w, bg);
+  return s;
+}
+
+template <int P, bool BF>
+static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, bool transposed, int steps, NsEpilogue e, float eps,
+                         NsSpace sp, hipStream_t s) {
+  const int vec = rows_aligned(g.p, g.ld, BF ? 2 : 4) && (g.stride * (BF ? 2 : 4)) % 16 == 0;
+  hipLaunchKernelGGL((k_ns_norm<BF>), dim3(NORM_PARTS, batch), dim3(256), 0, s, g, sp.norm);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  // G's rows padded to rp, its columns to cp
+  const int64_t rp = transposed ? np : mp, cp = transposed ? mp : np;
+  uint8_t *rows = transposed ? sp.xt : sp.x, *cols = transposed ? sp.x : sp.xt;
+  hipLaunchKernelGGL((k_ns_rows<P, BF>), dim3((unsigned)blocks_of(rp / 16 * (cp / 32), 4), batch), dim3(256), 0, s, g, vec, sp.norm, eps,
+                     rp / 16, cp / 32, rows);
+  if ((err = hipGetLastError()) != hipSuccess) return err;
+  hipLaunchKernelGGL((k_ns_cols<P, BF>), dim3((unsigned)(blocks_of(cp, 64) * (rp / 32)), batch), dim3(256), 0, s, g, sp.norm, eps, cp / 16,
+                     rp / 32, cols);
+  if ((err = hipGetLastError()) != hipSuccess) return err;
+  e.mp = (int32_t)mp;
+  e.np = (int32_t)np;
+  const int64_t sx = mp * np * 2 * P, sg = mp * mp * 2 * P;
+  for (int step = 0; step < steps; ++step) {
+    NtArgs a{};
+    a.A = a.B = NtOperand{sp.x, nullptr, (int32_t)(mp / 16), sx};
+    a.chunks = (int32_t)(np / 32);
+    a.tri = 1;
+    e.dst = sp.gram;
+    if ((err = ns_product<P, NS_GRAM>(a, mp, mp, batch, e, s)) != hipSuccess) return err;
+    a.A = a.B = NtOperand{sp.gram, nullptr, (int32_t)(mp / 16), sg};
+    a.chunks = (int32_t)(mp / 32);
+    e.gram = sp.gram;
+    e.dst = sp.poly;
+    if ((err = ns_product<P, NS_POLY>(a, mp, mp, batch, e, s)) != hipSuccess) return err;
+    a.A = NtOperand{sp.poly, nullptr, (int32_t)(mp / 16), sg};
+    a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx};
+    a.tri = 0;
+    e.dst = sp.x2;
+    e.dst_t = sp.xt2;
+    err = step + 1 == steps ? ns_product<P, NS_OUT>(a, mp, np, batch, e, s) : ns_product<P, NS_UPDATE>(a, mp, np, batch, e, s);
+    if (err != hipSuccess) return err;
+    std::swap(sp.x, sp.x2);
+    std::swap(sp.xt, sp.xt2);
+  }
+  return hipSuccess;
+}
+
+}  // namespace vcr
+
+using namespace vcr;
+
+extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t count, int64_t g_stride, const vcr_ns_opts *o,
+                                        const vcr_mat *base, int64_t base_stride, const vcr_mat *out, int64_t out_stride) {
+  if (!c) return VCR_ERR_ARG;
+  vcr_status st;
+  if ((st = check_mat(c, g, "g")) != VCR_OK || (st = check_mat(c, out, "out")) != VCR_OK) return st;
+  if (base && (st = check_mat(c, base, "base")) != VCR_OK) return st;
+  if (!o) return fail(c, VCR_ERR_ARG, "opts: null");
+  if (count < 0 || count > 65535) return fail(c, VCR_ERR_ARG, "count %d is not in [0, 65535]", count);
+  if (o->steps < 1 || o->steps > 100) return fail(c, VCR_ERR_ARG, "steps %d is not in [1, 100]", o->steps);
+  const float vals[] = {o->a, o->b, o->c, o->eps, o->gain, o->keep};
+  for (float v : vals)
+    if (!std::isfinite(v)) return fail(c, VCR_ERR_ARG, "an option is not finite");
+  if (o->eps < 0.f) return fail(c, VCR_ERR_ARG, "eps < 0");
+  if (out->rows != g->rows || out->cols != g->cols || (base && (base->rows != g->rows || base->cols != g->cols)))
+    return fail(c, VCR_ERR_SHAPE, "g, base and out differ in shape");
+  if (g->rows * g->cols > VCR_MAX_LAYER_WEIGHTS)
+    return fail(c, VCR_ERR_SHAPE, "%lld x %lld exceeds the limit of %lld weights", (long long)g->rows, (long long)g->cols,
+                (long long)VCR_MAX_LAYER_WEIGHTS);
+  auto span = [](const vcr_mat *m) { return m->rows > 0 ? (m->rows - 1) * m->ld + m->cols : 0; };
+  if (count > 1 && (g_stride < span(g) || out_stride < span(out) || (base && base_stride < span(base))))
+    return fail(c, VCR_ERR_SHAPE, "matrices of a batch overlap");
+  if ((st = op_begin(c)) != VCR_OK) return st;
+  if (count == 0 || g->rows == 0) return VCR_OK;
+  const bool tr = g->rows > g->cols, bf = g->type == VCR_BF16;
+  const int64_t mp = blocks_of(std::min(g->rows, g->cols), 32) * 32, np = blocks_of(std::max(g->rows, g->cols), 32) * 32;
+  const int P = bf ? 2 : 3;
+  Workspace size;
+  (void)ns_carve(size, mp, np, count, P);
+  Workspace *ws = nullptr;
+  if ((st = op_space(c, size.used, &ws)) != VCR_OK) return st;
+  const NsSpace sp = ns_carve(*ws, mp, np, count, P);
+  const DevMat d{g->p, bf, g->rows, g->cols, g->ld, g_stride};
+  NsEpilogue e{};
+  e.a = o->a;
+  e.b = o->b;
+  e.c = o->c;
+  e.base = base ? DevMat{base->p, base->type == VCR_BF16, base->rows, base->cols, base->ld, base_stride} : DevMat{};
+  e.out = out->p;
+  e.out_rows = out->rows;
+  e.out_cols = out->cols;
+  e.out_ld = out->ld;
+  e.out_stride = out_stride;
+  e.keep = o->keep;
+  e.gain = o->gain;
+  e.out_bf16 = out->type == VCR_BF16;
+  e.vec = (reinterpret_cast<uintptr_t>(out->p) & (e.out_bf16 ? 7 : 15)) == 0 && out->ld % 4 == 0 && out_stride % 4 == 0;
+  e.transposed = tr;
+  if (bf) HIP_TRY(c, (ns_run<2, true>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream)));
+  else HIP_TRY(c, (ns_run<3, false>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream)));
+  return op_end(c);
+}

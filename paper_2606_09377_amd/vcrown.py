@@ -78,6 +78,21 @@ class VcrBabResult(ctypes.Structure):
                 ("remaining", ctypes.c_int64), ("root_min_lb", ctypes.c_float), ("worst_lb", ctypes.c_float)]
 
 
+class VcrMat(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("type", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64)]
+
+
+class VcrMx(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
+class VcrNsOpts(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("eps", ctypes.c_float), ("gain", ctypes.c_float), ("keep", ctypes.c_float)]
+
+
 class VcrError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 7 else status}: {msg}")
@@ -114,6 +129,16 @@ def load_library(path: str = LIB_PATH):
         "vcr_beta_crown_bounds": ([P, P, F32, P, I32, ctypes.POINTER(VcrSplits), ctypes.POINTER(VcrBetaOpts), P, P],
                                   I32),
         "vcr_bab_verify": ([P, P, F32, P, I32, ctypes.POINTER(VcrBabOpts), ctypes.POINTER(VcrBabResult), P], I32),
+        "vcr_mx_bytes": ([ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_uint64),
+                          ctypes.POINTER(ctypes.c_uint64)], I32),
+        "vcr_mx_quantize": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMx)], I32),
+        "vcr_mx_dequantize": ([P, ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMat)], I32),
+        "vcr_mx_product": ([P, ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMx), P, I32, ctypes.POINTER(VcrMat)], I32),
+        "vcr_mx_linear": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMx), P, I32, ctypes.POINTER(VcrMat)], I32),
+        "vcr_mx_linear_grad": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat),
+                                ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat), P], I32),
+        "vcr_orthogonalize": ([P, ctypes.POINTER(VcrMat), I32, ctypes.c_int64, ctypes.POINTER(VcrNsOpts),
+                               ctypes.POINTER(VcrMat), ctypes.c_int64, ctypes.POINTER(VcrMat), ctypes.c_int64], I32),
         "vcr_crown_bounds_noalloc": ([P, P, I32, F32, P, I32, P, P], I32),
     }
     for name, (args, res) in sig.items():
@@ -136,6 +161,57 @@ def header_symbols(path: str = HEADER):
 
 def _ptr(t):
     return ctypes.c_void_p(t.data_ptr())
+
+
+class MX:
+    """A rows x cols matrix in microscaled 4-bit floating point (vcr_mx): uint8 CUDA tensors `codes` (row blocks,
+    column groups, 64, 16) and `scales` (row blocks, ceil(groups / 4), 64, 4).  Made by Ctx.mx_quantize, or by
+    MX.pack from codes and scales in row order."""
+
+    __slots__ = ("codes", "scales", "rows", "cols")
+
+    def __init__(self, codes, scales, rows, cols):
+        groups = -(-cols // 128)
+        want = (-(-rows // 16), groups, 64, 16), (-(-rows // 16), -(-groups // 4), 64, 4)
+        import torch
+        for t, shape in zip((codes, scales), want):
+            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+                raise ValueError(f"expected a contiguous uint8 CUDA tensor of shape {shape}")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        import torch
+        rb, groups = -(-rows // 16), -(-cols // 128)
+        return cls(torch.empty((rb, groups, 64, 16), dtype=torch.uint8, device=device),
+                   torch.empty((rb, -(-groups // 4), 64, 4), dtype=torch.uint8, device=device), rows, cols)
+
+    @classmethod
+    def pack(cls, codes, scales, cols):
+        """From codes (rows, ceil(cols / 2)), the even one of two columns in the low half of a byte, and scales
+        (rows, ceil(cols / 32)) in row order, as other programs store them."""
+        import torch
+        rows, groups = codes.shape[0], -(-cols // 128)
+        if tuple(codes.shape) != (rows, -(-cols // 2)) or tuple(scales.shape) != (rows, -(-cols // 32)):
+            raise ValueError("codes are (rows, ceil(cols / 2)), scales (rows, ceil(cols / 32))")
+        pad = torch.nn.functional.pad
+        if cols % 2:
+            codes = torch.cat((codes[:, :-1], codes[:, -1:] & 15), 1)
+        c = pad(codes, (0, 64 * groups - codes.shape[1], 0, -rows % 16)).view(-1, 16, groups, 4, 16)
+        n4 = -(-groups // 4)
+        s = pad(scales, (0, 16 * n4 - scales.shape[1], 0, -rows % 16)).view(-1, 16, n4, 4, 4)
+        return cls(c.permute(0, 2, 3, 1, 4).reshape(-1, groups, 64, 16).contiguous(),
+                   s.permute(0, 2, 4, 1, 3).reshape(-1, n4, 64, 4).contiguous(), rows, cols)
+
+    def unpack(self):
+        """(codes, scales) in row order (the reverse of pack)."""
+        rb, groups, n4 = self.codes.shape[0], self.codes.shape[1], self.scales.shape[1]
+        c = self.codes.view(rb, groups, 4, 16, 16).permute(0, 3, 1, 2, 4).reshape(rb * 16, groups * 64)
+        s = self.scales.view(rb, n4, 4, 16, 4).permute(0, 3, 1, 4, 2).reshape(rb * 16, n4 * 16)
+        return (c[:self.rows, :-(-self.cols // 2)].contiguous(), s[:self.rows, :-(-self.cols // 32)].contiguous())
+
+    def _c(self):
+        return VcrMx(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
 
 
 def _net_nodes(net):
@@ -363,6 +439,83 @@ class Ctx:
                                             _ptr(lb), _ptr(ub)))
         return lb, ub
 
+    # ---- layers in 4 bits, and the update that trains them ----
+    def mx_quantize(self, x, out=None):
+        """x (rows, cols), a float32 or bfloat16 CUDA tensor with contiguous rows, in 4 bits (an MX)."""
+        m = _mat(x)
+        q = MX.empty(m.rows, m.cols, x.device) if out is None else out
+        self._stream_sync()
+        self._check(self.lib.vcr_mx_quantize(self.h, ctypes.byref(m), ctypes.byref(q._c())))
+        return q
+
+    def mx_dequantize(self, q, dtype=None, out=None):
+        """The values of an MX, float32 unless `dtype` is bfloat16."""
+        import torch
+        y = torch.empty((q.rows, q.cols), dtype=dtype or torch.float32, device=q.codes.device) if out is None else out
+        self._stream_sync()
+        self._check(self.lib.vcr_mx_dequantize(self.h, ctypes.byref(q._c()), ctypes.byref(_mat(y))))
+        return y
+
+    def mx_product(self, a, w, bias=None, relu=False, dtype=None, out=None):
+        """act(a w^T + bias), a (rows, k) and w (n, k) both MX, float32 unless `dtype` is bfloat16."""
+        import torch
+        y = torch.empty((a.rows, w.rows), dtype=dtype or torch.float32, device=a.codes.device) if out is None else out
+        self._stream_sync()
+        self._check(self.lib.vcr_mx_product(self.h, ctypes.byref(a._c()), ctypes.byref(w._c()), _bias(bias, w.rows),
+                                            1 if relu else 0, ctypes.byref(_mat(y))))
+        return y
+
+    def mx_linear(self, x, w, bias=None, relu=False, out=None):
+        """act(x w^T + bias), x (rows, k) a float32 or bfloat16 tensor, w (n, k) an MX; of x's type."""
+        import torch
+        m = _mat(x)
+        y = torch.empty((m.rows, w.rows), dtype=x.dtype, device=x.device) if out is None else out
+        self._stream_sync()
+        self._check(self.lib.vcr_mx_linear(self.h, ctypes.byref(m), ctypes.byref(w._c()), _bias(bias, w.rows),
+                                           1 if relu else 0, ctypes.byref(_mat(y))))
+        return y
+
+    def mx_linear_grad(self, dy, x, w, y=None, need=(True, True, True)):
+        """(dx, dw, db) of mx_linear from dy (rows, n); y: the output of a call with relu.  dx of dy's type, dw
+        (n, k) and db (n) float32; None where `need` says so."""
+        import torch
+        g = _mat(dy)
+        dx = torch.empty((g.rows, w.cols), dtype=dy.dtype, device=dy.device) if need[0] else None
+        dw = torch.empty((g.cols, x.shape[1]), dtype=torch.float32, device=dy.device) if need[1] else None
+        db = torch.empty((g.cols,), dtype=torch.float32, device=dy.device) if need[2] else None
+        ref = lambda t: None if t is None else ctypes.byref(_mat(t))  # noqa: E731
+        self._stream_sync()
+        self._check(self.lib.vcr_mx_linear_grad(self.h, ctypes.byref(g), ref(y), ref(x if need[1] else None),
+                                                ctypes.byref(w._c()) if need[0] else None, ref(dx), ref(dw),
+                                                None if db is None else _ptr(db)))
+        return dx, dw, db
+
+    def orthogonalize(self, g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, gain=1.0, base=None,
+                      keep=1.0, out=None):
+        """gain X (+ keep base), X the Newton-Schulz orthogonalisation of g (m, n), or of every g[i] of (count, m,
+        n): float32 or bfloat16 CUDA tensors with contiguous rows.  `out` defaults to a tensor of base's type, or
+        g's, and may be base."""
+        import torch
+        if out is None:
+            out = torch.empty(g.shape, dtype=(g if base is None else base).dtype, device=g.device)
+        for t in (base, out):
+            if t is not None and t.shape != g.shape:
+                raise ValueError(f"expected shape {tuple(g.shape)}, got {tuple(t.shape)}")
+        count = g.shape[0] if g.dim() == 3 else 1
+
+        def one(t):
+            return (_mat(t), 0) if t.dim() == 2 else (_mat(t[0] if count else t.view(0, t.shape[2])), t.stride(0))
+        if g.dim() not in (2, 3):
+            raise ValueError("expected a tensor of 2 or 3 dimensions")
+        gm, om = one(g), one(out)
+        bm = (None, 0) if base is None else one(base)
+        o = VcrNsOpts(int(steps), *(float(v) for v in coefficients), float(eps), float(gain), float(keep))
+        self._stream_sync()
+        self._check(self.lib.vcr_orthogonalize(self.h, ctypes.byref(gm[0]), count, gm[1], ctypes.byref(o),
+                                               None if base is None else ctypes.byref(bm[0]), bm[1],
+                                               ctypes.byref(om[0]), om[1]))
+        return out
+
     def layer_bounds(self, relu_id, B):
         import torch
         n = self.relu_sizes[relu_id]
@@ -414,6 +567,24 @@ def _relu_sizes(net):
 
 def _out_size(net):
     return int(net.nodes[-1].W.shape[0])
+
+
+def _mat(t):
+    """A vcr_mat of a 2-d tensor."""
+    import torch
+    kind = {torch.float32: 0, torch.bfloat16: 1}.get(getattr(t, "dtype", None))
+    if kind is None or not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("expected a float32 or bfloat16 CUDA tensor of 2 dimensions with contiguous rows")
+    rows, cols = t.shape
+    # (a single row's stride is of no account)
+    return VcrMat(t.data_ptr(), kind, rows, cols, t.stride(0) if rows > 1 else max(cols, 1))
+
+
+def _bias(b, n):
+    if b is None:
+        return None
+    _check_tensor(b, (n,))
+    return _ptr(b)
 
 
 def _check_tensor(t, shape):
