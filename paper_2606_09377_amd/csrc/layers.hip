@@ -33,44 +33,53 @@ __device__ __forceinline__ int64_t mx_scale_at(int64_t rb, int64_t group, int64_
   return ((rb * ((groups + 3) >> 2) + (group >> 2)) * 64 + lane) * 4 + (group & 3);
 }
 
-// Quantisation: a thread per block.  A workgroup takes 16 rows by 512 columns, a wave one group of
-// 128 columns in lane order.
+// Quantisation.  A workgroup takes 16 rows by 512 columns: a wave reads a row's 512 at once, a thread 8 of
+// them, four threads a block; the codes go through LDS into the storage order.  Bound by memory: 8192 x 8192
+// float32 in QUANT_F32_US us.  (With a thread per block, whose 128 bytes a wave's loads reach in 16-byte
+// pieces of 64 lines, it took 80 us.)
 template <bool BF>
 __global__ __launch_bounds__(256) void k_mx_quantize(DevMat x, int vec, uint8_t *codes, uint8_t *scales) {
-  __shared__ uint8_t sb[256];
+  __shared__ uint32_t cs[4][4][16][4];   // [group][block][row][words]
+  __shared__ uint8_t sb[16][16];         // [block of the 512 columns][row]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t groups = mx_groups(x.cols), n4 = (groups + 3) >> 2;
-  const int64_t rb = blockIdx.x / n4, c4 = blockIdx.x - rb * n4, grp = c4 * 4 + wave;
-  const int64_t row = rb * 16 + (lane & 15), col = grp * 128 + (lane >> 4) * 32;
-  uint32_t byte = 0;
-  if (grp < groups) {
-    float v[4][8];
+  const int64_t rb = blockIdx.x / n4, c4 = blockIdx.x - rb * n4;
+  const int64_t row0 = rb * 16 + wave * 4, col = c4 * 512 + lane * 8;
+  float v[4][8];
+  if (vec && row0 + 4 <= x.rows && c4 * 512 + 512 <= x.cols) {   // uniform: all loads at once
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mat_row8<BF>(x, 0, row0 + i, col, true, v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mat_row8<BF>(x, 0, row0 + i, col, vec, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      mat_row8<BF>(x, 0, row, col + 8 * q, vec, v[q]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[q][i]) & 0x7fffffffu);
-    }
-    const uint32_t e = top >> 23;
-    byte = e == 255 ? 255 : e > 2 ? e - 2 : 0;
+    for (int q = 0; q < 8; ++q) top = max(top, __builtin_bit_cast(uint32_t, v[i][q]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 15, 15, true));
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 15, 15, true));
+    const uint32_t e = top >> 23, byte = e == 255 ? 255 : e > 2 ? e - 2 : 0;
     const float s = mx_scale(byte == 255 ? 127 : byte);
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint32_t u = 0;
-      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[q][0], v[q][1], s, 0);
-      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[q][2], v[q][3], s, 1);
-      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[q][4], v[q][5], s, 2);
-      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[q][6], v[q][7], s, 3);
-      w[q] = u;
-    }
-    *reinterpret_cast<uint4 *>(codes + ((rb * groups + grp) * 64 + lane) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    uint32_t u = 0;
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[i][0], v[i][1], s, 0);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[i][2], v[i][3], s, 1);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[i][4], v[i][5], s, 2);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, v[i][6], v[i][7], s, 3);
+    cs[lane >> 4][(lane >> 2) & 3][wave * 4 + i][lane & 3] = u;
+    if ((lane & 3) == 0) sb[lane >> 2][wave * 4 + i] = (uint8_t)byte;
   }
-  sb[lane * 4 + wave] = (uint8_t)byte;
   __syncthreads();
-  if (wave == 0)
-    *reinterpret_cast<uint32_t *>(scales + (rb * n4 + c4) * 256 + lane * 4) = *reinterpret_cast<uint32_t *>(sb + lane * 4);
+  // thread: group `wave`, slot `lane` (block lane / 16, row lane % 16)
+  const int64_t grp = c4 * 4 + wave;
+  if (grp < groups)
+    *reinterpret_cast<uint4 *>(codes + ((rb * groups + grp) * 64 + lane) * 16) = *reinterpret_cast<uint4 *>(cs[wave][lane >> 4][lane & 15]);
+  if (wave == 0) {
+    const int g = lane >> 4, r = lane & 15;
+    *reinterpret_cast<uint32_t *>(scales + (rb * n4 + c4) * 256 + lane * 4) =
+        sb[g][r] | (uint32_t)sb[4 + g][r] << 8 | (uint32_t)sb[8 + g][r] << 16 | (uint32_t)sb[12 + g][r] << 24;
+  }
 }
 
 // The values of a lane's block: 32 consecutive ones of a row
@@ -85,25 +94,38 @@ __device__ __forceinline__ uint4 mx_to_bf16(uint32_t u, float s) {   // eight va
                     c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 2)), c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 3)));
 }
 
+// The reverse, with the same division of work
 template <bool BF>
 __global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t ld, int vec) {
-  const int lane = threadIdx.x & 63;
-  const int64_t groups = mx_groups(w.cols), id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t rb = id / groups, grp = id - rb * groups, row = rb * 16 + (lane & 15), col = grp * 128 + (lane >> 4) * 32;
-  if (row >= w.rows) return;
-  uint4 q;
-  float s;
-  mx_block(w, rb, grp, groups, lane, q, s);
-  const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+  __shared__ uint32_t cs[4][4][16][4];
+  __shared__ float ss[16][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t groups = mx_groups(w.cols), n4 = (groups + 3) >> 2;
+  const int64_t rb = blockIdx.x / n4, c4 = blockIdx.x - rb * n4, grp = c4 * 4 + wave;
+  if (grp < groups) {
+    uint4 q;
+    float s;
+    mx_block(w, rb, grp, groups, lane, q, s);
+    *reinterpret_cast<uint4 *>(cs[wave][lane >> 4][lane & 15]) = q;
+    ss[wave * 4 + (lane >> 4)][lane & 15] = s;
+  }
+  __syncthreads();
+  const int64_t col = c4 * 512 + lane * 8;
+  if (col >= w.cols) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint4 b = mx_to_bf16(u[i], s);
+    const int r = wave * 4 + i;
+    const uint4 b = mx_to_bf16(cs[lane >> 4][(lane >> 2) & 3][r][lane & 3], ss[lane >> 2][r]);
+    if (BF && vec == 2 && rb * 16 + r < w.rows && col + 8 <= w.cols) {
+      *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(y) + (rb * 16 + r) * ld + col) = b;
+      continue;
+    }
     const uint32_t h[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const f32v4 v = {__builtin_bit_cast(float, h[2 * k] << 16), __builtin_bit_cast(float, h[2 * k] & 0xffff0000u),
                        __builtin_bit_cast(float, h[2 * k + 1] << 16), __builtin_bit_cast(float, h[2 * k + 1] & 0xffff0000u)};
-      store_row4(y, BF, ld, w.rows, w.cols, vec, row, col + 8 * i + 4 * k, v);
+      store_row4(y, BF, ld, w.rows, w.cols, vec, rb * 16 + r, col + 4 * k, v);
     }
   }
 }
@@ -292,6 +314,192 @@ static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipS
   return hipGetLastError();
 }
 
+// ---- few rows ---------------------------------------------------------------------------------
+// y = act(x w^T + bias) for at most 16 rows x: bound by reading the weights once.  A workgroup takes RB row
+// blocks of weights; its 8 waves go through their groups of 128 columns in turn, each with the next ones'
+// loads in flight, and the partial sums are added in LDS in wave order.  The matrix instruction does 16 rows
+// for the price of one, so one path serves 1 to 16.
+//   P = 3, 1: x's parts are made once per workgroup in LDS, [chunk of 32][part][8 columns][row]: only the M real
+//   rows; lanes of further rows read the last one, and their results are not stored.  The weights are expanded in
+//   registers: a lane has 32 columns of its row, of which instruction s takes the s-th eight, so the contraction's order
+//   is 8 columns of each of the group's four blocks at a time, alike for both operands.
+//   P = 0: x is in 4 bits, its fragments are read as they are (1 KB a group, shared by RB blocks of weights).
+// Columns that do not fit LDS together are taken in slices of `slice` groups.
+template <int P, bool BF>
+__device__ __forceinline__ void rows_stage(const DevMat &x, int vec, int M, int64_t g0, int n, uint8_t *lds) {
+  for (int it = threadIdx.x; it < n * 16 * M; it += 512) {
+    const int m = it / (n * 16), o = it - m * (n * 16);
+    float v[8];
+    mat_row8<BF>(x, 0, m, g0 * 128 + o * 8, vec, v);
+    uint32_t w[4][P];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) parts_of<P>(v[2 * i], v[2 * i + 1], w[i]);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *reinterpret_cast<uint4 *>(lds + ((((o >> 2) * P + p) * 4 + (o & 3)) * M + m) * 16) = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
+  }
+}
+
+template <int P, int RB, bool BF>
+__global__ __launch_bounds__(512, 2) void k_rows(DevMat x, int vec, MxDev a, MxDev w, int M, int slice, int z_groups, OutMat o, float *part) {
+  constexpr int U = RB == 1 ? 4 : 2;   // groups of a wave's batch
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
+  f32v4 *red = reinterpret_cast<f32v4 *>(rows_lds);   // [RB][8 waves][64]
+  uint8_t *lds = rows_lds + RB * 8 * 64 * 16;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t groups = mx_groups(w.cols), n4 = (groups + 3) >> 2, blocks = (w.rows + 15) >> 4;
+  const int64_t g0 = (int64_t)blockIdx.y * z_groups, g1 = min(groups, g0 + z_groups);
+  const int mr = min(r, M - 1);
+  const bool whole = g1 - g0 <= slice;
+  bool staged = false;
+  for (int64_t b0 = (int64_t)blockIdx.x * RB; b0 < blocks; b0 += (int64_t)gridDim.x * RB) {
+    f32v4 hi[RB], lo[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) hi[b] = lo[b] = f32v4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t s0 = g0; s0 < g1; s0 += slice) {
+      const int n = (int)min((int64_t)slice, g1 - s0);
+      i32x4 q[2][U][RB];
+      uint32_t sc[2][U][RB];
+      i32x4 qa[2][U];
+      uint32_t sa[2][U];
+      auto load = [&](int gi, int buf) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t gr = s0 + min(gi + 8 * u, n - 1);
+          if constexpr (P == 0) {
+            qa[buf][u] = *reinterpret_cast<const i32x4 *>(a.codes + (gr * 64 + lane) * 16);
+            sa[buf][u] = *reinterpret_cast<const uint32_t *>(a.scales + ((gr >> 2) * 64 + lane) * 4);
+          }
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            const int64_t rb = min(b0 + b, blocks - 1);
+            q[buf][u][b] = *reinterpret_cast<const i32x4 *>(w.codes + ((rb * groups + gr) * 64 + lane) * 16);
+            sc[buf][u][b] = *reinterpret_cast<const uint32_t *>(w.scales + ((rb * n4 + (gr >> 2)) * 64 + lane) * 4);
+          }
+        }
+      };
+      auto multiply = [&](int gi, int buf) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (gi + 8 * u >= n) break;   // wave-uniform
+          const int sh = 8 * (int)((s0 + gi + 8 * u) & 3);
+          if constexpr (P == 0) {
+            const i32x4 av = qa[buf][u];
+            const i32x8 aw = {av[0], av[1], av[2], av[3], 0, 0, 0, 0};
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+              const i32x4 bv = q[buf][u][b];
+              const i32x8 bw = {bv[0], bv[1], bv[2], bv[3], 0, 0, 0, 0};
+              hi[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw, aw, hi[b], 4, 4, 0, (int)(sc[buf][u][b] >> sh), 0,
+                                                                       (int)(sa[buf][u] >> sh));
+            }
+          } else {
+            float s[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) s[b] = mx_scale((sc[buf][u][b] >> sh) & 255);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              bf16x8 av[P];
+#pragma unroll
+              for (int p = 0; p < P; ++p)
+                av[p] = *reinterpret_cast<const bf16x8 *>(lds + (((((gi + 8 * u) * 4 + g) * P + p) * 4 + i) * M + mr) * 16);
+#pragma unroll
+              for (int b = 0; b < RB; ++b) {
+                const bf16x8 bw = __builtin_bit_cast(bf16x8, mx_to_bf16((uint32_t)q[buf][u][b][i], s[b]));
+                if constexpr (P == 3) {
+                  lo[b] = mfma_bf16(bw, av[2], lo[b]);
+                  lo[b] = mfma_bf16(bw, av[1], lo[b]);
+                }
+                hi[b] = mfma_bf16(bw, av[0], hi[b]);
+              }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);   // (a batch's reads of LDS all ahead of its products need more registers than there are)
+        }
+      };
+      load(wave, 0);   // ahead of the rows' staging
+      if constexpr (P > 0) {
+        if (!staged) {
+          if (s0 > g0 || b0 != (int64_t)blockIdx.x * RB) __syncthreads();   // the last slice has been read
+          rows_stage<P, BF>(x, vec, M, s0, n, lds);
+          __syncthreads();
+          staged = whole;
+        }
+      }
+      for (int gi = wave; gi < n; gi += 16 * U) {
+        if (gi + 8 * U < n) load(gi + 8 * U, 1);
+        multiply(gi, 0);
+        if (gi + 16 * U < n) load(gi + 16 * U, 0);
+        if (gi + 8 * U < n) multiply(gi + 8 * U, 1);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      f32v4 v = hi[b];
+      if constexpr (P == 3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < __builtin_huge_valf() ? v[i] + lo[b][i] : v[i];
+      }
+      red[(b * 8 + wave) * 64 + lane] = v;
+    }
+    __syncthreads();
+    for (int b = wave; b < RB; b += 8) {
+      f32v4 v = red[b * 512 + lane];
+      for (int k = 1; k < 8; ++k) v += red[b * 512 + k * 64 + lane];
+      const int64_t n = (b0 + b) * 16 + 4 * g;
+      if (r < M && b0 + b < blocks) {
+        if (part) *reinterpret_cast<f32v4 *>(part + ((int64_t)blockIdx.y * M + r) * (blocks * 16) + n) = v;
+        else o.put(r, n, v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int ROWS_MAX = 16;
+struct RowsPlan {
+  int rb, parts, slice;
+  int64_t wgs, z_groups;
+  size_t lds, part_bytes;
+};
+// A workgroup of 8 waves per compute unit or more; the contraction is divided among workgroups only where there are too
+// few row blocks for that and every wave keeps 4 groups.
+static RowsPlan rows_plan(int P, int64_t M, int64_t N, int64_t groups) {
+  RowsPlan p{};
+  const int64_t blocks = blocks_of(N, 16);
+  p.rb = blocks >= 4096 ? 4 : blocks >= 512 ? 2 : 1;
+  p.wgs = std::min<int64_t>(blocks_of(blocks, p.rb), 1024);
+  const int64_t z = std::max<int64_t>(1, std::min<int64_t>(256 / p.wgs, groups / 32));
+  p.z_groups = blocks_of(groups, z);
+  p.parts = (int)blocks_of(groups, p.z_groups);
+  const size_t per = (size_t)M * 256 * P;   // bytes of a group's rows
+  const size_t room = per * 16 > 64 << 10 ? 112 << 10 : 56 << 10;
+  p.slice = P == 0 ? (int)p.z_groups : (int)std::min<int64_t>(p.z_groups, std::max<int64_t>(8, room / per / 8 * 8));
+  p.lds = (size_t)p.rb * 8 * 64 * 16 + (P == 0 ? 0 : per * p.slice);
+  p.part_bytes = p.parts > 1 ? (size_t)p.parts * M * blocks * 64 : 0;
+  return p;
+}
+template <int P, bool BF>
+static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, const RowsPlan &p, const OutMat &o, float *part, hipStream_t s) {
+  const int vec = x.p && rows_aligned(x.p, x.ld, BF ? 2 : 4), M = (int)o.rows;
+  const dim3 grid((unsigned)p.wgs, (unsigned)p.parts);
+  if (p.parts == 1) part = nullptr;
+  auto go = [&](auto kernel) {
+    if (p.lds > 64 << 10) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid, dim3(512), p.lds, s, x, vec, a, w, M, p.slice, (int)p.z_groups, o, part);
+    return hipGetLastError();
+  };
+  hipError_t e = p.rb == 4 ? go(k_rows<P, 4, BF>) : p.rb == 2 ? go(k_rows<P, 2, BF>) : go(k_rows<P, 1, BF>);
+  if (e != hipSuccess || !part) return e;
+  const int64_t ld = blocks_of(o.cols, 16) * 16;
+  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
+  return hipGetLastError();
+}
+
 static hipError_t launch_planes(const DevMat &x, const DevMat &y, int parts, int64_t chunks, uint8_t *out, hipStream_t s) {
   const int bytes = x.bf16 ? 2 : 4;
   const int vec = rows_aligned(x.p, x.ld, bytes) && (!y.p || rows_aligned(y.p, y.ld, bytes));
@@ -444,8 +652,9 @@ vcr_status vcr_mx_dequantize(vcr_ctx *c, const vcr_mx *q, const vcr_mat *y) {
   TRY(op_begin(c));
   if (y->rows == 0) return VCR_OK;
   const OutMat o = out_mat(y, nullptr, 0);
-  const int64_t wg = blocks_of(blocks_of(y->rows, 16) * mx_groups(y->cols), 4);
-  if (o.bf16) hipLaunchKernelGGL((k_mx_dequantize<true>), dim3((unsigned)wg), dim3(256), 0, c->stream, dev(q), y->p, y->ld, o.vec);
+  const int64_t wg = blocks_of(y->rows, 16) * blocks_of(mx_groups(y->cols), 4);
+  const int vec = o.bf16 && rows_aligned(y->p, y->ld, 2) ? 2 : o.vec;   // 16-byte rows of bf16: 8 columns a store
+  if (o.bf16) hipLaunchKernelGGL((k_mx_dequantize<true>), dim3((unsigned)wg), dim3(256), 0, c->stream, dev(q), y->p, y->ld, vec);
   else hipLaunchKernelGGL((k_mx_dequantize<false>), dim3((unsigned)wg), dim3(256), 0, c->stream, dev(q), y->p, y->ld, o.vec);
   HIP_TRY(c, hipGetLastError());
   return op_end(c);
@@ -463,6 +672,13 @@ vcr_status vcr_mx_product(vcr_ctx *c, const vcr_mx *a, const vcr_mx *w, const fl
                 (long long)y->cols, (long long)a->rows, (long long)a->cols, (long long)w->rows, (long long)w->cols);
   TRY(op_begin(c));
   if (y->rows == 0) return VCR_OK;
+  if (y->rows <= ROWS_MAX) {
+    const RowsPlan p = rows_plan(0, y->rows, y->cols, mx_groups(a->cols));
+    Workspace *ws = nullptr;
+    TRY(op_space(c, p.part_bytes, &ws));
+    HIP_TRY(c, (launch_rows<0, false>(DevMat{}, dev(a), dev(w), p, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
+    return op_end(c);
+  }
   NtArgs g{};
   g.A = NtOperand{a->codes, a->scales, (int32_t)blocks_of(a->rows, 16), 0};
   g.B = NtOperand{w->codes, w->scales, (int32_t)blocks_of(w->rows, 16), 0};
@@ -488,6 +704,15 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
   if (y->rows == 0) return VCR_OK;
   const DevMat d = dev(x);
   const int P = d.bf16 ? 1 : 3;
+  if (y->rows <= ROWS_MAX) {
+    const RowsPlan p = rows_plan(P, y->rows, y->cols, mx_groups(x->cols));
+    Workspace *ws = nullptr;
+    TRY(op_space(c, p.part_bytes, &ws));
+    float *part = reinterpret_cast<float *>(ws->base);
+    if (d.bf16) HIP_TRY(c, (launch_rows<1, true>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
+    else HIP_TRY(c, (launch_rows<3, false>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
+    return op_end(c);
+  }
   const int64_t chunks = 4 * mx_groups(x->cols), rb = blocks_of(x->rows, 16), wb = blocks_of(w->rows, 16);
   const NtPlan plan = d.bf16 ? nt_plan<1, 1, false>(y->rows, y->cols, chunks) : nt_plan<3, 1, false>(y->rows, y->cols, chunks);
   const size_t xb = (size_t)rb * chunks * P * FRAG, wbytes = (size_t)wb * chunks * FRAG;

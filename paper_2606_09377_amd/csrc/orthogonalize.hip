@@ -19,26 +19,33 @@
 
 namespace vcr {
 
-constexpr int NORM_PARTS = 64;   // partial sums of a matrix's squares
+constexpr int NORM_PARTS = 1024;   // partial sums of a matrix's squares
 
+// Sums of squares in 64 bits (float32's range does not hold the squares of all its values): a wave per stretch of 512
+// columns of a row
 template <bool BF>
-__global__ __launch_bounds__(256) void k_ns_norm(DevMat g, double *part) {
+__global__ __launch_bounds__(256) void k_ns_norm(DevMat g, int vec, double *part) {
   __shared__ double sh[4];
-  const int64_t base = (int64_t)blockIdx.y * g.stride, total = g.rows * g.cols;
+  const int lane = threadIdx.x & 63;
+  const int64_t base = (int64_t)blockIdx.y * g.stride, per = (g.cols + 511) / 512, total = g.rows * per;
   double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += NORM_PARTS * 256) {
-    const int64_t r = i / g.cols;
-    const float x = mat_at<BF>(g, base, r, i - r * g.cols);
-    s += (double)x * x;
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < total; i += NORM_PARTS * 4) {
+    const int64_t r = i / per;
+    float v[8];
+    mat_row8<BF>(g, base, r, (i - r * per) * 512 + lane * 8, vec, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s = fma((double)v[q], (double)v[q], s);
   }
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  if (lane == 0) sh[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) part[blockIdx.y * NORM_PARTS + blockIdx.x] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 // 1 / (norm + eps), by every wave
 __device__ __forceinline__ float ns_scale(const double *part, int batch, float eps) {
-  double s = part[batch * NORM_PARTS + (threadIdx.x & 63)];
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < NORM_PARTS / 64; ++i) s += part[batch * NORM_PARTS + i * 64 + (threadIdx.x & 63)];
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
   return (float)(1.0 / (sqrt(s) + (double)eps));
 }
@@ -161,7 +168,7 @@ template <int P, bool BF>
 static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, bool transposed, int steps, NsEpilogue e, float eps,
                          NsSpace sp, hipStream_t s) {
   const int vec = rows_aligned(g.p, g.ld, BF ? 2 : 4) && (g.stride * (BF ? 2 : 4)) % 16 == 0;
-  hipLaunchKernelGGL((k_ns_norm<BF>), dim3(NORM_PARTS, batch), dim3(256), 0, s, g, sp.norm);
+  hipLaunchKernelGGL((k_ns_norm<BF>), dim3(NORM_PARTS, batch), dim3(256), 0, s, g, vec, sp.norm);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   // G's rows padded to rp, its columns to cp
