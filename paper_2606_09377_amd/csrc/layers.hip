@@ -9,7 +9,6 @@
 // block of columns 32 g .. 32 g + 31 of row r, the first value in the low bits; scales [rows /
 // 16][cols / 512][64 lanes][4 groups of 128 columns].  Rows are padded to 16 and columns to 128 with zeros.
 #include <algorithm>
-#include <type_traits>
 
 #include "ctx.h"
 #include "layers.h"
@@ -271,46 +270,31 @@ __global__ __launch_bounds__(256) void k_join(const float *p, int parts, int64_t
   o.put(m, n, v);
 }
 
-// ---- choice of tiles --------------------------------------------------------------------------
+// ---- products by tiles ------------------------------------------------------------------------
+// Parts of the contraction: few tiles of the smallest shape over a long contraction leave compute units idle; parts of
+// 16 chunks and more are then summed by their own workgroups and joined in order.
 template <int PA, int PB, bool FP4>
-struct Tiles {
-  static constexpr int KS = PA == 1 ? 2 : 1;
-  typedef std::conditional_t<PA == 3, NtTile<4, 4, 4, 2, PA, PB, KS, FP4>, NtTile<8, 4, 2, 4, PA, PB, KS, FP4>> L;
-  typedef std::conditional_t<PB == 3, NtTile<4, 2, 2, 4, PA, PB, KS, FP4>, NtTile<4, 4, 2, 2, PA, PB, KS, FP4>> M;
-  typedef NtTile<2, 2, 2, 2, PA, PB, KS, FP4> S;
-};
-static int64_t tiles_of(int64_t m, int64_t n, int bm, int bn) { return blocks_of(m, bm) * blocks_of(n, bn); }
-
-// 0: L, 1: M, 2: S; parts of the contraction (S only)
-struct NtPlan {
-  int kind, parts;
-  size_t part_bytes(int64_t M, int64_t N) const { return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0; }
-};
+static int nt_parts(int64_t M, int64_t N, int64_t chunks) {
+  const NtShape &x = NtTiles<PA, PB, FP4>::shapes[NT_SHAPES - 1];
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / nt_tiles(M, N, x.bm, x.bn, false), chunks / 16));
+}
 template <int PA, int PB, bool FP4>
-static NtPlan nt_plan(int64_t M, int64_t N, int64_t chunks) {
-  typedef Tiles<PA, PB, FP4> TS;
-  if (tiles_of(M, N, TS::L::BM, TS::L::BN) >= 200) return {0, 1};
-  if (tiles_of(M, N, TS::M::BM, TS::M::BN) >= 200) return {1, 1};
-  const int64_t t = tiles_of(M, N, TS::S::BM, TS::S::BN), steps = blocks_of(chunks, TS::S::KS);
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / 8));
-  return {2, (int)parts};
+static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
+  const int parts = nt_parts<PA, PB, FP4>(M, N, chunks);
+  return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
 }
-template <int PA, int PB, bool FP4, class EPI>
-static hipError_t nt_kind(int kind, const NtArgs &g, int64_t M, int64_t N, int parts, const EPI &e, hipStream_t s) {
-  typedef Tiles<PA, PB, FP4> TS;
-  if (kind == 0) return launch_nt<typename TS::L>(g, M, N, 1, parts, e, s);
-  if (kind == 1) return launch_nt<typename TS::M>(g, M, N, 1, parts, e, s);
-  return launch_nt<typename TS::S>(g, M, N, 1, parts, e, s);
-}
-// D = A B^T into o; part: room for nt_plan's partial sums
+// D = A B^T into o; part: room for part_bytes
 template <int PA, int PB, bool FP4>
 static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipStream_t s) {
-  const NtPlan p = nt_plan<PA, PB, FP4>(o.rows, o.cols, g.chunks);
-  if (p.parts == 1) return nt_kind<PA, PB, FP4>(p.kind, g, o.rows, o.cols, 1, EpiOut{o}, s);
+  typedef NtTiles<PA, PB, FP4> TS;
+  const int parts = nt_parts<PA, PB, FP4>(o.rows, o.cols, g.chunks);
+  if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, EpiOut{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
-  const hipError_t e = nt_kind<PA, PB, FP4>(p.kind, g, o.rows, o.cols, p.parts, EpiPart{part, o.rows, ld}, s);
+  const NtShape &x = TS::shapes[NT_SHAPES - 1];
+  const hipError_t e = launch_nt<typename TS::T4>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,
+                                                  EpiPart{part, o.rows, ld}, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
+  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, parts, o.rows, ld, o);
   return hipGetLastError();
 }
 
@@ -684,7 +668,7 @@ vcr_status vcr_mx_product(vcr_ctx *c, const vcr_mx *a, const vcr_mx *w, const fl
   g.B = NtOperand{w->codes, w->scales, (int32_t)blocks_of(w->rows, 16), 0};
   g.chunks = (int32_t)mx_groups(a->cols);
   Workspace *ws = nullptr;
-  const size_t room = nt_plan<1, 1, true>(y->rows, y->cols, g.chunks).part_bytes(y->rows, y->cols);
+  const size_t room = part_bytes<1, 1, true>(y->rows, y->cols, g.chunks);
   TRY(op_space(c, room, &ws));
   HIP_TRY(c, (nt_product<1, 1, true>(g, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
   return op_end(c);
@@ -714,10 +698,10 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
     return op_end(c);
   }
   const int64_t chunks = 4 * mx_groups(x->cols), rb = blocks_of(x->rows, 16), wb = blocks_of(w->rows, 16);
-  const NtPlan plan = d.bf16 ? nt_plan<1, 1, false>(y->rows, y->cols, chunks) : nt_plan<3, 1, false>(y->rows, y->cols, chunks);
+  const size_t room = d.bf16 ? part_bytes<1, 1, false>(y->rows, y->cols, chunks) : part_bytes<3, 1, false>(y->rows, y->cols, chunks);
   const size_t xb = (size_t)rb * chunks * P * FRAG, wbytes = (size_t)wb * chunks * FRAG;
   Workspace *ws = nullptr;
-  TRY(op_space(c, al(xb) + al(wbytes) + al(plan.part_bytes(y->rows, y->cols)), &ws));
+  TRY(op_space(c, al(xb) + al(wbytes) + al(room), &ws));
   uint8_t *xp = take<uint8_t>(*ws, xb), *wp = take<uint8_t>(*ws, wbytes);
   float *part = reinterpret_cast<float *>(ws->base + ws->used);
   HIP_TRY(c, launch_planes(d, dev(static_cast<const vcr_mat *>(nullptr)), P, chunks, xp, c->stream));
@@ -762,12 +746,12 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
   if (has_dx) {
     b_g = (size_t)mb * nch * P * FRAG;
     b_wt = (size_t)kxb * nch * FRAG;
-    b_part = (P == 1 ? nt_plan<1, 1, false>(M, kx, nch) : nt_plan<3, 1, false>(M, kx, nch)).part_bytes(M, kx);
+    b_part = P == 1 ? part_bytes<1, 1, false>(M, kx, nch) : part_bytes<3, 1, false>(M, kx, nch);
   }
   if (dw) {
     b_gt = (size_t)nb * mch * P * FRAG;
     b_xt = (size_t)kwb * mch * P * FRAG;
-    b_part = std::max(b_part, (P == 1 ? nt_plan<1, 1, false>(N, kw, mch) : nt_plan<3, 3, false>(N, kw, mch)).part_bytes(N, kw));
+    b_part = std::max(b_part, P == 1 ? part_bytes<1, 1, false>(N, kw, mch) : part_bytes<3, 3, false>(N, kw, mch));
   }
   if (db) b_sums = (size_t)mch * N * 4;
   Workspace *ws = nullptr;

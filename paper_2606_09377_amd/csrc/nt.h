@@ -17,12 +17,20 @@
 // Where a bar stands, the small products have an accumulator of their own, added at the end: summed into
 // the large one they are cut off at its precision, always downwards (split_bf16.h).
 //
-// A workgroup owns BM x BN outputs, WM x WN waves of MB x NB blocks of 16 x 16.  A stage holds KS
-// chunks of its rows; two stages are in LDS, the next one's loads run while one is multiplied, and the
-// one barrier of a stage both publishes it and frees the other.  The 16 x 16 x 32 (x 128 for 4-bit)
+// A workgroup owns BM x BN outputs: WM x WN x WK waves of MB x NB blocks of 16 x 16, of which WK share a
+// block and take every WK-th chunk (their sums are added in LDS, in order).  A stage holds KS chunks of
+// its rows; NS stages are in LDS, the later ones' loads run while one is multiplied, and the one barrier
+// of a stage both publishes it and frees the one before.  A stage's operands are read into registers
+// while the stage before is multiplied, and those reads and the loads of a later stage are spread between the
+// matrix instructions: a wave issues in order and would stand still until LDS and the memory pipe had taken them
+// all.  (256 x 256 tiles of one part over 96 chunks: 1220 TFLOP/s with them in one piece, 1520 spread; 64 x 64 of
+// three parts 760 and 1240.)  The 16 x 16 x 32 (x 128 for 4-bit)
 // instruction takes 16 cycles of its SIMD and 1 KB of each operand; MB x NB of them share MB + NB reads
 // of LDS, which at 128 bytes a cycle is what bounds small wave tiles.
 #pragma once
+
+#include <algorithm>
+#include <type_traits>
 
 #include "lds_dma.h"
 #include "split_bf16.h"
@@ -43,24 +51,32 @@ struct NtOperand {
 };
 struct NtArgs {
   NtOperand A, B;
-  int32_t chunks;      // of the contraction
-  int32_t n_mt, n_nt;  // tiles
-  int32_t tri;         // only the tiles that hold a block on or below the diagonal
-  int32_t z_chunks;    // chunks of one part of the contraction (a multiple of KS; grid z parts)
+  int32_t chunks;       // of the contraction
+  int32_t tri;          // only the tiles that hold a block on or below the diagonal
+  int32_t z_chunks;     // chunks of one part of the contraction (a multiple of KS; grid y parts)
+  // Tiles are counted in a shape of bm x bn, n_mt x n_nt of them and `tiles` in use per matrix of a batch.  A
+  // launch takes those from `first` on, each as sub_m x sub_n of its own.
+  int32_t bm, bn, n_mt, n_nt, tiles, first, sub_m, sub_n;
 };
 
-template <int MB_, int NB_, int WM_, int WN_, int PA_, int PB_, int KS_, bool FP4_ = false>
+template <int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_, bool FP4_ = false>
 struct NtTile {
-  static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, PA = PA_, PB = PB_, KS = KS_;
+  static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, PA = PA_, PB = PB_, KS = KS_, NS = NS_;
   static constexpr bool FP4 = FP4_;
-  static constexpr int NW = WM * WN, T = 64 * NW;
+  static constexpr int PRODUCTS = PA == 3 && PB == 3 ? 6 : PA > 1 ? 3 : 1;
+  static constexpr int KW = KS / WK;   // chunks of a stage that a wave multiplies
+  static constexpr int NW = WM * WN * WK, T = 64 * NW;
   static constexpr int BM = 16 * MB * WM, BN = 16 * NB * WN;
   static constexpr bool TWO = PA == 3;   // an accumulator for the small products
   static constexpr int FA = BM / 16 * KS * PA, FB = BN / 16 * KS * PB;   // fragments of a stage
   static constexpr int SA = FP4 ? BM / 16 : 0, SB = FP4 ? BN / 16 : 0;   // scale loads (256 bytes) of a stage
+  static constexpr int SQ = (SA + SB + NW - 1) / NW;                     // of a wave (the last ones' may be the same)
+  static constexpr int LOADS = (FA + FB) / NW + SQ;                      // of a wave
   static constexpr int STAGE = (FA + FB) * FRAG + (SA + SB) * 256;
-  static_assert(FA % NW == 0 && FB % NW == 0 && SA % NW == 0 && SB % NW == 0, "loads spread evenly over the waves");
-  static_assert(!FP4 || (4 % KS == 0), "a stage's scales are in one group of four chunks");
+  static constexpr int LDS = NS * STAGE;
+  static_assert(FA % NW == 0 && FB % NW == 0, "loads spread evenly over the waves");
+  static_assert(!FP4 || 4 % KS == 0, "a stage's scales are in one group of four chunks");
+  static_assert(KS % WK == 0 && (WK == 1 || NW * MB * NB * 1024 <= LDS), "waves that share a block");
 };
 
 // 4 bytes a lane from a wave-uniform base into LDS (dma16's form)
@@ -95,87 +111,116 @@ __device__ __forceinline__ f32v4 quad_transpose(f32v4 v, int lane) {
   return v;
 }
 
+// Columns of tiles in use of row mt of tiles: with tri, those up to its last row's diagonal
+__host__ __device__ inline int nt_row_tiles(int mt, int bm, int bn, int n_nt, bool tri) {
+  const int n = (int)(((int64_t)(mt + 1) * bm + bn - 1) / bn);
+  return tri && n < n_nt ? n : n_nt;
+}
 // The tile of a workgroup.  Workgroup ids go round the 8 XCDs; each XCD gets a contiguous range of
 // tiles in an order in which 4 rows of tiles sweep the columns together, so that its L2 serves them.
-template <class T>
-__device__ __forceinline__ void nt_tile(const NtArgs &g, int id, int total, int &mt, int &nt) {
+__device__ __forceinline__ void nt_tile(const NtArgs &g, int id, int total, int &batch, int &mt, int &nt) {
   const int x = id & 7, t = id >> 3, q = total >> 3, rem = total & 7;
-  const int at = x * q + min(x, rem) + t;
+  const int at = x * q + min(x, rem) + t, subs = g.sub_m * g.sub_n, par = g.first + at / subs, sub = at % subs;
+  batch = par / g.tiles;
+  int left = par - batch * g.tiles;
   if (!g.tri) {
-    const int per = 4 * g.n_nt, first = at / per * 4, rows = min(4, g.n_mt - first), i = at - first * g.n_nt;
+    const int per = 4 * g.n_nt, first = left / per * 4, rows = min(4, g.n_mt - first), i = left - first * g.n_nt;
     mt = first + i % rows;
     nt = i / rows;
-    return;
+  } else {
+    mt = 0;
+    for (;;) {
+      const int n = nt_row_tiles(mt, g.bm, g.bn, g.n_nt, true);
+      if (left < n || mt + 1 == g.n_mt) break;
+      left -= n;
+      ++mt;
+    }
+    nt = left;
   }
-  // row mt has the tiles nt whose first column is within or left of its last row
-  int left = at;
-  mt = 0;
-  for (;;) {
-    const int n = min(g.n_nt, ((mt + 1) * T::BM + T::BN - 1) / T::BN);
-    if (left < n || mt + 1 == g.n_mt) break;
-    left -= n;
-    ++mt;
-  }
-  nt = left;
-}
-template <class T>
-int nt_tiles(int n_mt, int n_nt, bool tri) {
-  if (!tri) return n_mt * n_nt;
-  int s = 0;
-  for (int mt = 0; mt < n_mt; ++mt) {
-    const int n = ((mt + 1) * T::BM + T::BN - 1) / T::BN;
-    s += n < n_nt ? n : n_nt;
-  }
-  return s;
+  mt = mt * g.sub_m + sub % g.sub_m;
+  nt = nt * g.sub_n + sub / g.sub_m;
 }
 
 // EPI: a struct with store(batch, part of the contraction, m, n, values of n .. n + 3, lane): called by
 // whole waves for every block, with the lane's row m and first column n; the other lanes of a block hold
 // its other rows and columns.
 template <class T, class EPI>
-__global__ __launch_bounds__(T::T, 2) void k_nt(const NtArgs g, const EPI epi) {
-  constexpr int MB = T::MB, NB = T::NB, NW = T::NW, KS = T::KS, PA = T::PA, PB = T::PB;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * T::STAGE];
+__global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2) void k_nt(const NtArgs g, const EPI epi) {
+  constexpr int MB = T::MB, NB = T::NB, NW = T::NW, KS = T::KS, NS = T::NS, PA = T::PA, PB = T::PB;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[T::LDS];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave % T::WM, wn = wave / T::WM;
-  int mt, nt;
-  nt_tile<T>(g, blockIdx.x, gridDim.x, mt, nt);
+  const int wm = wave % T::WM, wn = wave / T::WM % T::WN, wk = wave / (T::WM * T::WN);
+  int batch, mt, nt;
+  nt_tile(g, blockIdx.x, gridDim.x, batch, mt, nt);
   const int rb0 = mt * (T::BM / 16), cb0 = nt * (T::BN / 16);
-  const uint8_t *Ap = g.A.p + (int64_t)blockIdx.y * g.A.stride;
-  const uint8_t *Bp = g.B.p + (int64_t)blockIdx.y * g.B.stride;
-  const int kc0 = blockIdx.z * g.z_chunks, kc1 = min(g.chunks, kc0 + g.z_chunks);
+  // (parts of a larger tile may lie outside)
+  if (rb0 >= g.A.row_blocks || cb0 >= g.B.row_blocks || (g.tri && cb0 >= rb0 + T::BM / 16)) return;
+  const int kc0 = blockIdx.y * g.z_chunks, kc1 = min(g.chunks, kc0 + g.z_chunks);
   const int KT = (kc1 - kc0 + KS - 1) / KS;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)lds;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)lds + wave * FRAG;
 
+  // Loads: a wave-uniform address of the tile's first row block and the stage, and each load's own offset from it,
+  // formed once (32 bits: launch_nt).  Row blocks beyond the last one read that.  (Forming the addresses anew for every
+  // load cost a wave that has its SIMD to itself as much time as its products.)
+  const uint8_t *a_base = g.A.p + batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG;
+  const uint8_t *b_base = g.B.p + batch * g.B.stride + ((int64_t)cb0 * g.chunks + kc0) * PB * FRAG;
+  uint32_t a_off[T::FA / NW], b_off[T::FB / NW];
+#pragma unroll
+  for (int q = 0; q < T::FA / NW; ++q) {
+    const int f = q * NW + wave, i = f / (KS * PA), kp = f - i * (KS * PA);
+    a_off[q] = ((uint32_t)min(i, g.A.row_blocks - 1 - rb0) * g.chunks * PA + kp) * FRAG + lane * 16;
+  }
+#pragma unroll
+  for (int q = 0; q < T::FB / NW; ++q) {
+    const int f = q * NW + wave, i = f / (KS * PB), kp = f - i * (KS * PB);
+    b_off[q] = ((uint32_t)min(i, g.B.row_blocks - 1 - cb0) * g.chunks * PB + kp) * FRAG + lane * 16;
+  }
+  // scales: of four chunks together
+  const int c4 = (g.chunks + 3) / 4;
+  const uint8_t *s_base[T::FP4 ? T::SQ : 1];
+  if constexpr (T::FP4) {
+#pragma unroll
+    for (int q = 0; q < T::SQ; ++q) {
+      const int i = min(q * NW + wave, T::SA + T::SB - 1);
+      s_base[q] = i < T::SA ? g.A.scales + (int64_t)min(rb0 + i, g.A.row_blocks - 1) * c4 * 256
+                            : g.B.scales + (int64_t)min(cb0 + i - T::SA, g.B.row_blocks - 1) * c4 * 256;
+    }
+  }
+
+  struct Stage {   // wave-uniform addresses of a stage's loads
+    const uint8_t *a, *b;
+    uint32_t lds;
+    int at4, over;   // over: chunks of the stage beyond the contraction
+  };
+  auto stage = [&](int kt, int buf) {
+    return Stage{a_base + (int64_t)kt * (KS * PA * FRAG), b_base + (int64_t)kt * (KS * PB * FRAG), lds0 + buf * T::STAGE,
+                 (kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS)};
+  };
+  auto load = [&](const Stage &s, int q, auto last) {   // load q < LOADS of this wave
+    constexpr int QA = T::FA / NW, QB = T::FB / NW;
+    if (q < QA + QB) {
+      const int qq = q < QA ? q : q - QA, P = q < QA ? PA : PB;
+      uint32_t off = q < QA ? a_off[qq] : b_off[qq];
+      if constexpr (decltype(last)::value) {   // the contraction's last chunk is read in the place of those beyond it
+        const int kc = (qq * NW + wave) % (KS * P) / P;
+        off -= max(0, kc - (KS - s.over - 1)) * (P * FRAG);
+      }
+      nt_dma(q < QA ? s.a : s.b, off, s.lds + ((q < QA ? 0 : T::FA) + qq * NW) * FRAG, true);
+    } else if constexpr (T::FP4) {
+      const int qq = q - QA - QB;
+      nt_dma(s_base[qq] + s.at4, lane * 4,
+             s.lds - wave * FRAG + (T::FA + T::FB) * FRAG + min(qq * NW + wave, T::SA + T::SB - 1) * 256, false);
+    }
+  };
   auto issue = [&](int kt, int buf) {
-    const uint32_t st = lds0 + buf * T::STAGE;
+    const Stage s = stage(kt, buf);
+    if (KS == 1 || s.over <= 0) {
 #pragma unroll
-    for (int q = 0; q < T::FA / NW; ++q) {
-      const int f = q * NW + wave, i = f / (KS * PA), kp = f - i * (KS * PA), kc = kp / PA;
-      const int64_t at = (int64_t)min(rb0 + i, g.A.row_blocks - 1) * g.chunks + min(kc0 + kt * KS + kc, kc1 - 1);
-      nt_dma(Ap + (at * PA + (kp - kc * PA)) * FRAG, lane * 16, st + f * FRAG, true);
-    }
+      for (int q = 0; q < T::LOADS; ++q) load(s, q, std::false_type{});
+    } else {
 #pragma unroll
-    for (int q = 0; q < T::FB / NW; ++q) {
-      const int f = q * NW + wave, i = f / (KS * PB), kp = f - i * (KS * PB), kc = kp / PB;
-      const int64_t at = (int64_t)min(cb0 + i, g.B.row_blocks - 1) * g.chunks + min(kc0 + kt * KS + kc, kc1 - 1);
-      nt_dma(Bp + (at * PB + (kp - kc * PB)) * FRAG, lane * 16, st + (T::FA + f) * FRAG, true);
-    }
-    if constexpr (T::FP4) {
-      const int c4 = (g.chunks + 3) / 4, at4 = (kc0 + kt * KS) / 4;
-#pragma unroll
-      for (int q = 0; q < T::SA / NW; ++q) {
-        const int i = q * NW + wave;
-        nt_dma(g.A.scales + ((int64_t)min(rb0 + i, g.A.row_blocks - 1) * c4 + at4) * 256, lane * 4,
-               st + (T::FA + T::FB) * FRAG + i * 256, false);
-      }
-#pragma unroll
-      for (int q = 0; q < T::SB / NW; ++q) {
-        const int i = q * NW + wave;
-        nt_dma(g.B.scales + ((int64_t)min(cb0 + i, g.B.row_blocks - 1) * c4 + at4) * 256, lane * 4,
-               st + (T::FA + T::FB) * FRAG + (T::SA + i) * 256, false);
-      }
+      for (int q = 0; q < T::LOADS; ++q) load(s, q, std::true_type{});
     }
   };
 
@@ -188,108 +233,312 @@ __global__ __launch_bounds__(T::T, 2) void k_nt(const NtArgs g, const EPI epi) {
       if constexpr (T::TWO) lo[i][j] = f32v4{0.f, 0.f, 0.f, 0.f};
     }
 
-  auto multiply = [&](int kt, const uint8_t *st, int kc) {
-    const uint8_t *a = st + ((wm * MB * KS + kc) * PA) * FRAG + lane * 16;
-    const uint8_t *b = st + T::FA * FRAG + ((wn * NB * KS + kc) * PB) * FRAG + lane * 16;
+  // operands of a wave's chunk from LDS: columns' fragments, and rows' one by one
+  struct Chunk {
+    bf16x8 b[NB][PB], a[MB][PA];
+    int bs[T::FP4 ? NB : 1], as[T::FP4 ? MB : 1];
+  };
+  auto read_a = [&](Chunk &c, int at, int kt, const uint8_t *st, int kc, int i, int p) {
+    c.a[at][p] = *reinterpret_cast<const bf16x8 *>(st + (((wm * MB + i) * KS + kc) * PA + p) * FRAG + lane * 16);
     if constexpr (T::FP4) {
       const uint32_t *s = reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG) + lane;
-      const int sh = 8 * ((kc0 + kt * KS + kc) & 3);
-      i32x4 bv[NB];
-      int bs[NB];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        bv[j] = *reinterpret_cast<const i32x4 *>(b + j * KS * FRAG);
-        bs[j] = (int)(s[(T::SA + wn * NB + j) * 64] >> sh);
-      }
-#pragma unroll
-      for (int i = 0; i < MB; ++i) {
-        const i32x4 av = *reinterpret_cast<const i32x4 *>(a + i * KS * FRAG);
-        const int as = (int)(s[(wm * MB + i) * 64] >> sh);
-        const i32x8 aw = {av[0], av[1], av[2], av[3], 0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          const i32x8 bw = {bv[j][0], bv[j][1], bv[j][2], bv[j][3], 0, 0, 0, 0};
-          hi[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw, aw, hi[i][j], 4, 4, 0, bs[j], 0, as);
-        }
-      }
-    } else {
-      bf16x8 bv[NB][PB];
+      c.as[at] = (int)(s[(wm * MB + i) * 64] >> 8 * ((kc0 + kt * KS + kc) & 3));
+    }
+  };
+  auto read_b = [&](Chunk &c, int kt, const uint8_t *st, int kc, int j, int p) {
+    c.b[j][p] = *reinterpret_cast<const bf16x8 *>(st + (T::FA + ((wn * NB + j) * KS + kc) * PB + p) * FRAG + lane * 16);
+    if constexpr (T::FP4) {
+      const uint32_t *s = reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG) + lane;
+      c.bs[j] = (int)(s[(T::SA + wn * NB + j) * 64] >> 8 * ((kc0 + kt * KS + kc) & 3));
+    }
+  };
+  auto multiply = [&](const Chunk &c, int at, int i, int p) {   // product p of row block i with the wave's columns
+    if constexpr (T::FP4) {
+      auto wide = [](bf16x8 v) {
+        const i32x4 q = __builtin_bit_cast(i32x4, v);
+        return i32x8{q[0], q[1], q[2], q[3], 0, 0, 0, 0};
+      };
 #pragma unroll
       for (int j = 0; j < NB; ++j)
+        hi[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(c.b[j][0]), wide(c.a[at][0]), hi[i][j], 4, 4, 0, c.bs[j], 0, c.as[at]);
+    } else {
+      // (A part, B part) and accumulator of product p
+      constexpr int pa33[6] = {0, 2, 1, 0, 1, 0}, pb33[6] = {2, 0, 1, 1, 0, 0}, pa31[3] = {2, 1, 0}, pa22[3] = {0, 1, 0}, pb22[3] = {1, 0, 0};
+      const int pa = T::PRODUCTS == 6 ? pa33[p] : PA == 3 ? pa31[p] : PA == 2 ? pa22[p] : 0;
+      const int pb = T::PRODUCTS == 6 ? pb33[p] : PA == 2 ? pb22[p] : 0;
+      const bool small = T::TWO && p + 1 < T::PRODUCTS;
 #pragma unroll
-        for (int p = 0; p < PB; ++p) bv[j][p] = *reinterpret_cast<const bf16x8 *>(b + (j * KS * PB + p) * FRAG);
-#pragma unroll
-      for (int i = 0; i < MB; ++i) {
-        bf16x8 av[PA];
-#pragma unroll
-        for (int p = 0; p < PA; ++p) av[p] = *reinterpret_cast<const bf16x8 *>(a + (i * KS * PA + p) * FRAG);
-        auto each = [&](int pa, int pb, f32v4 (&acc)[NB]) {
-#pragma unroll
-          for (int j = 0; j < NB; ++j) acc[j] = mfma_bf16(bv[j][pb], av[pa], acc[j]);
-        };
-        if constexpr (PA == 3 && PB == 3) {
-          each(0, 2, lo[i]);
-          each(2, 0, lo[i]);
-          each(1, 1, lo[i]);
-          each(0, 1, lo[i]);
-          each(1, 0, lo[i]);
-          each(0, 0, hi[i]);
-        } else if constexpr (PA == 3) {
-          each(2, 0, lo[i]);
-          each(1, 0, lo[i]);
-          each(0, 0, hi[i]);
-        } else if constexpr (PA == 2) {
-          each(0, 1, hi[i]);
-          each(1, 0, hi[i]);
-          each(0, 0, hi[i]);
-        } else {
-          each(0, 0, hi[i]);
-        }
+      for (int j = 0; j < NB; ++j) {
+        f32v4 &acc = small ? lo[T::TWO ? i : 0][T::TWO ? j : 0] : hi[i][j];
+        acc = mfma_bf16(c.b[j][pb], c.a[at][pa], acc);
       }
     }
   };
+  auto landed = [&](int kt, int later) {   // this wave's loads of stage kt, with `later` stages issued after it
+    if (later > 1 && kt + later < KT) wait_vmcnt<2 * T::LOADS>();
+    else if (later > 0 && kt + 1 < KT) wait_vmcnt<T::LOADS>();
+    else wait_vmcnt<0>();
+  };
 
-  if (KT > 0) issue(0, 0);
-  int cur = 0;
-  for (int kt = 0; kt < KT; ++kt) {
-    wait_vmcnt<0>();   // this wave's loads of the stage have landed
-    barrier_only();    // every wave's have, and the other stage has been read
-    if (kt + 1 < KT) issue(kt + 1, cur ^ 1);
-    const uint8_t *st = lds + cur * T::STAGE;
+  static_assert(NS >= 2 && NS <= 4, "at most two stages in flight behind the one waited for");
+  // Step kt: stage kt + 1 has landed; the barrier publishes it and frees stage kt, whose operands every wave has in
+  // registers, for stage kt + NS.  (Two register sets, the loop unrolled by two, so that no set is copied.)
+  constexpr int KW = T::KW, READS = KW * (NB * PB + MB * PA), GROUPS = KW * MB * T::PRODUCTS;
+  struct Set {
+    Chunk c[KW];
+  };
+  auto read = [&](Set &s, int kt, const uint8_t *st, int n) {   // read n < READS of a stage
+    const int k = n / (NB * PB + MB * PA), m = n % (NB * PB + MB * PA);
+    if (m < NB * PB) read_b(s.c[k], kt, st, k * T::WK + wk, m / PB, m % PB);
+    else read_a(s.c[k], (m - NB * PB) / PA, kt, st, k * T::WK + wk, (m - NB * PB) / PA, (m - NB * PB) % PA);
+  };
+  auto group = [&](const Set &s, int n) {   // group n < GROUPS of NB matrix instructions of a stage
+    const int k = n / (MB * T::PRODUCTS), i = n / T::PRODUCTS % MB;
+    multiply(s.c[k], i, i, n % T::PRODUCTS);
+  };
+  // `now` is in registers: told to the compiler before the reads of `next`, whose end it would otherwise wait for before
+  // the products of `now`
+  auto arrived = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
+  auto steady = [&](int kt, const Set &now, Set &next) {   // kt + NS + 1 < KT
+    arrived();
+    wait_vmcnt<(NS - 2) * T::LOADS>();
+    barrier_only();
+    const uint8_t *st = lds + (kt + 1) % NS * T::STAGE;
+    const Stage ns = stage(kt + NS, kt % NS);
+    // Loads and reads are spread between the groups: a wave issues in order, and would stand still until LDS and the
+    // memory pipe have taken all of them.
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) {
+#pragma unroll
+      for (int q = n * T::LOADS / GROUPS; q < (n + 1) * T::LOADS / GROUPS; ++q) load(ns, q, std::false_type{});
+#pragma unroll
+      for (int q = n * READS / GROUPS; q < (n + 1) * READS / GROUPS; ++q) read(next, kt + 1, st, q);
+      group(now, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto step = [&](int kt, const Set &now, Set &next) {
+    arrived();
+    if (kt + 1 < KT) {
+      landed(kt + 1, NS - 2);
+      barrier_only();
+      if (kt + NS < KT) issue(kt + NS, kt % NS);
+      const uint8_t *st = lds + (kt + 1) % NS * T::STAGE;
+#pragma unroll
+      for (int n = 0; n < READS; ++n) read(next, kt + 1, st, n);
+    }
     const int left = kc1 - kc0 - kt * KS;
 #pragma unroll
-    for (int kc = 0; kc < KS; ++kc)
-      if (kc < left) multiply(kt, st, kc);   // wave-uniform
-    cur ^= 1;
+    for (int n = 0; n < GROUPS; ++n)
+      if (n / (MB * T::PRODUCTS) * T::WK + wk < left) group(now, n);   // wave-uniform
+  };
+  Set s0, s1;
+  if (KT > 0) {
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+      if (t < KT) issue(t, t);
+    // stage 0, with up to NS - 1 behind it
+    if (NS > 3 && KT > 3) wait_vmcnt<3 * T::LOADS>();
+    else if (NS > 2 && KT > 2) wait_vmcnt<2 * T::LOADS>();
+    else if (KT > 1) wait_vmcnt<T::LOADS>();
+    else wait_vmcnt<0>();
+    barrier_only();
+#pragma unroll
+    for (int n = 0; n < READS; ++n) read(s0, 0, lds, n);
+  }
+  int kt = 0;
+  for (; kt + NS + 2 < KT; kt += 2) {
+    steady(kt, s0, s1);
+    steady(kt + 1, s1, s0);
+  }
+#pragma unroll 1
+  for (; kt < KT; kt += 2) {
+    step(kt, s0, s1);
+    if (kt + 1 < KT) step(kt + 1, s1, s0);
   }
 
   const int r16 = lane & 15, g4 = lane >> 4;
+  auto joined = [&](int i, int j) {
+    f32v4 v = hi[i][j];
+    if constexpr (T::TWO) {
+      // (an infinite or NaN large product is the result: the small ones of such operands are NaN)
 #pragma unroll
-  for (int i = 0; i < MB; ++i)
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      f32v4 v = hi[i][j];
-      if constexpr (T::TWO) {
-        // (an infinite or NaN large product is the result: the small ones of such operands are NaN)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = fabsf(v[q]) < __builtin_huge_valf() ? v[q] + lo[i][j][q] : v[q];
-      }
-      epi.store(blockIdx.y, blockIdx.z, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
+      for (int q = 0; q < 4; ++q) v[q] = fabsf(v[q]) < __builtin_huge_valf() ? v[q] + lo[i][j][q] : v[q];
     }
+    return v;
+  };
+  auto put = [&](int i, int j, f32v4 v) {
+    epi.store(batch, blockIdx.y, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
+  };
+  if constexpr (T::WK == 1) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) put(i, j, joined(i, j));
+  } else {
+    f32v4 *red = reinterpret_cast<f32v4 *>(lds) + (wm + T::WM * wn) * T::WK * MB * NB * 64 + lane;
+    barrier_only();   // the last stage has been read
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) red[(wk * MB * NB + i * NB + j) * 64] = joined(i, j);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        if ((i * NB + j) % T::WK == wk) {
+          f32v4 v = red[(i * NB + j) * 64];
+#pragma unroll
+          for (int q = 1; q < T::WK; ++q) v += red[(q * MB * NB + i * NB + j) * 64];
+          put(i, j, v);
+        }
+  }
 }
 
+// ---- which tiles -------------------------------------------------------------------------------
+// The shapes of one class of products, largest first; a tile of one is whole tiles of every later one.  A product's
+// time is taken as rounds x chunks x us, with so many workgroups on the chip at once; a large shape spends less per
+// output, a small one wastes less of its last round.  So the whole rounds may go to one shape and what is left of the
+// last to another, in a launch of its own.
+struct NtShape {
+  int bm, bn;
+  int slots;   // workgroups on the chip at once
+  float us;    // of a chunk, measured at one full round and more
+};
+constexpr int NT_SHAPES = 5;
+constexpr float NT_LAUNCH_US = 3.f;
+struct NtPlan {
+  int main = 0, rest = -1;   // shapes
+  int64_t main_tiles = 0, rest_tiles = 0;   // counted in main's shape, over the batch
+  float us = 0.f;
+};
+inline int64_t nt_tiles(int64_t M, int64_t N, int bm, int bn, bool tri) {
+  const int64_t mt = (M + bm - 1) / bm, nt = (N + bn - 1) / bn;
+  if (!tri) return mt * nt;
+  int64_t s = 0;
+  for (int64_t i = 0; i < mt; ++i) s += nt_row_tiles((int)i, bm, bn, (int)nt, true);
+  return s;
+}
+inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri) {
+  auto rounds = [](int64_t tiles, int slots) { return (float)((tiles + slots - 1) / slots); };
+  NtPlan best;
+  for (int a = 0; a < NT_SHAPES; ++a) {
+    const int64_t t = nt_tiles(M, N, sh[a].bm, sh[a].bn, tri) * batch;
+    const float per = sh[a].us * (float)chunks, all = rounds(t, sh[a].slots) * per;
+    if (a == 0 || all < best.us) {
+      best.main = a;
+      best.rest = -1;
+      best.main_tiles = t;
+      best.rest_tiles = 0;
+      best.us = all;
+    }
+    const int64_t full = t / sh[a].slots * sh[a].slots;
+    if (full == 0 || full == t) continue;
+    for (int b = a + 1; b < NT_SHAPES; ++b) {
+      const int64_t subs = (int64_t)(sh[a].bm / sh[b].bm) * (sh[a].bn / sh[b].bn);
+      const float us = (float)(full / sh[a].slots) * per + rounds((t - full) * subs, sh[b].slots) * sh[b].us * (float)chunks + NT_LAUNCH_US;
+      if (us < best.us) {
+        best.main = a;
+        best.rest = b;
+        best.main_tiles = full;
+        best.rest_tiles = t - full;
+        best.us = us;
+      }
+    }
+  }
+  return best;
+}
+
+// `count` tiles of shape (bm, bn) from `first` on, by kernels of shape T
 template <class T, class EPI>
-hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int batch, int zs, const EPI &epi, hipStream_t s) {
-  const int64_t mt = (M + T::BM - 1) / T::BM, nt = (N + T::BN - 1) / T::BN;
-  if (mt <= 0 || nt <= 0 || g.chunks <= 0 || mt * nt > 0x7fffffff || batch <= 0 || batch > 65535 || zs <= 0 || zs > 65535)
-    return hipErrorInvalidValue;
+hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t first, int64_t count, int parts, const EPI &epi, hipStream_t s) {
+  const int64_t mt = (M + bm - 1) / bm, nt = (N + bn - 1) / bn;
+  g.bm = bm;
+  g.bn = bn;
   g.n_mt = (int32_t)mt;
   g.n_nt = (int32_t)nt;
+  const int64_t tiles = nt_tiles(M, N, bm, bn, g.tri);
+  g.tiles = (int32_t)tiles;
+  g.first = (int32_t)first;
+  g.sub_m = bm / T::BM;
+  g.sub_n = bn / T::BN;
+  const int64_t grid = count * g.sub_m * g.sub_n;
+  // (a tile's row blocks are reached by 32-bit offsets)
+  if ((int64_t)g.chunks * 3 * FRAG * (std::max(T::BM, T::BN) / 16) > 0xffffffffll) return hipErrorInvalidValue;
+  if (mt <= 0 || nt <= 0 || g.chunks <= 0 || tiles > 0x7fffffff || grid <= 0 || grid > 0x7fffffff || first + count > 0x7fffffff ||
+      g.sub_m * T::BM != bm || g.sub_n * T::BN != bn || parts <= 0 || parts > 65535)
+    return hipErrorInvalidValue;
   const int kt = (g.chunks + T::KS - 1) / T::KS;
-  g.z_chunks = (kt + zs - 1) / zs * T::KS;
-  const dim3 grid((unsigned)nt_tiles<T>(g.n_mt, g.n_nt, g.tri), (unsigned)batch, (unsigned)zs);
-  hipLaunchKernelGGL((k_nt<T, EPI>), grid, dim3(T::T), 0, s, g, epi);
+  g.z_chunks = (kt + parts - 1) / parts * T::KS;
+  hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)grid, (unsigned)parts), dim3(T::T), 0, s, g, epi);
   return hipGetLastError();
 }
+// A product by the shapes of TS (T0 .. T4 and their `shapes`)
+template <class TS, class EPI>
+hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, const EPI &epi, hipStream_t s) {
+  const NtPlan p = nt_plan(TS::shapes, M, N, g.chunks, batch, g.tri);
+  auto go = [&](int shape, int64_t first, int64_t count) {
+    const int bm = TS::shapes[p.main].bm, bn = TS::shapes[p.main].bn;
+    switch (shape) {
+      case 0: return launch_nt<typename TS::T0>(g, M, N, bm, bn, first, count, 1, epi, s);
+      case 1: return launch_nt<typename TS::T1>(g, M, N, bm, bn, first, count, 1, epi, s);
+      case 2: return launch_nt<typename TS::T2>(g, M, N, bm, bn, first, count, 1, epi, s);
+      case 3: return launch_nt<typename TS::T3>(g, M, N, bm, bn, first, count, 1, epi, s);
+      default: return launch_nt<typename TS::T4>(g, M, N, bm, bn, first, count, 1, epi, s);
+    }
+  };
+  const hipError_t e = go(p.main, 0, p.main_tiles);
+  return e != hipSuccess || p.rest < 0 ? e : go(p.rest, p.main_tiles, p.rest_tiles);
+}
+
+// The shapes of products of PA and PB parts.  8 waves, two on every SIMD, where registers and LDS allow it.
+template <int PA, int PB, bool FP4>
+struct NtTiles;
+template <>
+struct NtTiles<1, 1, true> {
+  typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4, true> T0;
+  typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4, true> T1;
+  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4, true> T2;
+  typedef NtTile<2, 2, 2, 2, 2, 1, 1, 4, 3, true> T3;
+  typedef NtTile<2, 2, 1, 2, 4, 1, 1, 4, 4, true> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 256, 1.03f}, {128, 128, 512, .59f}, {64, 128, 256, .245f}, {64, 64, 256, .145f}, {32, 64, 256, .104f}};
+};
+template <>
+struct NtTiles<1, 1, false> {
+  typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
+  typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
+  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
+  typedef NtTile<2, 2, 2, 2, 2, 1, 1, 4, 4> T3;
+  typedef NtTile<2, 2, 1, 2, 4, 1, 1, 4, 4> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 256, .71f}, {128, 128, 512, .41f}, {64, 128, 256, .165f}, {64, 64, 256, .116f}, {32, 64, 256, .09f}};
+};
+template <>
+struct NtTiles<3, 1, false> {
+  typedef NtTile<4, 2, 2, 4, 1, 3, 1, 1, 3> T0;
+  typedef NtTile<2, 2, 2, 4, 1, 3, 1, 2, 3> T1;
+  typedef NtTile<2, 2, 2, 2, 2, 3, 1, 2, 4> T2;
+  typedef NtTile<2, 2, 1, 2, 4, 3, 1, 4, 3> T3;
+  typedef NtTile<2, 2, 1, 1, 4, 3, 1, 4, 4> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 256, .58f}, {64, 128, 256, .32f}, {64, 64, 256, .215f}, {32, 64, 256, .142f}, {32, 32, 256, .112f}};
+};
+template <>
+struct NtTiles<3, 3, false> {
+  typedef NtTile<4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
+  typedef NtTile<2, 4, 2, 2, 2, 3, 3, 2, 2> T1;
+  typedef NtTile<2, 2, 2, 2, 2, 3, 3, 2, 3> T2;
+  typedef NtTile<2, 2, 1, 2, 4, 3, 3, 4, 2> T3;
+  typedef NtTile<2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 256, 1.07f}, {64, 128, 256, .63f}, {64, 64, 256, .326f}, {32, 64, 256, .285f}, {32, 32, 256, .162f}};
+};
+template <>
+struct NtTiles<2, 2, false> {
+  typedef NtTile<4, 4, 4, 2, 1, 2, 2, 1, 3> T0;
+  typedef NtTile<4, 2, 2, 4, 1, 2, 2, 1, 4> T1;
+  typedef NtTile<2, 2, 2, 4, 1, 2, 2, 1, 4> T2;
+  typedef NtTile<2, 2, 2, 2, 2, 2, 2, 2, 4> T3;
+  typedef NtTile<2, 2, 1, 2, 4, 2, 2, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 256, 1.04f}, {128, 128, 256, .557f}, {64, 128, 256, .337f}, {64, 64, 256, .21f}, {32, 64, 256, .156f}};
+};
 
 }  // namespace vcr

@@ -12,7 +12,6 @@
 // the rounding of one part, 2^-9 of the largest, with it.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "layers.h"
 #include "planes.h"
@@ -131,22 +130,6 @@ struct EpiNs : NsEpilogue {
   }
 };
 
-template <int P>
-struct NsTiles {
-  typedef std::conditional_t<P == 3, NtTile<4, 4, 4, 2, P, P, 1>, NtTile<8, 4, 2, 4, P, P, 1>> L;
-  typedef std::conditional_t<P == 3, NtTile<4, 2, 2, 4, P, P, 1>, NtTile<4, 4, 2, 2, P, P, 1>> M;
-  typedef NtTile<2, 2, 2, 2, P, P, 1> S;
-};
-template <int P, int MODE>
-static hipError_t ns_product(const NtArgs &g, int64_t M, int64_t N, int batch, const NsEpilogue &base, hipStream_t s) {
-  typedef NsTiles<P> TS;
-  const EpiNs<P, MODE> e{base};
-  auto tiles = [&](int bm, int bn) { return blocks_of(M, bm) * blocks_of(N, bn) * batch / (g.tri ? 2 : 1); };
-  if (tiles(TS::L::BM, TS::L::BN) >= 200) return launch_nt<typename TS::L>(g, M, N, batch, 1, e, s);
-  if (tiles(TS::M::BM, TS::M::BN) >= 200) return launch_nt<typename TS::M>(g, M, N, batch, 1, e, s);
-  return launch_nt<typename TS::S>(g, M, N, batch, 1, e, s);
-}
-
 struct NsSpace {
   double *norm;
   uint8_t *x, *xt, *x2, *xt2, *gram, *poly;
@@ -189,18 +172,18 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
     a.chunks = (int32_t)(np / 32);
     a.tri = 1;
     e.dst = sp.gram;
-    if ((err = ns_product<P, NS_GRAM>(a, mp, mp, batch, e, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<P, P, false>>(a, mp, mp, batch, EpiNs<P, NS_GRAM>{e}, s)) != hipSuccess) return err;
     a.A = a.B = NtOperand{sp.gram, nullptr, (int32_t)(mp / 16), sg};
     a.chunks = (int32_t)(mp / 32);
     e.gram = sp.gram;
     e.dst = sp.poly;
-    if ((err = ns_product<P, NS_POLY>(a, mp, mp, batch, e, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<P, P, false>>(a, mp, mp, batch, EpiNs<P, NS_POLY>{e}, s)) != hipSuccess) return err;
     a.A = NtOperand{sp.poly, nullptr, (int32_t)(mp / 16), sg};
     a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx};
     a.tri = 0;
     e.dst = sp.x2;
     e.dst_t = sp.xt2;
-    err = step + 1 == steps ? ns_product<P, NS_OUT>(a, mp, np, batch, e, s) : ns_product<P, NS_UPDATE>(a, mp, np, batch, e, s);
+    err = step + 1 == steps ? launch_nt_plan<NtTiles<P, P, false>>(a, mp, np, batch, EpiNs<P, NS_OUT>{e}, s) : launch_nt_plan<NtTiles<P, P, false>>(a, mp, np, batch, EpiNs<P, NS_UPDATE>{e}, s);
     if (err != hipSuccess) return err;
     std::swap(sp.x, sp.x2);
     std::swap(sp.xt, sp.xt2);

@@ -168,7 +168,7 @@ class MX:
     column groups, 64, 16) and `scales` (row blocks, ceil(groups / 4), 64, 4).  Made by Ctx.mx_quantize, or by
     MX.pack from codes and scales in row order."""
 
-    __slots__ = ("codes", "scales", "rows", "cols")
+    __slots__ = ("rows", "cols", "device", "_codes", "_scales", "_buf", "_s", "_ref")
 
     def __init__(self, codes, scales, rows, cols):
         groups = -(-cols // 128)
@@ -177,14 +177,42 @@ class MX:
         for t, shape in zip((codes, scales), want):
             if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
                 raise ValueError(f"expected a contiguous uint8 CUDA tensor of shape {shape}")
-        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self._codes, self._scales, self._buf = codes, scales, None
+        self._set(rows, cols, codes.device, codes.data_ptr(), scales.data_ptr())
+
+    def _set(self, rows, cols, device, codes, scales):
+        self.rows, self.cols, self.device = rows, cols, device
+        self._s = VcrMx(codes, scales, rows, cols)
+        self._ref = ctypes.byref(self._s)
 
     @classmethod
     def empty(cls, rows, cols, device="cuda"):
         import torch
+        self = cls.__new__(cls)
         rb, groups = -(-rows // 16), -(-cols // 128)
-        return cls(torch.empty((rb, groups, 64, 16), dtype=torch.uint8, device=device),
-                   torch.empty((rb, -(-groups // 4), 64, 4), dtype=torch.uint8, device=device), rows, cols)
+        self._codes = self._scales = None
+        # one allocation: the codes, then the scales (their tensors are made when asked for)
+        self._buf = torch.empty(rb * (groups * 1024 + -(-groups // 4) * 256), dtype=torch.uint8, device=device)
+        at = self._buf.data_ptr()
+        self._set(rows, cols, self._buf.device, at, at + rb * groups * 1024)
+        return self
+
+    def _views(self):
+        rb, groups = -(-self.rows // 16), -(-self.cols // 128)
+        self._codes = self._buf[:rb * groups * 1024].view(rb, groups, 64, 16)
+        self._scales = self._buf[rb * groups * 1024:].view(rb, -(-groups // 4), 64, 4)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._views()
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._views()
+        return self._scales
 
     @classmethod
     def pack(cls, codes, scales, cols):
@@ -209,9 +237,6 @@ class MX:
         c = self.codes.view(rb, groups, 4, 16, 16).permute(0, 3, 1, 2, 4).reshape(rb * 16, groups * 64)
         s = self.scales.view(rb, n4, 4, 16, 4).permute(0, 3, 1, 4, 2).reshape(rb * 16, n4 * 16)
         return (c[:self.rows, :-(-self.cols // 2)].contiguous(), s[:self.rows, :-(-self.cols // 32)].contiguous())
-
-    def _c(self):
-        return VcrMx(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
 
 
 def _net_nodes(net):
@@ -250,6 +275,7 @@ class Ctx:
             raise VcrError(st, f"vcr_create({device}) failed")
         self.h = h
         self.device = device
+        self._raw_stream = 0   # the stream the library was given last (it begins with the null stream)
         self.n_relu = 0
         self.relu_sizes = []
 
@@ -275,6 +301,7 @@ class Ctx:
         """Queue work on a torch stream (default: torch's current stream)."""
         import torch
         s = torch.cuda.current_stream() if stream is None else stream
+        self._raw_stream = s.cuda_stream
         self._check(self.lib.vcr_set_stream(self.h, ctypes.c_void_p(s.cuda_stream)))
 
     def load_net(self, net):
@@ -287,6 +314,12 @@ class Ctx:
 
     def _stream_sync(self):
         if self.device >= 0:
+            self.set_stream()
+
+    def _current_stream(self):
+        """_stream_sync for calls of a few microseconds: torch's current stream by its handle alone."""
+        import torch
+        if self.device >= 0 and torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
             self.set_stream()
 
     def crown_bounds(self, x0, eps, C, splits=None, out=None):
@@ -444,24 +477,24 @@ class Ctx:
         """x (rows, cols), a float32 or bfloat16 CUDA tensor with contiguous rows, in 4 bits (an MX)."""
         m = _mat(x)
         q = MX.empty(m.rows, m.cols, x.device) if out is None else out
-        self._stream_sync()
-        self._check(self.lib.vcr_mx_quantize(self.h, ctypes.byref(m), ctypes.byref(q._c())))
+        self._current_stream()
+        self._check(self.lib.vcr_mx_quantize(self.h, ctypes.byref(m), q._ref))
         return q
 
     def mx_dequantize(self, q, dtype=None, out=None):
         """The values of an MX, float32 unless `dtype` is bfloat16."""
         import torch
-        y = torch.empty((q.rows, q.cols), dtype=dtype or torch.float32, device=q.codes.device) if out is None else out
-        self._stream_sync()
-        self._check(self.lib.vcr_mx_dequantize(self.h, ctypes.byref(q._c()), ctypes.byref(_mat(y))))
+        y = torch.empty((q.rows, q.cols), dtype=dtype or torch.float32, device=q.device) if out is None else out
+        self._current_stream()
+        self._check(self.lib.vcr_mx_dequantize(self.h, q._ref, ctypes.byref(_mat(y))))
         return y
 
     def mx_product(self, a, w, bias=None, relu=False, dtype=None, out=None):
         """act(a w^T + bias), a (rows, k) and w (n, k) both MX, float32 unless `dtype` is bfloat16."""
         import torch
-        y = torch.empty((a.rows, w.rows), dtype=dtype or torch.float32, device=a.codes.device) if out is None else out
-        self._stream_sync()
-        self._check(self.lib.vcr_mx_product(self.h, ctypes.byref(a._c()), ctypes.byref(w._c()), _bias(bias, w.rows),
+        y = torch.empty((a.rows, w.rows), dtype=dtype or torch.float32, device=a.device) if out is None else out
+        self._current_stream()
+        self._check(self.lib.vcr_mx_product(self.h, a._ref, w._ref, _bias(bias, w.rows),
                                             1 if relu else 0, ctypes.byref(_mat(y))))
         return y
 
@@ -470,8 +503,8 @@ class Ctx:
         import torch
         m = _mat(x)
         y = torch.empty((m.rows, w.rows), dtype=x.dtype, device=x.device) if out is None else out
-        self._stream_sync()
-        self._check(self.lib.vcr_mx_linear(self.h, ctypes.byref(m), ctypes.byref(w._c()), _bias(bias, w.rows),
+        self._current_stream()
+        self._check(self.lib.vcr_mx_linear(self.h, ctypes.byref(m), w._ref, _bias(bias, w.rows),
                                            1 if relu else 0, ctypes.byref(_mat(y))))
         return y
 
@@ -484,9 +517,9 @@ class Ctx:
         dw = torch.empty((g.cols, x.shape[1]), dtype=torch.float32, device=dy.device) if need[1] else None
         db = torch.empty((g.cols,), dtype=torch.float32, device=dy.device) if need[2] else None
         ref = lambda t: None if t is None else ctypes.byref(_mat(t))  # noqa: E731
-        self._stream_sync()
+        self._current_stream()
         self._check(self.lib.vcr_mx_linear_grad(self.h, ctypes.byref(g), ref(y), ref(x if need[1] else None),
-                                                ctypes.byref(w._c()) if need[0] else None, ref(dx), ref(dw),
+                                                w._ref if need[0] else None, ref(dx), ref(dw),
                                                 None if db is None else _ptr(db)))
         return dx, dw, db
 
@@ -510,7 +543,7 @@ class Ctx:
         gm, om = one(g), one(out)
         bm = (None, 0) if base is None else one(base)
         o = VcrNsOpts(int(steps), *(float(v) for v in coefficients), float(eps), float(gain), float(keep))
-        self._stream_sync()
+        self._current_stream()
         self._check(self.lib.vcr_orthogonalize(self.h, ctypes.byref(gm[0]), count, gm[1], ctypes.byref(o),
                                                None if base is None else ctypes.byref(bm[0]), bm[1],
                                                ctypes.byref(om[0]), om[1]))
@@ -569,15 +602,22 @@ def _out_size(net):
     return int(net.nodes[-1].W.shape[0])
 
 
+_TYPES = {}   # vcr_mat's types by torch's
+
+
 def _mat(t):
     """A vcr_mat of a 2-d tensor."""
-    import torch
-    kind = {torch.float32: 0, torch.bfloat16: 1}.get(getattr(t, "dtype", None))
-    if kind is None or not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: 0, torch.bfloat16: 1})
+    kind = _TYPES.get(getattr(t, "dtype", None))
+    if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError("expected a float32 or bfloat16 CUDA tensor of 2 dimensions with contiguous rows")
-    rows, cols = t.shape
+    (rows, cols), (ld, one) = t.shape, t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError("expected a float32 or bfloat16 CUDA tensor of 2 dimensions with contiguous rows")
     # (a single row's stride is of no account)
-    return VcrMat(t.data_ptr(), kind, rows, cols, t.stride(0) if rows > 1 else max(cols, 1))
+    return VcrMat(t.data_ptr(), kind, rows, cols, ld if rows > 1 else max(cols, 1))
 
 
 def _bias(b, n):
