@@ -271,12 +271,14 @@ __global__ __launch_bounds__(256) void k_join(const float *p, int parts, int64_t
 }
 
 // ---- products by tiles ------------------------------------------------------------------------
-// Parts of the contraction: few tiles of the smallest shape over a long contraction leave compute units idle; parts of
-// 16 chunks and more are then summed by their own workgroups and joined in order.
+// Parts of the contraction: few tiles over a long contraction leave compute units idle.  Parts of 16 chunks and more are
+// then summed by their own workgroups (the smallest shape) and joined in order, where that pays for the second launch.
 template <int PA, int PB, bool FP4>
 static int nt_parts(int64_t M, int64_t N, int64_t chunks) {
-  const NtShape &x = NtTiles<PA, PB, FP4>::shapes[NT_SHAPES - 1];
-  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / nt_tiles(M, N, x.bm, x.bn, false), chunks / 16));
+  const NtShape *sh = NtTiles<PA, PB, FP4>::shapes, &x = sh[NT_SHAPES - 1];
+  const int64_t t = nt_tiles(M, N, x.bm, x.bn, false), parts = std::min<int64_t>(NT_CUS / t, chunks / 16);
+  if (parts < 2) return 1;
+  return nt_us(x, t * parts, (chunks + parts - 1) / parts) + NT_LAUNCH_US < nt_plan(sh, M, N, chunks, 1, false).us ? (int)parts : 1;
 }
 template <int PA, int PB, bool FP4>
 static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {

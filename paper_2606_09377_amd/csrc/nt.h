@@ -397,17 +397,16 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
 }
 
 // ---- which tiles -------------------------------------------------------------------------------
-// The shapes of one class of products, largest first; a tile of one is whole tiles of every later one.  A product's
-// time is taken as rounds x chunks x us, with so many workgroups on the chip at once; a large shape spends less per
-// output, a small one wastes less of its last round.  So the whole rounds may go to one shape and what is left of the
-// last to another, in a launch of its own.
+// The shapes of one class of products, largest first; a tile of one is whole tiles of every later one.  A large shape
+// spends less per output, a small one wastes less of the chip's last round, and where two workgroups fit a compute unit
+// each hides the other's start and end.  So a product's time is estimated for each from what was measured (us1, us2),
+// and the whole rounds may go to one shape and what is left of the last to another, in a launch of its own.
 struct NtShape {
   int bm, bn;
-  int slots;   // workgroups on the chip at once
-  float us;    // of a chunk, measured at one full round and more
+  float us1, us2;   // us of a chunk of a workgroup alone on its compute unit, of two together (0: only one fits)
 };
-constexpr int NT_SHAPES = 5;
-constexpr float NT_LAUNCH_US = 3.f;
+constexpr int NT_SHAPES = 5, NT_CUS = 256;
+constexpr float NT_LAUNCH_US = 4.f, NT_ROUND_US = 2.f;   // of a launch, of a workgroup's start and end
 struct NtPlan {
   int main = 0, rest = -1;   // shapes
   int64_t main_tiles = 0, rest_tiles = 0;   // counted in main's shape, over the batch
@@ -420,12 +419,16 @@ inline int64_t nt_tiles(int64_t M, int64_t N, int bm, int bn, bool tri) {
   for (int64_t i = 0; i < mt; ++i) s += nt_row_tiles((int)i, bm, bn, (int)nt, true);
   return s;
 }
+inline float nt_us(const NtShape &s, int64_t tiles, int64_t chunks) {
+  const int64_t n = (tiles + NT_CUS - 1) / NT_CUS;
+  const float one = s.us1 * (float)chunks + NT_ROUND_US, two = s.us2 * (float)chunks + NT_ROUND_US;
+  return NT_LAUNCH_US + (s.us2 > 0.f ? (float)(n / 2) * two + (float)(n % 2) * one : (float)n * one);
+}
 inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri) {
-  auto rounds = [](int64_t tiles, int slots) { return (float)((tiles + slots - 1) / slots); };
   NtPlan best;
   for (int a = 0; a < NT_SHAPES; ++a) {
     const int64_t t = nt_tiles(M, N, sh[a].bm, sh[a].bn, tri) * batch;
-    const float per = sh[a].us * (float)chunks, all = rounds(t, sh[a].slots) * per;
+    const float all = nt_us(sh[a], t, chunks);
     if (a == 0 || all < best.us) {
       best.main = a;
       best.rest = -1;
@@ -433,11 +436,11 @@ inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, i
       best.rest_tiles = 0;
       best.us = all;
     }
-    const int64_t full = t / sh[a].slots * sh[a].slots;
+    const int64_t round = sh[a].us2 > 0.f ? 2 * NT_CUS : NT_CUS, full = t / round * round;
     if (full == 0 || full == t) continue;
     for (int b = a + 1; b < NT_SHAPES; ++b) {
       const int64_t subs = (int64_t)(sh[a].bm / sh[b].bm) * (sh[a].bn / sh[b].bn);
-      const float us = (float)(full / sh[a].slots) * per + rounds((t - full) * subs, sh[b].slots) * sh[b].us * (float)chunks + NT_LAUNCH_US;
+      const float us = nt_us(sh[a], full, chunks) + nt_us(sh[b], (t - full) * subs, chunks);
       if (us < best.us) {
         best.main = a;
         best.rest = b;
@@ -492,53 +495,53 @@ hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, 
   return e != hipSuccess || p.rest < 0 ? e : go(p.rest, p.main_tiles, p.rest_tiles);
 }
 
-// The shapes of products of PA and PB parts.  8 waves, two on every SIMD, where registers and LDS allow it.
+// The shapes of products of PA and PB parts
 template <int PA, int PB, bool FP4>
 struct NtTiles;
 template <>
 struct NtTiles<1, 1, true> {
   typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4, true> T0;
   typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4, true> T1;
-  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4, true> T2;
-  typedef NtTile<2, 2, 2, 2, 2, 1, 1, 4, 3, true> T3;
-  typedef NtTile<2, 2, 1, 2, 4, 1, 1, 4, 4, true> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 256, 1.03f}, {128, 128, 512, .59f}, {64, 128, 256, .245f}, {64, 64, 256, .145f}, {32, 64, 256, .104f}};
+  typedef NtTile<2, 4, 2, 2, 1, 1, 1, 1, 4, true> T2;
+  typedef NtTile<2, 2, 2, 2, 1, 1, 1, 2, 4, true> T3;
+  typedef NtTile<2, 4, 1, 1, 4, 1, 1, 4, 3, true> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 1.03f, 0.f}, {128, 128, .406f, .57f}, {64, 128, .292f, .402f}, {64, 64, .139f, .218f}, {32, 64, .083f, .161f}};
 };
 template <>
 struct NtTiles<1, 1, false> {
   typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
   typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
-  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
-  typedef NtTile<2, 2, 2, 2, 2, 1, 1, 4, 4> T3;
-  typedef NtTile<2, 2, 1, 2, 4, 1, 1, 4, 4> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 256, .71f}, {128, 128, 512, .41f}, {64, 128, 256, .165f}, {64, 64, 256, .116f}, {32, 64, 256, .09f}};
+  typedef NtTile<2, 4, 2, 2, 1, 1, 1, 2, 3> T2;
+  typedef NtTile<2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
+  typedef NtTile<2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .71f, 0.f}, {128, 128, .241f, .393f}, {64, 128, .154f, .273f}, {64, 64, .083f, .176f}, {32, 64, .052f, .142f}};
 };
 template <>
 struct NtTiles<3, 1, false> {
   typedef NtTile<4, 2, 2, 4, 1, 3, 1, 1, 3> T0;
-  typedef NtTile<2, 2, 2, 4, 1, 3, 1, 2, 3> T1;
-  typedef NtTile<2, 2, 2, 2, 2, 3, 1, 2, 4> T2;
-  typedef NtTile<2, 2, 1, 2, 4, 3, 1, 4, 3> T3;
-  typedef NtTile<2, 2, 1, 1, 4, 3, 1, 4, 4> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 256, .58f}, {64, 128, 256, .32f}, {64, 64, 256, .215f}, {32, 64, 256, .142f}, {32, 32, 256, .112f}};
+  typedef NtTile<2, 4, 2, 2, 1, 3, 1, 1, 4> T1;
+  typedef NtTile<2, 2, 2, 2, 1, 3, 1, 1, 4> T2;
+  typedef NtTile<2, 2, 1, 2, 2, 3, 1, 2, 4> T3;
+  typedef NtTile<2, 2, 1, 1, 4, 3, 1, 4, 2> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .57f, 0.f}, {64, 128, .302f, .539f}, {64, 64, .2f, .365f}, {32, 64, .112f, .218f}, {32, 32, .1f, .153f}};
 };
 template <>
 struct NtTiles<3, 3, false> {
   typedef NtTile<4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
-  typedef NtTile<2, 4, 2, 2, 2, 3, 3, 2, 2> T1;
-  typedef NtTile<2, 2, 2, 2, 2, 3, 3, 2, 3> T2;
-  typedef NtTile<2, 2, 1, 2, 4, 3, 3, 4, 2> T3;
+  typedef NtTile<2, 2, 2, 2, 1, 3, 3, 1, 3> T1;
+  typedef NtTile<2, 2, 1, 2, 4, 3, 3, 4, 2> T2;
+  typedef NtTile<2, 2, 1, 2, 2, 3, 3, 2, 2> T3;
   typedef NtTile<2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 256, 1.07f}, {64, 128, 256, .63f}, {64, 64, 256, .326f}, {32, 64, 256, .285f}, {32, 32, 256, .162f}};
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.05f, 0.f}, {64, 64, .323f, .567f}, {32, 64, .28f, 0.f}, {32, 64, .355f, .393f}, {32, 32, .141f, 0.f}};
 };
 template <>
 struct NtTiles<2, 2, false> {
   typedef NtTile<4, 4, 4, 2, 1, 2, 2, 1, 3> T0;
   typedef NtTile<4, 2, 2, 4, 1, 2, 2, 1, 4> T1;
-  typedef NtTile<2, 2, 2, 4, 1, 2, 2, 1, 4> T2;
-  typedef NtTile<2, 2, 2, 2, 2, 2, 2, 2, 4> T3;
+  typedef NtTile<2, 2, 2, 2, 1, 2, 2, 1, 4> T2;
+  typedef NtTile<2, 2, 1, 2, 2, 2, 2, 2, 3> T3;
   typedef NtTile<2, 2, 1, 2, 4, 2, 2, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 256, 1.04f}, {128, 128, 256, .557f}, {64, 128, 256, .337f}, {64, 64, 256, .21f}, {32, 64, 256, .156f}};
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 1.04f, 0.f}, {128, 128, .54f, 0.f}, {64, 64, .192f, .362f}, {32, 64, .151f, .271f}, {32, 64, .135f, 0.f}};
 };
 
 }  // namespace vcr
