@@ -130,52 +130,25 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t
 }
 
 // ---- operands of the bf16 products ------------------------------------------------------------
-// x, or x where y > 0 (mask), in P parts: a wave per (row block, chunk)
+// (a workgroup goes through the column tiles of 64 rows in the grid's order)
 template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_planes(DevMat x, DevMat y, int vec, int64_t chunks, uint8_t *out) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rb = id / chunks, ch = id - rb * chunks;
-  const int64_t row = rb * 16 + (lane & 15), col = ch * 32 + (lane >> 4) * 8;
-  if (rb * 16 >= x.rows) return;
-  float v[8];
-  mat_row8<BF>(x, 0, row, col, vec, v);
-  if (y.p) {
-    float m[8];
-    mat_row8<BF>(y, 0, row, col, vec, m);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = m[i] > 0.f ? v[i] : 0.f;
-  }
-  store_slot<P>(out, id, lane, v);
+__global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t col_tiles) {
+  __shared__ float tile[64][65];
+  const int64_t tr = blockIdx.x / col_tiles;
+  planes_tile<P, BF>(g, 0, tr, blockIdx.x - tr * col_tiles, 1.f, tile);
 }
 
-// The same transposed (rows of the operand: columns of x), and the column sums of every 32 rows: a
-// wave reads 8 rows of 64 columns, a workgroup 32.
-template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_planes_t(DevMat x, DevMat y, int64_t chunks, uint8_t *out, float *sums) {
+// out[c] = the sum of a column over the groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
+__global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t groups, int64_t cols, float *out) {
   __shared__ float part[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t nc = (x.cols + 63) / 64, ch = blockIdx.x / nc, col = (blockIdx.x - ch * nc) * 64 + lane;
-  float v[8], s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t r = ch * 32 + wave * 8 + i;
-    v[i] = mat_at<BF>(x, 0, r, col);
-    if (y.p) v[i] = mat_at<BF>(y, 0, r, col) > 0.f ? v[i] : 0.f;
-    s += v[i];
-  }
-  if (out && col < (x.cols + 15) / 16 * 16) store_slot<P>(out, (col >> 4) * chunks + ch, wave * 16 + (int)(col & 15), v);
-  if (!sums) return;   // uniform
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  float s = 0.f;
+#pragma unroll 8
+  for (int64_t p = wave; p < groups; p += 4) s += c < cols ? sums[p * cols + c] : 0.f;
   part[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < x.cols) sums[ch * x.cols + col] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-}
-
-__global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t parts, int64_t cols, float *out) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
-  float s = 0.f;
-  for (int64_t p = 0; p < parts; ++p) s += sums[p * cols + c];
-  out[c] = s;
+  if (wave == 0 && c < cols) out[c] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
 }
 
 // 4-bit weights as a bf16 operand (exact): a thread per block
@@ -486,19 +459,15 @@ static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, c
   return hipGetLastError();
 }
 
-static hipError_t launch_planes(const DevMat &x, const DevMat &y, int parts, int64_t chunks, uint8_t *out, hipStream_t s) {
-  const int bytes = x.bf16 ? 2 : 4;
-  const int vec = rows_aligned(x.p, x.ld, bytes) && (!y.p || rows_aligned(y.p, y.ld, bytes));
-  const dim3 grid((unsigned)blocks_of(blocks_of(x.rows, 16) * chunks, 4));
-  if (x.bf16) hipLaunchKernelGGL((k_planes<1, true>), grid, dim3(256), 0, s, x, y, vec, chunks, out);
-  else hipLaunchKernelGGL((k_planes<3, false>), grid, dim3(256), 0, s, x, y, vec, chunks, out);
-  (void)parts;
-  return hipGetLastError();
-}
-static hipError_t launch_planes_t(const DevMat &x, const DevMat &y, int64_t chunks, uint8_t *out, float *sums, hipStream_t s) {
-  const dim3 grid((unsigned)(chunks * blocks_of(x.cols, 64)));
-  if (x.bf16) hipLaunchKernelGGL((k_planes_t<1, true>), grid, dim3(256), 0, s, x, y, chunks, out, sums);
-  else hipLaunchKernelGGL((k_planes_t<3, false>), grid, dim3(256), 0, s, x, y, chunks, out, sums);
+static hipError_t launch_planes(PlanesArgs g, hipStream_t s) {
+  const int bytes = g.x.bf16 ? 2 : 4;
+  g.vec = rows_aligned(g.x.p, g.x.ld, bytes) && (!g.y.p || rows_aligned(g.y.p, g.y.ld, bytes));
+  // tiles of 64 rows and columns, those of the padding among them
+  const int64_t rt = std::max(blocks_of(g.x.rows, 64), g.cols ? blocks_of(g.col_chunks, 2) : 0);
+  const int64_t ct = std::max(blocks_of(g.x.cols, 64), g.rows ? blocks_of(g.row_chunks, 2) : 0);
+  if (rt * ct > 0x7fffffff) return hipErrorInvalidValue;
+  if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), dim3((unsigned)(rt * ct)), dim3(256), 0, s, g, ct);
+  else hipLaunchKernelGGL((k_planes<3, false>), dim3((unsigned)(rt * ct)), dim3(256), 0, s, g, ct);
   return hipGetLastError();
 }
 
@@ -706,7 +675,12 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
   TRY(op_space(c, al(xb) + al(wbytes) + al(room), &ws));
   uint8_t *xp = take<uint8_t>(*ws, xb), *wp = take<uint8_t>(*ws, wbytes);
   float *part = reinterpret_cast<float *>(ws->base + ws->used);
-  HIP_TRY(c, launch_planes(d, dev(static_cast<const vcr_mat *>(nullptr)), P, chunks, xp, c->stream));
+  PlanesArgs pl{};
+  pl.x = d;
+  pl.rows = xp;
+  pl.row_blocks = rb;
+  pl.row_chunks = chunks;
+  HIP_TRY(c, launch_planes(pl, c->stream));
   hipLaunchKernelGGL(k_mx_planes, dim3((unsigned)blocks_of(wb * (chunks / 4), 4)), dim3(256), 0, c->stream, dev(w), wp);
   HIP_TRY(c, hipGetLastError());
   NtArgs g{};
@@ -755,14 +729,34 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     b_xt = (size_t)kwb * mch * P * FRAG;
     b_part = std::max(b_part, P == 1 ? part_bytes<1, 1, false>(N, kw, mch) : part_bytes<3, 3, false>(N, kw, mch));
   }
-  if (db) b_sums = (size_t)mch * N * 4;
+  const int64_t mg = blocks_of(std::max<int64_t>(M, 1), 64);
+  if (db) b_sums = (size_t)mg * N * 4;
   Workspace *ws = nullptr;
   TRY(op_space(c, al(b_g) + al(b_wt) + al(b_gt) + al(b_xt) + al(b_sums) + al(b_part) + 6 * 256, &ws));
   uint8_t *gp = take<uint8_t>(*ws, b_g), *wt = take<uint8_t>(*ws, b_wt), *gt = take<uint8_t>(*ws, b_gt), *xt = take<uint8_t>(*ws, b_xt);
   float *sums = take<float>(*ws, b_sums / 4), *part = take<float>(*ws, b_part / 4);
-  const DevMat none = dev(static_cast<const vcr_mat *>(nullptr));
+  if (has_dx || dw || db) {   // g's rows, its columns and their sums in one pass
+    PlanesArgs pl{};
+    pl.x = g;
+    pl.y = mask;
+    if (has_dx) {
+      pl.rows = gp;
+      pl.row_blocks = mb;
+      pl.row_chunks = nch;
+    }
+    if (dw) {
+      pl.cols = gt;
+      pl.col_blocks = nb;
+      pl.col_chunks = mch;
+    }
+    pl.sums = db ? sums : nullptr;
+    HIP_TRY(c, launch_planes(pl, s));
+  }
+  if (db) {
+    hipLaunchKernelGGL(k_column_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, M > 0 ? mg : 0, N, db);
+    HIP_TRY(c, hipGetLastError());
+  }
   if (has_dx) {
-    HIP_TRY(c, launch_planes(g, mask, P, nch, gp, s));
     hipLaunchKernelGGL(k_mx_planes_t, dim3((unsigned)blocks_of(4 * nch * 4 * mx_groups(kx), 256)), dim3(256), 0, s, dev(w), nch, kxb, wt);
     HIP_TRY(c, hipGetLastError());
     NtArgs a{};
@@ -773,15 +767,13 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     if (P == 1) HIP_TRY(c, (nt_product<1, 1, false>(a, o, part, s)));
     else HIP_TRY(c, (nt_product<3, 1, false>(a, o, part, s)));
   }
-  if (dw || db) {
-    HIP_TRY(c, launch_planes_t(g, mask, mch, dw ? gt : nullptr, db ? sums : nullptr, s));
-    if (db) {
-      hipLaunchKernelGGL(k_column_sums, dim3((unsigned)blocks_of(N, 256)), dim3(256), 0, s, sums, mch, N, db);
-      HIP_TRY(c, hipGetLastError());
-    }
-  }
   if (dw) {
-    HIP_TRY(c, launch_planes_t(dev(x), none, mch, xt, nullptr, s));
+    PlanesArgs pl{};
+    pl.x = dev(x);
+    pl.cols = xt;
+    pl.col_blocks = kwb;
+    pl.col_chunks = mch;
+    HIP_TRY(c, launch_planes(pl, s));
     NtArgs a{};
     a.A = NtOperand{gt, nullptr, (int32_t)nb, 0};
     a.B = NtOperand{xt, nullptr, (int32_t)kwb, 0};

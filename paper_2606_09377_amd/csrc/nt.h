@@ -511,10 +511,10 @@ template <>
 struct NtTiles<1, 1, false> {
   typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
   typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
-  typedef NtTile<2, 4, 2, 2, 1, 1, 1, 2, 3> T2;
+  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
   typedef NtTile<2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
   typedef NtTile<2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .71f, 0.f}, {128, 128, .241f, .393f}, {64, 128, .154f, .273f}, {64, 64, .083f, .176f}, {32, 64, .052f, .142f}};
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .71f, 0.f}, {128, 128, .241f, .393f}, {64, 128, .148f, 0.f}, {64, 64, .083f, .176f}, {32, 64, .052f, .142f}};
 };
 template <>
 struct NtTiles<3, 1, false> {

@@ -49,31 +49,15 @@ __device__ __forceinline__ float ns_scale(const double *part, int batch, float e
   return (float)(1.0 / (sqrt(s) + (double)eps));
 }
 
-// X's parts from G: rows as they are, and transposed
+// X's parts from G, its rows' and its columns'
 template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_ns_rows(DevMat g, int vec, const double *part, float eps, int64_t row_blocks, int64_t chunks,
-                                                 uint8_t *out) {
-  const int lane = threadIdx.x & 63;
+__global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps) {
+  __shared__ float tile[64][65];
   const float sc = ns_scale(part, blockIdx.y, eps);
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rb = id / chunks, ch = id - rb * chunks;
-  if (rb >= row_blocks) return;
-  float v[8];
-  mat_row8<BF>(g, (int64_t)blockIdx.y * g.stride, rb * 16 + (lane & 15), ch * 32 + (lane >> 4) * 8, vec, v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= sc;
-  store_slot<P>(out + blockIdx.y * row_blocks * chunks * P * FRAG, id, lane, v);
-}
-template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_ns_cols(DevMat g, const double *part, float eps, int64_t row_blocks, int64_t chunks,
-                                                 uint8_t *out) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float sc = ns_scale(part, blockIdx.y, eps);
-  const int64_t nc = (row_blocks + 3) / 4, ch = blockIdx.x / nc, col = (blockIdx.x - ch * nc) * 64 + lane;
-  if (col >= row_blocks * 16) return;
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = sc * mat_at<BF>(g, (int64_t)blockIdx.y * g.stride, ch * 32 + wave * 8 + i, col);
-  store_slot<P>(out + blockIdx.y * row_blocks * chunks * P * FRAG, (col >> 4) * chunks + ch, wave * 16 + (int)(col & 15), v);
+  const int64_t tr = blockIdx.x / col_tiles, bytes = g.row_blocks * g.row_chunks * P * FRAG;   // of either
+  g.rows += blockIdx.y * bytes;
+  g.cols += blockIdx.y * bytes;
+  planes_tile<P, BF>(g, (int64_t)blockIdx.y * g.x.stride, tr, blockIdx.x - tr * col_tiles, sc, tile);
 }
 
 enum NsMode : int32_t { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2, NS_OUT = 3 };
@@ -157,11 +141,17 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
   // G's rows padded to rp, its columns to cp
   const int64_t rp = transposed ? np : mp, cp = transposed ? mp : np;
   uint8_t *rows = transposed ? sp.xt : sp.x, *cols = transposed ? sp.x : sp.xt;
-  hipLaunchKernelGGL((k_ns_rows<P, BF>), dim3((unsigned)blocks_of(rp / 16 * (cp / 32), 4), batch), dim3(256), 0, s, g, vec, sp.norm, eps,
-                     rp / 16, cp / 32, rows);
-  if ((err = hipGetLastError()) != hipSuccess) return err;
-  hipLaunchKernelGGL((k_ns_cols<P, BF>), dim3((unsigned)(blocks_of(cp, 64) * (rp / 32)), batch), dim3(256), 0, s, g, sp.norm, eps, cp / 16,
-                     rp / 32, cols);
+  PlanesArgs pl{};
+  pl.x = g;
+  pl.vec = vec;
+  pl.rows = rows;
+  pl.row_blocks = rp / 16;
+  pl.row_chunks = cp / 32;
+  pl.cols = cols;
+  pl.col_blocks = cp / 16;
+  pl.col_chunks = rp / 32;
+  const int64_t ct = blocks_of(cp, 64);
+  hipLaunchKernelGGL((k_ns_planes<P, BF>), dim3((unsigned)(blocks_of(rp, 64) * ct), batch), dim3(256), 0, s, pl, ct, sp.norm, eps);
   if ((err = hipGetLastError()) != hipSuccess) return err;
   e.mp = (int32_t)mp;
   e.np = (int32_t)np;

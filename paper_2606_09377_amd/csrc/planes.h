@@ -103,6 +103,68 @@ __device__ __forceinline__ void store_slot(uint8_t *planes, int64_t frag, int l,
     *reinterpret_cast<uint4 *>(planes + (frag * P + p) * FRAG + l * 16) = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
 }
 
+// Operands made from a matrix, its rows and its columns in one pass (either may be null): a workgroup takes 64 x 64 values, a
+// wave 16 rows of them as the fragments of its row block, the transposed ones from LDS.  Bound by memory.
+//   x      rows x cols of it, or only those where y > 0; times scale
+//   rows   operand of x's rows, row_chunks chunks of 32 columns
+//   cols   operand of x's columns, col_chunks chunks of 32 rows
+//   sums   [64-row group][cols]: column sums (null: none)
+// Chunks beyond x hold zeros; row blocks beyond x's rows or columns, rounded up to 16, are not written unless they are
+// below row_blocks, col_blocks.
+struct PlanesArgs {
+  DevMat x, y;
+  int32_t vec;
+  uint8_t *rows, *cols;
+  int64_t row_blocks, row_chunks, col_blocks, col_chunks;
+  float *sums;
+};
+template <int P, bool BF>
+__device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, float scale, float (&tile)[64][65]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, oct = lane >> 4;
+  const int64_t rb = tr * 4 + wave, row = rb * 16 + r;
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t col = tc * 64 + h * 32 + oct * 8;
+    mat_row8<BF>(g.x, base, row, col, g.vec, v[h]);
+    if (g.y.p) {
+      float m[8];
+      mat_row8<BF>(g.y, base, row, col, g.vec, m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[h][i] = m[i] > 0.f ? v[h][i] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[h][i] *= scale;
+    const int64_t ch = tc * 2 + h;
+    if (g.rows && rb < g.row_blocks && ch < g.row_chunks) store_slot<P>(g.rows, rb * g.row_chunks + ch, lane, v[h]);
+  }
+  if (!g.cols && !g.sums) return;   // uniform
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tile[wave * 16 + r][h * 32 + oct * 8 + i] = v[h][i];
+  __syncthreads();
+  // wave: 16 columns; lane: column r, rows 32 h + 8 oct ..
+  float s = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      t[i] = tile[h * 32 + oct * 8 + i][wave * 16 + r];
+      s += t[i];
+    }
+    const int64_t cb = tc * 4 + wave, ch = tr * 2 + h;
+    if (g.cols && cb < g.col_blocks && ch < g.col_chunks) store_slot<P>(g.cols, cb * g.col_chunks + ch, lane, t);
+  }
+  if (g.sums) {
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    const int64_t col = tc * 64 + wave * 16 + r;
+    if (oct == 0 && col < g.x.cols) g.sums[tr * g.x.cols + col] = s;
+  }
+}
+
 // Four consecutive k of one row, into an operand of P parts with so many chunks
 template <int P>
 __device__ __forceinline__ void store_quad(uint8_t *planes, int64_t row, int64_t k, int64_t chunks, f32v4 v) {
