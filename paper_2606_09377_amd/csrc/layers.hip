@@ -19,11 +19,6 @@ namespace vcr {
 // ---- 4-bit values ---------------------------------------------------------------------------
 __host__ __device__ inline int64_t mx_groups(int64_t cols) { return (cols + 127) / 128; }
 
-// the float of a scale byte, as the conversions take it
-__device__ __forceinline__ float mx_scale(uint32_t byte) {
-  return __builtin_bit_cast(float, byte == 255 ? 0x7fc00000u : byte == 0 ? 0x00400000u : byte << 23);
-}
-
 struct MxDev {
   const uint8_t *codes, *scales;
   int64_t rows, cols;
@@ -87,12 +82,6 @@ __device__ __forceinline__ void mx_block(const MxDev &w, int64_t rb, int64_t grp
   q = *reinterpret_cast<const uint4 *>(w.codes + ((rb * groups + grp) * 64 + lane) * 16);
   s = mx_scale(w.scales[mx_scale_at(rb, grp, groups, lane)]);
 }
-__device__ __forceinline__ uint4 mx_to_bf16(uint32_t u, float s) {   // eight values
-  auto c = [](auto v) { return __builtin_bit_cast(uint32_t, v); };
-  return make_uint4(c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 0)), c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 1)),
-                    c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 2)), c(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 3)));
-}
-
 // The reverse, with the same division of work
 template <bool BF>
 __global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t ld, int vec) {
@@ -149,21 +138,6 @@ __global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t 
   part[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && c < cols) out[c] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-}
-
-// 4-bit weights as a bf16 operand (exact): a thread per block
-__global__ __launch_bounds__(256) void k_mx_planes(MxDev w, uint8_t *out) {
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int64_t groups = mx_groups(w.cols), id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t rb = id / groups, grp = id - rb * groups;
-  if (rb * 16 >= w.rows) return;
-  uint4 q;
-  float s;
-  mx_block(w, rb, grp, groups, lane, q, s);
-  const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-  uint8_t *d = out + (rb * groups * 4 + grp * 4 + g) * FRAG + r * 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(d + i * 256) = mx_to_bf16(u[i], s);
 }
 
 // The transposed weights as a bf16 operand, rows k and contraction n: a thread per 32 k of 8 rows n
@@ -246,23 +220,23 @@ __global__ __launch_bounds__(256) void k_join(const float *p, int parts, int64_t
 // ---- products by tiles ------------------------------------------------------------------------
 // Parts of the contraction: few tiles over a long contraction leave compute units idle.  Parts of 16 chunks and more are
 // then summed by their own workgroups (the smallest shape) and joined in order, where that pays for the second launch.
-template <int PA, int PB, bool FP4>
+template <int PA, int PB, int KIND>
 static int nt_parts(int64_t M, int64_t N, int64_t chunks) {
-  const NtShape *sh = NtTiles<PA, PB, FP4>::shapes, &x = sh[NT_SHAPES - 1];
+  const NtShape *sh = NtTiles<PA, PB, KIND>::shapes, &x = sh[NT_SHAPES - 1];
   const int64_t t = nt_tiles(M, N, x.bm, x.bn, false), parts = std::min<int64_t>(NT_CUS / t, chunks / 16);
   if (parts < 2) return 1;
   return nt_us(x, t * parts, (chunks + parts - 1) / parts) + NT_LAUNCH_US < nt_plan(sh, M, N, chunks, 1, false).us ? (int)parts : 1;
 }
-template <int PA, int PB, bool FP4>
+template <int PA, int PB, int KIND>
 static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
-  const int parts = nt_parts<PA, PB, FP4>(M, N, chunks);
+  const int parts = nt_parts<PA, PB, KIND>(M, N, chunks);
   return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
 }
 // D = A B^T into o; part: room for part_bytes
-template <int PA, int PB, bool FP4>
+template <int PA, int PB, int KIND>
 static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipStream_t s) {
-  typedef NtTiles<PA, PB, FP4> TS;
-  const int parts = nt_parts<PA, PB, FP4>(o.rows, o.cols, g.chunks);
+  typedef NtTiles<PA, PB, KIND> TS;
+  const int parts = nt_parts<PA, PB, KIND>(o.rows, o.cols, g.chunks);
   if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, EpiOut{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
   const NtShape &x = TS::shapes[NT_SHAPES - 1];
@@ -639,9 +613,9 @@ vcr_status vcr_mx_product(vcr_ctx *c, const vcr_mx *a, const vcr_mx *w, const fl
   g.B = NtOperand{w->codes, w->scales, (int32_t)blocks_of(w->rows, 16), 0};
   g.chunks = (int32_t)mx_groups(a->cols);
   Workspace *ws = nullptr;
-  const size_t room = part_bytes<1, 1, true>(y->rows, y->cols, g.chunks);
+  const size_t room = part_bytes<1, 1, NT_FP4>(y->rows, y->cols, g.chunks);
   TRY(op_space(c, room, &ws));
-  HIP_TRY(c, (nt_product<1, 1, true>(g, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
+  HIP_TRY(c, (nt_product<1, 1, NT_FP4>(g, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
   return op_end(c);
 }
 
@@ -668,28 +642,27 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
     else HIP_TRY(c, (launch_rows<3, false>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
     return op_end(c);
   }
-  const int64_t chunks = 4 * mx_groups(x->cols), rb = blocks_of(x->rows, 16), wb = blocks_of(w->rows, 16);
-  const size_t room = d.bf16 ? part_bytes<1, 1, false>(y->rows, y->cols, chunks) : part_bytes<3, 1, false>(y->rows, y->cols, chunks);
-  const size_t xb = (size_t)rb * chunks * P * FRAG, wbytes = (size_t)wb * chunks * FRAG;
+  const int64_t chunks = 4 * mx_groups(x->cols), rb = blocks_of(x->rows, 16);
+  const size_t room = d.bf16 ? part_bytes<1, 1, NT_MIXED>(y->rows, y->cols, chunks) : part_bytes<3, 1, NT_MIXED>(y->rows, y->cols, chunks);
+  const size_t xb = (size_t)rb * chunks * P * FRAG;
   Workspace *ws = nullptr;
-  TRY(op_space(c, al(xb) + al(wbytes) + al(room), &ws));
-  uint8_t *xp = take<uint8_t>(*ws, xb), *wp = take<uint8_t>(*ws, wbytes);
+  TRY(op_space(c, al(xb) + al(room), &ws));
+  uint8_t *xp = take<uint8_t>(*ws, xb);
   float *part = reinterpret_cast<float *>(ws->base + ws->used);
   PlanesArgs pl{};
   pl.x = d;
   pl.rows = xp;
   pl.row_blocks = rb;
   pl.row_chunks = chunks;
+  pl.grouped = 1;
   HIP_TRY(c, launch_planes(pl, c->stream));
-  hipLaunchKernelGGL(k_mx_planes, dim3((unsigned)blocks_of(wb * (chunks / 4), 4)), dim3(256), 0, c->stream, dev(w), wp);
-  HIP_TRY(c, hipGetLastError());
   NtArgs g{};
   g.A = NtOperand{xp, nullptr, (int32_t)rb, 0};
-  g.B = NtOperand{wp, nullptr, (int32_t)wb, 0};
+  g.B = NtOperand{w->codes, w->scales, (int32_t)blocks_of(w->rows, 16), 0};
   g.chunks = (int32_t)chunks;
   const OutMat o = out_mat(y, bias, relu != 0);
-  if (d.bf16) HIP_TRY(c, (nt_product<1, 1, false>(g, o, part, c->stream)));
-  else HIP_TRY(c, (nt_product<3, 1, false>(g, o, part, c->stream)));
+  if (d.bf16) HIP_TRY(c, (nt_product<1, 1, NT_MIXED>(g, o, part, c->stream)));
+  else HIP_TRY(c, (nt_product<3, 1, NT_MIXED>(g, o, part, c->stream)));
   return op_end(c);
 }
 
@@ -722,12 +695,12 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
   if (has_dx) {
     b_g = (size_t)mb * nch * P * FRAG;
     b_wt = (size_t)kxb * nch * FRAG;
-    b_part = P == 1 ? part_bytes<1, 1, false>(M, kx, nch) : part_bytes<3, 1, false>(M, kx, nch);
+    b_part = P == 1 ? part_bytes<1, 1, NT_BF16>(M, kx, nch) : part_bytes<3, 1, NT_BF16>(M, kx, nch);
   }
   if (dw) {
     b_gt = (size_t)nb * mch * P * FRAG;
     b_xt = (size_t)kwb * mch * P * FRAG;
-    b_part = std::max(b_part, P == 1 ? part_bytes<1, 1, false>(N, kw, mch) : part_bytes<3, 3, false>(N, kw, mch));
+    b_part = std::max(b_part, P == 1 ? part_bytes<1, 1, NT_BF16>(N, kw, mch) : part_bytes<3, 3, NT_BF16>(N, kw, mch));
   }
   const int64_t mg = blocks_of(std::max<int64_t>(M, 1), 64);
   if (db) b_sums = (size_t)mg * N * 4;
@@ -764,8 +737,8 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     a.B = NtOperand{wt, nullptr, (int32_t)kxb, 0};
     a.chunks = (int32_t)nch;
     const OutMat o = out_mat(dx, nullptr, 0);
-    if (P == 1) HIP_TRY(c, (nt_product<1, 1, false>(a, o, part, s)));
-    else HIP_TRY(c, (nt_product<3, 1, false>(a, o, part, s)));
+    if (P == 1) HIP_TRY(c, (nt_product<1, 1, NT_BF16>(a, o, part, s)));
+    else HIP_TRY(c, (nt_product<3, 1, NT_BF16>(a, o, part, s)));
   }
   if (dw) {
     PlanesArgs pl{};
@@ -779,8 +752,8 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     a.B = NtOperand{xt, nullptr, (int32_t)kwb, 0};
     a.chunks = (int32_t)mch;
     const OutMat o = out_mat(dw, nullptr, 0);
-    if (P == 1) HIP_TRY(c, (nt_product<1, 1, false>(a, o, part, s)));
-    else HIP_TRY(c, (nt_product<3, 3, false>(a, o, part, s)));
+    if (P == 1) HIP_TRY(c, (nt_product<1, 1, NT_BF16>(a, o, part, s)));
+    else HIP_TRY(c, (nt_product<3, 3, NT_BF16>(a, o, part, s)));
   }
   return op_end(c);
 }

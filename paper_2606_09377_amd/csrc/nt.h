@@ -8,6 +8,10 @@
 // registers by one conflict-free 16-byte read a lane, with no swizzle and no edge: padding rows and
 // columns are in memory, and hold zeros.
 //
+// A bf16 operand may meet a 4-bit one as it is stored (NT_MIXED): the four chunks of a group of 128 are then, for both, the
+// first to fourth eight columns of each of its blocks of 32, so that the 16 bytes a lane has of a 4-bit fragment
+// are its columns of four instructions in turn; they become bf16 in registers, exactly, where they are multiplied.
+//
 // Parts.  float32 values are three bf16 parts h + m + l (split_bf16.h); P parts keep 8 P bits.  Products of
 // (A parts, B parts), in order of their size:
 //   (1, 1)  h h
@@ -33,6 +37,7 @@
 #include <type_traits>
 
 #include "lds_dma.h"
+#include "mx_bits.h"
 #include "split_bf16.h"
 
 namespace vcr {
@@ -59,24 +64,28 @@ struct NtArgs {
   int32_t bm, bn, n_mt, n_nt, tiles, first, sub_m, sub_n;
 };
 
-template <int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_, bool FP4_ = false>
+enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2 };   // both bf16, both 4-bit, A bf16 (grouped) and B 4-bit
+
+template <int KIND_, int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_>
 struct NtTile {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, PA = PA_, PB = PB_, KS = KS_, NS = NS_;
-  static constexpr bool FP4 = FP4_;
+  static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED;
   static constexpr int PRODUCTS = PA == 3 && PB == 3 ? 6 : PA > 1 ? 3 : 1;
   static constexpr int KW = KS / WK;   // chunks of a stage that a wave multiplies
   static constexpr int NW = WM * WN * WK, T = 64 * NW;
   static constexpr int BM = 16 * MB * WM, BN = 16 * NB * WN;
   static constexpr bool TWO = PA == 3;   // an accumulator for the small products
-  static constexpr int FA = BM / 16 * KS * PA, FB = BN / 16 * KS * PB;   // fragments of a stage
-  static constexpr int SA = FP4 ? BM / 16 : 0, SB = FP4 ? BN / 16 : 0;   // scale loads (256 bytes) of a stage
-  static constexpr int SQ = (SA + SB + NW - 1) / NW;                     // of a wave (the last ones' may be the same)
-  static constexpr int LOADS = (FA + FB) / NW + SQ;                      // of a wave
+  static constexpr int BF = MIXED ? KS / 4 : KS * PB;              // fragments of a stage of 16 columns
+  static constexpr int FA = BM / 16 * KS * PA, FB = BN / 16 * BF;   // fragments of a stage
+  static constexpr int SA = FP4 ? BM / 16 : 0, SB = FP4 || MIXED ? BN / 16 : 0;   // scale loads (256 bytes) of a stage
+  static constexpr int FQ = (FA + FB + NW - 1) / NW, SQ = (SA + SB + NW - 1) / NW;
+  static constexpr int LOADS = FQ + SQ;   // of a wave (the last of them may be the same for several)
   static constexpr int STAGE = (FA + FB) * FRAG + (SA + SB) * 256;
   static constexpr int LDS = NS * STAGE;
-  static_assert(FA % NW == 0 && FB % NW == 0, "loads spread evenly over the waves");
   static_assert(!FP4 || 4 % KS == 0, "a stage's scales are in one group of four chunks");
+  static_assert(!MIXED || (KS == 4 && PB == 1), "a stage is a group");
   static_assert(KS % WK == 0 && (WK == 1 || NW * MB * NB * 1024 <= LDS), "waves that share a block");
+  static_assert(KW == 1 || KW % 2 == 0, "register sets alternate");
 };
 
 // 4 bytes a lane from a wave-uniform base into LDS (dma16's form)
@@ -158,28 +167,31 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   if (rb0 >= g.A.row_blocks || cb0 >= g.B.row_blocks || (g.tri && cb0 >= rb0 + T::BM / 16)) return;
   const int kc0 = blockIdx.y * g.z_chunks, kc1 = min(g.chunks, kc0 + g.z_chunks);
   const int KT = (kc1 - kc0 + KS - 1) / KS;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)lds + wave * FRAG;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)lds;
 
   // Loads: a wave-uniform address of the tile's first row block and the stage, and each load's own offset from it,
   // formed once (32 bits: launch_nt).  Row blocks beyond the last one read that.  (Forming the addresses anew for every
   // load cost a wave that has its SIMD to itself as much time as its products.)
+  const int b_chunks = T::MIXED ? g.chunks / 4 : g.chunks, bk0 = T::MIXED ? kc0 / 4 : kc0;   // B's fragments of a row block
   const uint8_t *a_base = g.A.p + batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG;
-  const uint8_t *b_base = g.B.p + batch * g.B.stride + ((int64_t)cb0 * g.chunks + kc0) * PB * FRAG;
-  uint32_t a_off[T::FA / NW], b_off[T::FB / NW];
+  const uint8_t *b_base = g.B.p + batch * g.B.stride + ((int64_t)cb0 * b_chunks + bk0) * PB * FRAG;
+  uint32_t f_off[T::FQ];
 #pragma unroll
-  for (int q = 0; q < T::FA / NW; ++q) {
-    const int f = q * NW + wave, i = f / (KS * PA), kp = f - i * (KS * PA);
-    a_off[q] = ((uint32_t)min(i, g.A.row_blocks - 1 - rb0) * g.chunks * PA + kp) * FRAG + lane * 16;
+  for (int q = 0; q < T::FQ; ++q) {
+    const int f = min(q * NW + wave, T::FA + T::FB - 1);
+    if (f < T::FA) {   // wave-uniform
+      const int i = f / (KS * PA);
+      f_off[q] = ((uint32_t)min(i, g.A.row_blocks - 1 - rb0) * g.chunks * PA + (f - i * (KS * PA))) * FRAG + lane * 16;
+    } else {
+      const int i = (f - T::FA) / T::BF;
+      f_off[q] = ((uint32_t)min(i, g.B.row_blocks - 1 - cb0) * b_chunks * PB + (f - T::FA - i * T::BF)) * FRAG + lane * 16;
+    }
   }
-#pragma unroll
-  for (int q = 0; q < T::FB / NW; ++q) {
-    const int f = q * NW + wave, i = f / (KS * PB), kp = f - i * (KS * PB);
-    b_off[q] = ((uint32_t)min(i, g.B.row_blocks - 1 - cb0) * g.chunks * PB + kp) * FRAG + lane * 16;
-  }
-  // scales: of four chunks together
-  const int c4 = (g.chunks + 3) / 4;
-  const uint8_t *s_base[T::FP4 ? T::SQ : 1];
-  if constexpr (T::FP4) {
+  // scales: of four fragments together
+  constexpr bool SCALES = T::SQ > 0;
+  const int c4 = (b_chunks + 3) / 4;
+  const uint8_t *s_base[SCALES ? T::SQ : 1];
+  if constexpr (SCALES) {
 #pragma unroll
     for (int q = 0; q < T::SQ; ++q) {
       const int i = min(q * NW + wave, T::SA + T::SB - 1);
@@ -194,28 +206,27 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     int at4, over;   // over: chunks of the stage beyond the contraction
   };
   auto stage = [&](int kt, int buf) {
-    return Stage{a_base + (int64_t)kt * (KS * PA * FRAG), b_base + (int64_t)kt * (KS * PB * FRAG), lds0 + buf * T::STAGE,
-                 (kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS)};
+    return Stage{a_base + (int64_t)kt * (KS * PA * FRAG), b_base + (int64_t)kt * (T::BF * FRAG), lds0 + buf * T::STAGE,
+                 (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS)};
   };
   auto load = [&](const Stage &s, int q, auto last) {   // load q < LOADS of this wave
-    constexpr int QA = T::FA / NW, QB = T::FB / NW;
-    if (q < QA + QB) {
-      const int qq = q < QA ? q : q - QA, P = q < QA ? PA : PB;
-      uint32_t off = q < QA ? a_off[qq] : b_off[qq];
+    if (q < T::FQ) {
+      const int f = min(q * NW + wave, T::FA + T::FB - 1);
+      const bool is_a = (q + 1) * NW <= T::FA || (q * NW < T::FA && f < T::FA);
+      uint32_t off = f_off[q];
       if constexpr (decltype(last)::value) {   // the contraction's last chunk is read in the place of those beyond it
-        const int kc = (qq * NW + wave) % (KS * P) / P;
+        const int P = is_a ? PA : PB, kc = (is_a ? f : f - T::FA) % (KS * P) / P;
         off -= max(0, kc - (KS - s.over - 1)) * (P * FRAG);
       }
-      nt_dma(q < QA ? s.a : s.b, off, s.lds + ((q < QA ? 0 : T::FA) + qq * NW) * FRAG, true);
-    } else if constexpr (T::FP4) {
-      const int qq = q - QA - QB;
-      nt_dma(s_base[qq] + s.at4, lane * 4,
-             s.lds - wave * FRAG + (T::FA + T::FB) * FRAG + min(qq * NW + wave, T::SA + T::SB - 1) * 256, false);
+      nt_dma(is_a ? s.a : s.b, off, s.lds + f * FRAG, true);
+    } else if constexpr (SCALES) {
+      const int i = min((q - T::FQ) * NW + wave, T::SA + T::SB - 1);
+      nt_dma(s_base[q - T::FQ] + s.at4, lane * 4, s.lds + (T::FA + T::FB) * FRAG + i * 256, false);
     }
   };
   auto issue = [&](int kt, int buf) {
     const Stage s = stage(kt, buf);
-    if (KS == 1 || s.over <= 0) {
+    if (KS == 1 || T::MIXED || s.over <= 0) {
 #pragma unroll
       for (int q = 0; q < T::LOADS; ++q) load(s, q, std::false_type{});
     } else {
@@ -233,16 +244,20 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       if constexpr (T::TWO) lo[i][j] = f32v4{0.f, 0.f, 0.f, 0.f};
     }
 
-  // operands of a wave's chunk from LDS: columns' fragments, and rows' one by one
+  // operands of a wave's chunk in registers; of a 4-bit B, the stage's
   struct Chunk {
-    bf16x8 b[NB][PB], a[MB][PA];
+    bf16x8 b[T::MIXED ? 1 : NB][PB], a[MB][PA];
     int bs[T::FP4 ? NB : 1], as[T::FP4 ? MB : 1];
   };
-  auto read_a = [&](Chunk &c, int at, int kt, const uint8_t *st, int kc, int i, int p) {
-    c.a[at][p] = *reinterpret_cast<const bf16x8 *>(st + (((wm * MB + i) * KS + kc) * PA + p) * FRAG + lane * 16);
+  constexpr int CW = T::WK == 1 ? 4 : T::KW;   // words of a 4-bit fragment that a wave multiplies
+  struct Codes {
+    uint32_t w[NB][CW], s[NB];
+  };
+  auto read_a = [&](Chunk &c, int kt, const uint8_t *st, int kc, int i, int p) {
+    c.a[i][p] = *reinterpret_cast<const bf16x8 *>(st + (((wm * MB + i) * KS + kc) * PA + p) * FRAG + lane * 16);
     if constexpr (T::FP4) {
       const uint32_t *s = reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG) + lane;
-      c.as[at] = (int)(s[(wm * MB + i) * 64] >> 8 * ((kc0 + kt * KS + kc) & 3));
+      c.as[i] = (int)(s[(wm * MB + i) * 64] >> 8 * ((kc0 + kt * KS + kc) & 3));
     }
   };
   auto read_b = [&](Chunk &c, int kt, const uint8_t *st, int kc, int j, int p) {
@@ -252,7 +267,19 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       c.bs[j] = (int)(s[(T::SA + wn * NB + j) * 64] >> 8 * ((kc0 + kt * KS + kc) & 3));
     }
   };
-  auto multiply = [&](const Chunk &c, int at, int i, int p) {   // product p of row block i with the wave's columns
+  auto read_codes = [&](Codes &c, int kt, const uint8_t *st, int j) {
+    const uint8_t *f = st + (T::FA + wn * NB + j) * FRAG + lane * 16;
+    if constexpr (T::WK == 1) {
+      const i32x4 q = *reinterpret_cast<const i32x4 *>(f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c.w[j][k] = (uint32_t)q[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < CW; ++k) c.w[j][k] = *reinterpret_cast<const uint32_t *>(f + (k * T::WK + wk) * 4);
+    }
+    c.s[j] = *reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG + (wn * NB + j) * 256 + lane * 4) >> 8 * ((bk0 + kt) & 3);
+  };
+  auto multiply = [&](const Chunk &c, const bf16x8 (&mixed)[T::MIXED ? NB : 1], int i, int p) {   // product p of row block i with the wave's columns
     if constexpr (T::FP4) {
       auto wide = [](bf16x8 v) {
         const i32x4 q = __builtin_bit_cast(i32x4, v);
@@ -260,7 +287,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       };
 #pragma unroll
       for (int j = 0; j < NB; ++j)
-        hi[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(c.b[j][0]), wide(c.a[at][0]), hi[i][j], 4, 4, 0, c.bs[j], 0, c.as[at]);
+        hi[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(c.b[j][0]), wide(c.a[i][0]), hi[i][j], 4, 4, 0, c.bs[j], 0, c.as[i]);
     } else {
       // (A part, B part) and accumulator of product p
       constexpr int pa33[6] = {0, 2, 1, 0, 1, 0}, pb33[6] = {2, 0, 1, 1, 0, 0}, pa31[3] = {2, 1, 0}, pa22[3] = {0, 1, 0}, pb22[3] = {1, 0, 0};
@@ -270,7 +297,8 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         f32v4 &acc = small ? lo[T::TWO ? i : 0][T::TWO ? j : 0] : hi[i][j];
-        acc = mfma_bf16(c.b[j][pb], c.a[at][pa], acc);
+        if constexpr (T::MIXED) acc = mfma_bf16(mixed[j], c.a[i][pa], acc);
+        else acc = mfma_bf16(c.b[j][pb], c.a[i][pa], acc);
       }
     }
   };
@@ -281,58 +309,99 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   };
 
   static_assert(NS >= 2 && NS <= 4, "at most two stages in flight behind the one waited for");
-  // Step kt: stage kt + 1 has landed; the barrier publishes it and frees stage kt, whose operands every wave has in
-  // registers, for stage kt + NS.  (Two register sets, the loop unrolled by two, so that no set is copied.)
-  constexpr int KW = T::KW, READS = KW * (NB * PB + MB * PA), GROUPS = KW * MB * T::PRODUCTS;
-  struct Set {
-    Chunk c[KW];
+  // A wave's chunks in turn: chunk k of stage kt is multiplied while the operands of the next one are read.  With the last
+  // chunk of a stage, stage kt + 1 has landed; the barrier publishes it and frees stage kt, whose operands every wave has
+  // in registers, for stage kt + NS.  (Two register sets, and the loop takes two stages at a time, so that none is copied.)
+  constexpr int KW = T::KW, AREADS = MB * PA, BREADS = T::MIXED ? 0 : NB * PB, GROUPS = MB * T::PRODUCTS;
+  Chunk set[2];
+  Codes codes[T::MIXED ? 2 : 1];
+  auto read = [&](Chunk &c, Codes &q, int kt, int k, int n) {   // read n of chunk k of stage kt, and of a stage's codes with its first
+    const uint8_t *st = lds + kt % NS * T::STAGE;
+    if (n < BREADS) read_b(c, kt, st, k * T::WK + wk, n / PB, n % PB);
+    else if (n < BREADS + AREADS) read_a(c, kt, st, k * T::WK + wk, (n - BREADS) / PA, (n - BREADS) % PA);
+    else if constexpr (T::MIXED) read_codes(q, kt, st, n - BREADS - AREADS);
   };
-  auto read = [&](Set &s, int kt, const uint8_t *st, int n) {   // read n < READS of a stage
-    const int k = n / (NB * PB + MB * PA), m = n % (NB * PB + MB * PA);
-    if (m < NB * PB) read_b(s.c[k], kt, st, k * T::WK + wk, m / PB, m % PB);
-    else read_a(s.c[k], (m - NB * PB) / PA, kt, st, k * T::WK + wk, (m - NB * PB) / PA, (m - NB * PB) % PA);
+  auto reads = [](int k) { return BREADS + AREADS + (T::MIXED && k == 0 ? NB : 0); };
+  // 4-bit columns as bf16: those of a stage's first chunk ahead of its products, the later ones' between the products before
+  bf16x8 mixed[2][T::MIXED ? NB : 1];
+  float m_scale[T::MIXED ? NB : 1];
+  auto expand = [&](const Codes &q, int k, int j) {
+    if constexpr (T::MIXED) {
+      if (k == 0) m_scale[j] = mx_scale(q.s[j] & 255);
+      mixed[k & 1][j] = __builtin_bit_cast(bf16x8, mx_to_bf16(q.w[j][k], m_scale[j]));
+    }
   };
-  auto group = [&](const Set &s, int n) {   // group n < GROUPS of NB matrix instructions of a stage
-    const int k = n / (MB * T::PRODUCTS), i = n / T::PRODUCTS % MB;
-    multiply(s.c[k], i, i, n % T::PRODUCTS);
-  };
-  // `now` is in registers: told to the compiler before the reads of `next`, whose end it would otherwise wait for before
+  // `now` is in registers: told to the compiler before the reads of the next set, whose end it would otherwise wait for before
   // the products of `now`
   auto arrived = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
-  auto steady = [&](int kt, const Set &now, Set &next) {   // kt + NS + 1 < KT
-    arrived();
-    wait_vmcnt<(NS - 2) * T::LOADS>();
-    barrier_only();
-    const uint8_t *st = lds + (kt + 1) % NS * T::STAGE;
-    const Stage ns = stage(kt + NS, kt % NS);
-    // Loads and reads are spread between the groups: a wave issues in order, and would stand still until LDS and the
-    // memory pipe have taken all of them.
+  auto steady = [&](int kt, auto sp) {   // stage kt (sp: its parity), kt + NS + 1 < KT
+    constexpr int SP = decltype(sp)::value;
 #pragma unroll
-    for (int n = 0; n < GROUPS; ++n) {
+    for (int k = 0; k < KW; ++k) {
+      const Chunk &now = set[(SP * KW + k) & 1];
+      Chunk &next = set[(SP * KW + k + 1) & 1];
+      const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
+      Codes &ncodes = codes[T::MIXED ? SP ^ 1 : 0];   // (read with a stage's first chunk)
+      arrived();
+      Stage ns{};
+      if (k + 1 == KW) {
+        wait_vmcnt<(NS - 2) * T::LOADS>();
+        barrier_only();
+        ns = stage(kt + NS, kt % NS);
+      }
+      if (T::MIXED && k == 0) {
 #pragma unroll
-      for (int q = n * T::LOADS / GROUPS; q < (n + 1) * T::LOADS / GROUPS; ++q) load(ns, q, std::false_type{});
+        for (int j = 0; j < NB; ++j) expand(codes[T::MIXED ? SP : 0], 0, j);
+      }
+      // Loads and reads are spread between the groups: a wave issues in order, and would stand still until LDS and the
+      // memory pipe have taken all of them.
 #pragma unroll
-      for (int q = n * READS / GROUPS; q < (n + 1) * READS / GROUPS; ++q) read(next, kt + 1, st, q);
-      group(now, n);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int n = 0; n < GROUPS; ++n) {
+        if (k + 1 == KW) {
+#pragma unroll
+          for (int q = n * T::LOADS / GROUPS; q < (n + 1) * T::LOADS / GROUPS; ++q) load(ns, q, std::false_type{});
+        }
+#pragma unroll
+        for (int q = n * reads(nk) / GROUPS; q < (n + 1) * reads(nk) / GROUPS; ++q) read(next, ncodes, nkt, nk, q);
+        if (T::MIXED && k + 1 < KW) {
+#pragma unroll
+          for (int j = n * NB / GROUPS; j < (n + 1) * NB / GROUPS; ++j) expand(codes[T::MIXED ? SP : 0], k + 1, j);
+        }
+        multiply(now, mixed[k & 1], n / T::PRODUCTS, n % T::PRODUCTS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
-  auto step = [&](int kt, const Set &now, Set &next) {
-    arrived();
-    if (kt + 1 < KT) {
-      landed(kt + 1, NS - 2);
-      barrier_only();
-      if (kt + NS < KT) issue(kt + NS, kt % NS);
-      const uint8_t *st = lds + (kt + 1) % NS * T::STAGE;
-#pragma unroll
-      for (int n = 0; n < READS; ++n) read(next, kt + 1, st, n);
-    }
+  auto last = [&](int kt, auto sp) {   // the same, of the last stages
+    constexpr int SP = decltype(sp)::value;
     const int left = kc1 - kc0 - kt * KS;
 #pragma unroll
-    for (int n = 0; n < GROUPS; ++n)
-      if (n / (MB * T::PRODUCTS) * T::WK + wk < left) group(now, n);   // wave-uniform
+    for (int k = 0; k < KW; ++k) {
+      const Chunk &now = set[(SP * KW + k) & 1];
+      Chunk &next = set[(SP * KW + k + 1) & 1];
+      const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
+      arrived();
+      if (k + 1 == KW && nkt < KT) {
+        landed(nkt, NS - 2);
+        barrier_only();
+        if (kt + NS < KT) issue(kt + NS, kt % NS);
+      }
+      if (nkt < KT) {
+#pragma unroll
+        for (int n = 0; n < reads(nk); ++n) read(next, codes[T::MIXED ? SP ^ 1 : 0], nkt, nk, n);
+      }
+      if (k * T::WK + wk < left) {   // wave-uniform
+        if constexpr (T::MIXED) {
+#pragma unroll
+          for (int j = 0; j < NB; ++j) expand(codes[T::MIXED ? SP : 0], k, j);
+        }
+#pragma unroll
+        for (int n = 0; n < GROUPS; ++n) multiply(now, mixed[k & 1], n / T::PRODUCTS, n % T::PRODUCTS);
+      }
+    }
   };
-  Set s0, s1;
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
   if (KT > 0) {
 #pragma unroll
     for (int t = 0; t < NS; ++t)
@@ -344,17 +413,17 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     else wait_vmcnt<0>();
     barrier_only();
 #pragma unroll
-    for (int n = 0; n < READS; ++n) read(s0, 0, lds, n);
+    for (int n = 0; n < reads(0); ++n) read(set[0], codes[0], 0, 0, n);
   }
   int kt = 0;
   for (; kt + NS + 2 < KT; kt += 2) {
-    steady(kt, s0, s1);
-    steady(kt + 1, s1, s0);
+    steady(kt, Even{});
+    steady(kt + 1, Odd{});
   }
 #pragma unroll 1
   for (; kt < KT; kt += 2) {
-    step(kt, s0, s1);
-    if (kt + 1 < KT) step(kt + 1, s1, s0);
+    last(kt, Even{});
+    if (kt + 1 < KT) last(kt + 1, Odd{});
   }
 
   const int r16 = lane & 15, g4 = lane >> 4;
@@ -496,52 +565,71 @@ hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, 
 }
 
 // The shapes of products of PA and PB parts
-template <int PA, int PB, bool FP4>
+template <int PA, int PB, int KIND>
 struct NtTiles;
 template <>
-struct NtTiles<1, 1, true> {
-  typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4, true> T0;
-  typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4, true> T1;
-  typedef NtTile<2, 4, 2, 2, 1, 1, 1, 1, 4, true> T2;
-  typedef NtTile<2, 2, 2, 2, 1, 1, 1, 2, 4, true> T3;
-  typedef NtTile<2, 4, 1, 1, 4, 1, 1, 4, 3, true> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, 1.03f, 0.f}, {128, 128, .406f, .57f}, {64, 128, .292f, .402f}, {64, 64, .139f, .218f}, {32, 64, .083f, .161f}};
+struct NtTiles<1, 1, NT_FP4> {
+  typedef NtTile<NT_FP4, 8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
+  typedef NtTile<NT_FP4, 4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
+  typedef NtTile<NT_FP4, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
+  typedef NtTile<NT_FP4, 2, 2, 2, 2, 2, 1, 1, 4, 3> T3;
+  typedef NtTile<NT_FP4, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .98f, 0.f}, {128, 128, .406f, .562f}, {64, 128, .235f, 0.f}, {64, 64, .113f, 0.f}, {32, 64, .084f, .167f}};
 };
 template <>
-struct NtTiles<1, 1, false> {
-  typedef NtTile<8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
-  typedef NtTile<4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
-  typedef NtTile<2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
-  typedef NtTile<2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
-  typedef NtTile<2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .71f, 0.f}, {128, 128, .241f, .393f}, {64, 128, .148f, 0.f}, {64, 64, .083f, .176f}, {32, 64, .052f, .142f}};
+struct NtTiles<1, 1, NT_BF16> {
+  typedef NtTile<NT_BF16, 8, 4, 2, 4, 1, 1, 1, 1, 4> T0;
+  typedef NtTile<NT_BF16, 4, 4, 2, 2, 1, 1, 1, 1, 4> T1;
+  typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
+  typedef NtTile<NT_BF16, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
 template <>
-struct NtTiles<3, 1, false> {
-  typedef NtTile<4, 2, 2, 4, 1, 3, 1, 1, 3> T0;
-  typedef NtTile<2, 4, 2, 2, 1, 3, 1, 1, 4> T1;
-  typedef NtTile<2, 2, 2, 2, 1, 3, 1, 1, 4> T2;
-  typedef NtTile<2, 2, 1, 2, 2, 3, 1, 2, 4> T3;
-  typedef NtTile<2, 2, 1, 1, 4, 3, 1, 4, 2> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .57f, 0.f}, {64, 128, .302f, .539f}, {64, 64, .2f, .365f}, {32, 64, .112f, .218f}, {32, 32, .1f, .153f}};
+struct NtTiles<3, 1, NT_BF16> {
+  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 3, 1, 1, 3> T0;
+  typedef NtTile<NT_BF16, 2, 4, 2, 2, 1, 3, 1, 1, 4> T1;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 1, 1, 4> T2;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 1, 2, 4> T3;
+  typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 1, 4, 2> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .568f, 0.f}, {64, 128, .316f, .532f}, {64, 64, .197f, .366f}, {32, 64, .114f, .221f}, {32, 32, .104f, .152f}};
 };
 template <>
-struct NtTiles<3, 3, false> {
-  typedef NtTile<4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
-  typedef NtTile<2, 2, 2, 2, 1, 3, 3, 1, 3> T1;
-  typedef NtTile<2, 2, 1, 2, 4, 3, 3, 4, 2> T2;
-  typedef NtTile<2, 2, 1, 2, 2, 3, 3, 2, 2> T3;
-  typedef NtTile<2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.05f, 0.f}, {64, 64, .323f, .567f}, {32, 64, .28f, 0.f}, {32, 64, .355f, .393f}, {32, 32, .141f, 0.f}};
+struct NtTiles<3, 3, NT_BF16> {
+  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 3, 1, 3> T1;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 4, 3, 3, 4, 2> T2;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 3, 2, 2> T3;
+  typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .28f, 0.f}, {32, 64, .35f, .39f}, {32, 32, .138f, 0.f}};
 };
 template <>
-struct NtTiles<2, 2, false> {
-  typedef NtTile<4, 4, 4, 2, 1, 2, 2, 1, 3> T0;
-  typedef NtTile<4, 2, 2, 4, 1, 2, 2, 1, 4> T1;
-  typedef NtTile<2, 2, 2, 2, 1, 2, 2, 1, 4> T2;
-  typedef NtTile<2, 2, 1, 2, 2, 2, 2, 2, 3> T3;
-  typedef NtTile<2, 2, 1, 2, 4, 2, 2, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 1.04f, 0.f}, {128, 128, .54f, 0.f}, {64, 64, .192f, .362f}, {32, 64, .151f, .271f}, {32, 64, .135f, 0.f}};
+struct NtTiles<2, 2, NT_BF16> {
+  typedef NtTile<NT_BF16, 4, 4, 4, 2, 1, 2, 2, 1, 3> T0;
+  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 2, 2, 1, 4> T1;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 2, 2, 1, 4> T2;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 2, 2, 2, 3> T3;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 4, 2, 2, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 1.f, 0.f}, {128, 128, .533f, 0.f}, {64, 64, .197f, .372f}, {32, 64, .155f, .265f}, {32, 64, .137f, 0.f}};
+};
+
+template <>
+struct NtTiles<1, 1, NT_MIXED> {
+  typedef NtTile<NT_MIXED, 8, 2, 1, 8, 1, 1, 1, 4, 3> T0;
+  typedef NtTile<NT_MIXED, 4, 2, 1, 4, 2, 1, 1, 4, 4> T1;
+  typedef NtTile<NT_MIXED, 4, 2, 1, 4, 1, 1, 1, 4, 3> T2;
+  typedef NtTile<NT_MIXED, 4, 1, 1, 4, 1, 1, 1, 4, 3> T3;
+  typedef NtTile<NT_MIXED, 2, 1, 1, 4, 1, 1, 1, 4, 4> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 256, .366f, 0.f}, {64, 128, .126f, 0.f}, {64, 128, .148f, .234f}, {64, 64, .101f, .149f}, {32, 64, .078f, .107f}};
+};
+template <>
+struct NtTiles<3, 1, NT_MIXED> {
+  typedef NtTile<NT_MIXED, 2, 4, 2, 4, 1, 3, 1, 4, 2> T0;
+  typedef NtTile<NT_MIXED, 2, 2, 2, 4, 1, 3, 1, 4, 2> T1;
+  typedef NtTile<NT_MIXED, 2, 2, 1, 4, 1, 3, 1, 4, 2> T2;
+  typedef NtTile<NT_MIXED, 2, 4, 1, 1, 4, 3, 1, 4, 2> T3;
+  typedef NtTile<NT_MIXED, 2, 2, 1, 1, 4, 3, 1, 4, 3> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{64, 256, .49f, 0.f}, {64, 128, .291f, 0.f}, {32, 128, .18f, .305f}, {32, 64, .115f, .174f}, {32, 32, .093f, .147f}};
 };
 
 }  // namespace vcr

@@ -117,6 +117,7 @@ struct PlanesArgs {
   uint8_t *rows, *cols;
   int64_t row_blocks, row_chunks, col_blocks, col_chunks;
   float *sums;
+  int32_t grouped;   // rows: chunks in the order of 4-bit operands (NT_MIXED); row_chunks is a multiple of 4
 };
 template <int P, bool BF>
 __device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, float scale, float (&tile)[64][65]) {
@@ -135,8 +136,11 @@ __device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, i
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[h][i] *= scale;
-    const int64_t ch = tc * 2 + h;
-    if (g.rows && rb < g.row_blocks && ch < g.row_chunks) store_slot<P>(g.rows, rb * g.row_chunks + ch, lane, v[h]);
+    const int64_t ch = tc * 2 + h;   // 32 columns
+    if (g.rows && rb < g.row_blocks && ch < g.row_chunks) {
+      if (g.grouped) store_slot<P>(g.rows, rb * g.row_chunks + (ch & ~(int64_t)3) + oct, (int)(ch & 3) * 16 + r, v[h]);
+      else store_slot<P>(g.rows, rb * g.row_chunks + ch, lane, v[h]);
+    }
   }
   if (!g.cols && !g.sums) return;   // uniform
 #pragma unroll
