@@ -140,41 +140,37 @@ __global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t 
   if (wave == 0 && c < cols) out[c] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
 }
 
-// The transposed weights as a bf16 operand, rows k and contraction n: a thread per 32 k of 8 rows n
+// The transposed weights as a bf16 operand (exact), rows k and contraction n: a workgroup takes 32 n by 512 k through LDS,
+// so that codes are read and fragments written whole.  Bound by what it writes: 8192 x 8192 in MXT_US us (with the eight n
+// of a slot gathered in one thread's registers, whose stores are 16 bytes apart by rows, 64 us).
 __global__ __launch_bounds__(256) void k_mx_planes_t(MxDev w, int64_t chunks, int64_t row_blocks, uint8_t *out) {
-  const int64_t groups = mx_groups(w.cols), octets = chunks * 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t o = id % octets, gk = id / octets, grp = gk >> 2;   // 32 k from 32 gk on
-  if (grp >= groups) return;
-  uint4 q[8];
-  float s[8];
+  constexpr int PITCH = 512 + 8;
+  __shared__ __attribute__((aligned(16))) uint16_t t[32 * PITCH];   // [n][k]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int64_t groups = mx_groups(w.cols), n4 = (groups + 3) >> 2;
+  const int64_t ch = blockIdx.x / n4, c4 = blockIdx.x - ch * n4, grp = c4 * 4 + wave;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t n = o * 8 + i;
-    q[i] = make_uint4(0, 0, 0, 0);
-    s[i] = 1.f;
-    if (n < w.rows) mx_block(w, n >> 4, grp, groups, (int)((gk & 3) * 16 + (n & 15)), q[i], s[i]);
+  for (int h = 0; h < 2; ++h) {   // row blocks 2 ch, 2 ch + 1
+    uint4 q = make_uint4(0, 0, 0, 0);
+    float s = 1.f;
+    if (grp < groups && (ch * 2 + h) * 16 + r < w.rows) mx_block(w, ch * 2 + h, grp, groups, lane, q, s);
+    uint16_t *d = t + (h * 16 + r) * PITCH + wave * 128 + g * 32;
+    *reinterpret_cast<uint4 *>(d) = mx_to_bf16(q.x, s);
+    *reinterpret_cast<uint4 *>(d + 8) = mx_to_bf16(q.y, s);
+    *reinterpret_cast<uint4 *>(d + 16) = mx_to_bf16(q.z, s);
+    *reinterpret_cast<uint4 *>(d + 24) = mx_to_bf16(q.w, s);
   }
-  const int lane0 = (int)(o & 3) * 16;
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint4 b[8];   // 8 k of every n
+  for (int i = 0; i < 8; ++i) {   // row blocks of 16 k; lane: k = r, n = 8 g ..
+    const int kb = i * 4 + wave;
+    const int64_t rb = c4 * 32 + kb;
+    if (rb >= row_blocks) continue;
+    const uint16_t *s = t + g * 8 * PITCH + kb * 16 + r;
+    uint32_t v[4];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) b[n] = mx_to_bf16(i == 0 ? q[n].x : i == 1 ? q[n].y : i == 2 ? q[n].z : q[n].w, s[n]);
-    const int64_t rb = gk * 2 + (i >> 1);
-    if (rb >= row_blocks) return;
-    uint8_t *d = out + (rb * chunks + (o >> 2)) * FRAG + (lane0 + (i & 1) * 8) * 16;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      uint32_t h[8];
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const uint32_t p = k < 2 ? b[n].x : k < 4 ? b[n].y : k < 6 ? b[n].z : b[n].w;
-        h[n] = k & 1 ? p >> 16 : p & 0xffffu;
-      }
-      *reinterpret_cast<uint4 *>(d + k * 16) =
-          make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-    }
+    for (int j = 0; j < 4; ++j) v[j] = s[2 * j * PITCH] | (uint32_t)s[(2 * j + 1) * PITCH] << 16;
+    *reinterpret_cast<uint4 *>(out + (rb * chunks + ch) * FRAG + lane * 16) = make_uint4(v[0], v[1], v[2], v[3]);
   }
 }
 
@@ -248,34 +244,36 @@ static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipS
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
-// y = act(x w^T + bias) for at most 16 rows x: bound by reading the weights once.  A workgroup takes RB row
-// blocks of weights; its 8 waves go through their groups of 128 columns in turn, each with the next ones'
-// loads in flight, and the partial sums are added in LDS in wave order.  The matrix instruction does 16 rows
-// for the price of one, so one path serves 1 to 16.
-//   P = 3, 1: x's parts are made once per workgroup in LDS, [chunk of 32][part][8 columns][row]: only the M real
-//   rows; lanes of further rows read the last one, and their results are not stored.  The weights are expanded in
-//   registers: a lane has 32 columns of its row, of which instruction s takes the s-th eight, so the contraction's order
-//   is 8 columns of each of the group's four blocks at a time, alike for both operands.
-//   P = 0: x is in 4 bits, its fragments are read as they are (1 KB a group, shared by RB blocks of weights).
+// y = act(x w^T + bias) for few rows x: bound by reading the weights once.  A workgroup takes RB row blocks of weights;
+// its 8 waves go through their groups of 128 columns in turn, each with the next ones' loads in flight, and the partial
+// sums are added in LDS in wave order.  The matrix instruction has 16 rows whether they are used or not: a bf16 row
+// takes one, a float32 row three, one for each of its parts, which are added at the end (1 x 4096 x 262144: 172 us with an
+// instruction for each part, ROWS_US us so).
+// The rows are laid out once per workgroup in LDS, [chunk of 32][8 columns][row]; lanes of unused rows read the last one,
+// and their results are not stored.  The weights are expanded in registers: a lane has 32 columns of its row, of which
+// instruction s takes the s-th eight.  A 4-bit x (X4) is read as it is, 1 KB a group, shared by the RB blocks.
 // Columns that do not fit LDS together are taken in slices of `slice` groups.
-template <int P, bool BF>
+enum RowsKind : int { X4 = 0, XBF = 1, XF32 = 3 };   // the rows of the instruction that a row takes
+
+template <int X>
 __device__ __forceinline__ void rows_stage(const DevMat &x, int vec, int M, int64_t g0, int n, uint8_t *lds) {
+  const int rows = M * X;
   for (int it = threadIdx.x; it < n * 16 * M; it += 512) {
     const int m = it / (n * 16), o = it - m * (n * 16);
     float v[8];
-    mat_row8<BF>(x, 0, m, g0 * 128 + o * 8, vec, v);
-    uint32_t w[4][P];
+    mat_row8<X == XBF>(x, 0, m, g0 * 128 + o * 8, vec, v);
+    uint32_t w[4][X];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) parts_of<P>(v[2 * i], v[2 * i + 1], w[i]);
+    for (int i = 0; i < 4; ++i) parts_of<X>(v[2 * i], v[2 * i + 1], w[i]);
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      *reinterpret_cast<uint4 *>(lds + ((((o >> 2) * P + p) * 4 + (o & 3)) * M + m) * 16) = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
+    for (int p = 0; p < X; ++p)
+      *reinterpret_cast<uint4 *>(lds + (o * rows + m * X + p) * 16) = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
   }
 }
 
-template <int P, int RB, bool BF>
+template <int X, int RB>
 __global__ __launch_bounds__(512, 2) void k_rows(DevMat x, int vec, MxDev a, MxDev w, int M, int slice, int z_groups, OutMat o, float *part) {
-  constexpr int U = RB == 1 ? 4 : 2;   // groups of a wave's batch
+  constexpr int U = RB == 4 ? 2 : 4;   // groups of a wave's batch
   extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
   f32v4 *red = reinterpret_cast<f32v4 *>(rows_lds);   // [RB][8 waves][64]
   uint8_t *lds = rows_lds + RB * 8 * 64 * 16;
@@ -283,105 +281,105 @@ __global__ __launch_bounds__(512, 2) void k_rows(DevMat x, int vec, MxDev a, MxD
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t groups = mx_groups(w.cols), n4 = (groups + 3) >> 2, blocks = (w.rows + 15) >> 4;
   const int64_t g0 = (int64_t)blockIdx.y * z_groups, g1 = min(groups, g0 + z_groups);
-  const int mr = min(r, M - 1);
+  const int rows = M * X, mr = min(r, rows - 1);
   const bool whole = g1 - g0 <= slice;
+  const int64_t stride = (int64_t)gridDim.x * RB;
   bool staged = false;
-  for (int64_t b0 = (int64_t)blockIdx.x * RB; b0 < blocks; b0 += (int64_t)gridDim.x * RB) {
-    f32v4 hi[RB], lo[RB];
+  i32x4 q[2][U][RB], qa[2][X == X4 ? U : 1];
+  uint32_t sc[2][U][RB], sa[2][X == X4 ? U : 1];
+  f32v4 acc[RB];
+  auto load = [&](int64_t b0, int64_t s0, int n, int gi, int buf) {   // groups gi, gi + 8, .. of the n from s0 on
 #pragma unroll
-    for (int b = 0; b < RB; ++b) hi[b] = lo[b] = f32v4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < U; ++u) {
+      const int64_t gr = s0 + min(gi + 8 * u, n - 1);
+      if constexpr (X == X4) {
+        qa[buf][u] = *reinterpret_cast<const i32x4 *>(a.codes + (gr * 64 + lane) * 16);
+        sa[buf][u] = *reinterpret_cast<const uint32_t *>(a.scales + ((gr >> 2) * 64 + lane) * 4);
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const int64_t rb = min(b0 + b, blocks - 1);
+        q[buf][u][b] = *reinterpret_cast<const i32x4 *>(w.codes + ((rb * groups + gr) * 64 + lane) * 16);
+        sc[buf][u][b] = *reinterpret_cast<const uint32_t *>(w.scales + ((rb * n4 + (gr >> 2)) * 64 + lane) * 4);
+      }
+    }
+  };
+  auto first = [&](int64_t b0, int64_t s0, int n) {
+    load(b0, s0, n, wave, 0);
+    if (wave + 8 * U < n) load(b0, s0, n, wave + 8 * U, 1);
+  };
+  auto multiply = [&](int64_t s0, int n, int gi, int buf) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (gi + 8 * u >= n) break;   // wave-uniform
+      const int sh = 8 * (int)((s0 + gi + 8 * u) & 3);
+      if constexpr (X == X4) {
+        const i32x4 av = qa[buf][u];
+        const i32x8 aw = {av[0], av[1], av[2], av[3], 0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          const i32x4 bv = q[buf][u][b];
+          const i32x8 bw = {bv[0], bv[1], bv[2], bv[3], 0, 0, 0, 0};
+          acc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw, aw, acc[b], 4, 4, 0, (int)(sc[buf][u][b] >> sh), 0,
+                                                                    (int)(sa[buf][u] >> sh));
+        }
+      } else {
+        float s[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) s[b] = mx_scale((sc[buf][u][b] >> sh) & 255);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bf16x8 av = *reinterpret_cast<const bf16x8 *>(lds + ((((gi + 8 * u) * 4 + g) * 4 + i) * rows + mr) * 16);
+#pragma unroll
+          for (int b = 0; b < RB; ++b)
+            acc[b] = mfma_bf16(__builtin_bit_cast(bf16x8, mx_to_bf16((uint32_t)q[buf][u][b][i], s[b])), av, acc[b]);
+        }
+      }
+    }
+  };
+  for (int64_t b0 = (int64_t)blockIdx.x * RB; b0 < blocks; b0 += stride) {
+    const bool begun = whole && b0 >= stride;   // its first loads were issued before the last blocks' results
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[b] = f32v4{0.f, 0.f, 0.f, 0.f};
     for (int64_t s0 = g0; s0 < g1; s0 += slice) {
       const int n = (int)min((int64_t)slice, g1 - s0);
-      i32x4 q[2][U][RB];
-      uint32_t sc[2][U][RB];
-      i32x4 qa[2][U];
-      uint32_t sa[2][U];
-      auto load = [&](int gi, int buf) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int64_t gr = s0 + min(gi + 8 * u, n - 1);
-          if constexpr (P == 0) {
-            qa[buf][u] = *reinterpret_cast<const i32x4 *>(a.codes + (gr * 64 + lane) * 16);
-            sa[buf][u] = *reinterpret_cast<const uint32_t *>(a.scales + ((gr >> 2) * 64 + lane) * 4);
-          }
-#pragma unroll
-          for (int b = 0; b < RB; ++b) {
-            const int64_t rb = min(b0 + b, blocks - 1);
-            q[buf][u][b] = *reinterpret_cast<const i32x4 *>(w.codes + ((rb * groups + gr) * 64 + lane) * 16);
-            sc[buf][u][b] = *reinterpret_cast<const uint32_t *>(w.scales + ((rb * n4 + (gr >> 2)) * 64 + lane) * 4);
-          }
-        }
-      };
-      auto multiply = [&](int gi, int buf) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (gi + 8 * u >= n) break;   // wave-uniform
-          const int sh = 8 * (int)((s0 + gi + 8 * u) & 3);
-          if constexpr (P == 0) {
-            const i32x4 av = qa[buf][u];
-            const i32x8 aw = {av[0], av[1], av[2], av[3], 0, 0, 0, 0};
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-              const i32x4 bv = q[buf][u][b];
-              const i32x8 bw = {bv[0], bv[1], bv[2], bv[3], 0, 0, 0, 0};
-              hi[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw, aw, hi[b], 4, 4, 0, (int)(sc[buf][u][b] >> sh), 0,
-                                                                       (int)(sa[buf][u] >> sh));
-            }
-          } else {
-            float s[RB];
-#pragma unroll
-            for (int b = 0; b < RB; ++b) s[b] = mx_scale((sc[buf][u][b] >> sh) & 255);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              bf16x8 av[P];
-#pragma unroll
-              for (int p = 0; p < P; ++p)
-                av[p] = *reinterpret_cast<const bf16x8 *>(lds + (((((gi + 8 * u) * 4 + g) * P + p) * 4 + i) * M + mr) * 16);
-#pragma unroll
-              for (int b = 0; b < RB; ++b) {
-                const bf16x8 bw = __builtin_bit_cast(bf16x8, mx_to_bf16((uint32_t)q[buf][u][b][i], s[b]));
-                if constexpr (P == 3) {
-                  lo[b] = mfma_bf16(bw, av[2], lo[b]);
-                  lo[b] = mfma_bf16(bw, av[1], lo[b]);
-                }
-                hi[b] = mfma_bf16(bw, av[0], hi[b]);
-              }
-            }
-          }
-          __builtin_amdgcn_sched_barrier(0);   // (a batch's reads of LDS all ahead of its products need more registers than there are)
-        }
-      };
-      load(wave, 0);   // ahead of the rows' staging
-      if constexpr (P > 0) {
+      if (!begun) first(b0, s0, n);   // ahead of the rows' staging
+      if constexpr (X != X4) {
         if (!staged) {
-          if (s0 > g0 || b0 != (int64_t)blockIdx.x * RB) __syncthreads();   // the last slice has been read
-          rows_stage<P, BF>(x, vec, M, s0, n, lds);
+          if (s0 > g0 || b0 >= stride) __syncthreads();   // the last slice has been read
+          rows_stage<X>(x, vec, M, s0, n, lds);
           __syncthreads();
           staged = whole;
         }
       }
       for (int gi = wave; gi < n; gi += 16 * U) {
-        if (gi + 8 * U < n) load(gi + 8 * U, 1);
-        multiply(gi, 0);
-        if (gi + 16 * U < n) load(gi + 16 * U, 0);
-        if (gi + 8 * U < n) multiply(gi + 8 * U, 1);
+        multiply(s0, n, gi, 0);
+        if (gi + 16 * U < n) load(b0, s0, n, gi + 16 * U, 0);
+        if (gi + 8 * U < n) {
+          multiply(s0, n, gi + 8 * U, 1);
+          if (gi + 24 * U < n) load(b0, s0, n, gi + 24 * U, 1);
+        }
       }
     }
+    if (whole && b0 + stride < blocks) first(b0 + stride, g0, (int)(g1 - g0));
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      f32v4 v = hi[b];
-      if constexpr (P == 3) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < __builtin_huge_valf() ? v[i] + lo[b][i] : v[i];
-      }
-      red[(b * 8 + wave) * 64 + lane] = v;
-    }
+    for (int b = 0; b < RB; ++b) red[(b * 8 + wave) * 64 + lane] = acc[b];
     __syncthreads();
     for (int b = wave; b < RB; b += 8) {
-      f32v4 v = red[b * 512 + lane];
-      for (int k = 1; k < 8; ++k) v += red[b * 512 + k * 64 + lane];
-      const int64_t n = (b0 + b) * 16 + 4 * g;
+      auto sum = [&](int row) {
+        const f32v4 *d = red + b * 512 + g * 16 + row;
+        f32v4 v = d[0];
+        for (int k = 1; k < 8; ++k) v += d[k * 64];
+        return v;
+      };
       if (r < M && b0 + b < blocks) {
+        f32v4 v = sum(X == XF32 ? 3 * r : r);
+        if constexpr (X == XF32) {   // the parts, small ones first; an infinite or NaN large one is the result (nt.h)
+          const f32v4 l = sum(3 * r + 2) + sum(3 * r + 1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < __builtin_huge_valf() ? v[i] + l[i] : v[i];
+        }
+        const int64_t n = (b0 + b) * 16 + 4 * g;
         if (part) *reinterpret_cast<f32v4 *>(part + ((int64_t)blockIdx.y * M + r) * (blocks * 16) + n) = v;
         else o.put(r, n, v);
       }
@@ -390,15 +388,17 @@ __global__ __launch_bounds__(512, 2) void k_rows(DevMat x, int vec, MxDev a, MxD
   }
 }
 
-constexpr int ROWS_MAX = 16;
 struct RowsPlan {
   int rb, parts, slice;
   int64_t wgs, z_groups;
   size_t lds, part_bytes;
 };
+// Up to 16 rows in 4 bits, 8 of bf16 and 5 of float32: laying out more of the others in every workgroup takes longer than
+// their operand made once for the products by tiles (8192 x 8192, bf16: FEW_ROWS_US).
+inline bool few_rows(int X, int64_t M) { return M <= (X == X4 ? 16 : X == XBF ? 8 : 5); }
 // A workgroup of 8 waves per compute unit or more; the contraction is divided among workgroups only where there are too
 // few row blocks for that and every wave keeps 4 groups.
-static RowsPlan rows_plan(int P, int64_t M, int64_t N, int64_t groups) {
+static RowsPlan rows_plan(int X, int64_t M, int64_t N, int64_t groups) {
   RowsPlan p{};
   const int64_t blocks = blocks_of(N, 16);
   p.rb = blocks >= 4096 ? 4 : blocks >= 512 ? 2 : 1;
@@ -406,16 +406,16 @@ static RowsPlan rows_plan(int P, int64_t M, int64_t N, int64_t groups) {
   const int64_t z = std::max<int64_t>(1, std::min<int64_t>(256 / p.wgs, groups / 32));
   p.z_groups = blocks_of(groups, z);
   p.parts = (int)blocks_of(groups, p.z_groups);
-  const size_t per = (size_t)M * 256 * P;   // bytes of a group's rows
-  const size_t room = per * 16 > 64 << 10 ? 112 << 10 : 56 << 10;
-  p.slice = P == 0 ? (int)p.z_groups : (int)std::min<int64_t>(p.z_groups, std::max<int64_t>(8, room / per / 8 * 8));
-  p.lds = (size_t)p.rb * 8 * 64 * 16 + (P == 0 ? 0 : per * p.slice);
+  const size_t per = (size_t)M * 256 * X;   // bytes of a group's rows
+  const size_t room = 112 << 10;   // (registers let one workgroup on a compute unit)
+  p.slice = X == X4 ? (int)p.z_groups : (int)std::min<int64_t>(p.z_groups, std::max<int64_t>(8, room / per / 8 * 8));
+  p.lds = (size_t)p.rb * 8 * 64 * 16 + per * (X == X4 ? 0 : p.slice);
   p.part_bytes = p.parts > 1 ? (size_t)p.parts * M * blocks * 64 : 0;
   return p;
 }
-template <int P, bool BF>
+template <int X>
 static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, const RowsPlan &p, const OutMat &o, float *part, hipStream_t s) {
-  const int vec = x.p && rows_aligned(x.p, x.ld, BF ? 2 : 4), M = (int)o.rows;
+  const int vec = x.p && rows_aligned(x.p, x.ld, X == XBF ? 2 : 4), M = (int)o.rows;
   const dim3 grid((unsigned)p.wgs, (unsigned)p.parts);
   if (p.parts == 1) part = nullptr;
   auto go = [&](auto kernel) {
@@ -426,7 +426,7 @@ static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, c
     hipLaunchKernelGGL(kernel, grid, dim3(512), p.lds, s, x, vec, a, w, M, p.slice, (int)p.z_groups, o, part);
     return hipGetLastError();
   };
-  hipError_t e = p.rb == 4 ? go(k_rows<P, 4, BF>) : p.rb == 2 ? go(k_rows<P, 2, BF>) : go(k_rows<P, 1, BF>);
+  hipError_t e = p.rb == 4 ? go(k_rows<X, 4>) : p.rb == 2 ? go(k_rows<X, 2>) : go(k_rows<X, 1>);
   if (e != hipSuccess || !part) return e;
   const int64_t ld = blocks_of(o.cols, 16) * 16;
   hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
@@ -601,11 +601,11 @@ vcr_status vcr_mx_product(vcr_ctx *c, const vcr_mx *a, const vcr_mx *w, const fl
                 (long long)y->cols, (long long)a->rows, (long long)a->cols, (long long)w->rows, (long long)w->cols);
   TRY(op_begin(c));
   if (y->rows == 0) return VCR_OK;
-  if (y->rows <= ROWS_MAX) {
-    const RowsPlan p = rows_plan(0, y->rows, y->cols, mx_groups(a->cols));
+  if (few_rows(X4, y->rows)) {
+    const RowsPlan p = rows_plan(X4, y->rows, y->cols, mx_groups(a->cols));
     Workspace *ws = nullptr;
     TRY(op_space(c, p.part_bytes, &ws));
-    HIP_TRY(c, (launch_rows<0, false>(DevMat{}, dev(a), dev(w), p, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
+    HIP_TRY(c, (launch_rows<X4>(DevMat{}, dev(a), dev(w), p, out_mat(y, bias, relu != 0), reinterpret_cast<float *>(ws->base), c->stream)));
     return op_end(c);
   }
   NtArgs g{};
@@ -633,13 +633,13 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
   if (y->rows == 0) return VCR_OK;
   const DevMat d = dev(x);
   const int P = d.bf16 ? 1 : 3;
-  if (y->rows <= ROWS_MAX) {
+  if (few_rows(P, y->rows)) {
     const RowsPlan p = rows_plan(P, y->rows, y->cols, mx_groups(x->cols));
     Workspace *ws = nullptr;
     TRY(op_space(c, p.part_bytes, &ws));
     float *part = reinterpret_cast<float *>(ws->base);
-    if (d.bf16) HIP_TRY(c, (launch_rows<1, true>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
-    else HIP_TRY(c, (launch_rows<3, false>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
+    if (d.bf16) HIP_TRY(c, (launch_rows<XBF>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
+    else HIP_TRY(c, (launch_rows<XF32>(d, MxDev{}, dev(w), p, out_mat(y, bias, relu != 0), part, c->stream)));
     return op_end(c);
   }
   const int64_t chunks = 4 * mx_groups(x->cols), rb = blocks_of(x->rows, 16);
@@ -730,7 +730,7 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     HIP_TRY(c, hipGetLastError());
   }
   if (has_dx) {
-    hipLaunchKernelGGL(k_mx_planes_t, dim3((unsigned)blocks_of(4 * nch * 4 * mx_groups(kx), 256)), dim3(256), 0, s, dev(w), nch, kxb, wt);
+    hipLaunchKernelGGL(k_mx_planes_t, dim3((unsigned)(nch * blocks_of(mx_groups(kx), 4))), dim3(256), 0, s, dev(w), nch, kxb, wt);
     HIP_TRY(c, hipGetLastError());
     NtArgs a{};
     a.A = NtOperand{gp, nullptr, (int32_t)mb, 0};
