@@ -591,17 +591,17 @@ struct NtTiles<3, 1, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 4, 2, 2, 1, 3, 1, 1, 4> T1;
   typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 1, 1, 4> T2;
   typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 1, 2, 4> T3;
-  typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 1, 4, 2> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .568f, 0.f}, {64, 128, .316f, .532f}, {64, 64, .197f, .366f}, {32, 64, .114f, .221f}, {32, 32, .104f, .152f}};
+  typedef NtTile<NT_BF16, 2, 1, 1, 2, 2, 3, 1, 2, 4> T4;
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .568f, 0.f}, {64, 128, .316f, .532f}, {64, 64, .197f, .366f}, {32, 64, .114f, .221f}, {32, 32, .078f, .157f}};
 };
 template <>
 struct NtTiles<3, 3, NT_BF16> {
   typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
-  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 3, 1, 3> T1;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 4, 3, 3, 4, 2> T2;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 3, 2, 2> T3;
+  typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 3, 3, 2, 2> T1;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 3, 1, 3> T2;
+  typedef NtTile<NT_BF16, 2, 1, 1, 4, 1, 3, 3, 1, 4> T3;
   typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .28f, 0.f}, {32, 64, .35f, .39f}, {32, 32, .138f, 0.f}};
+  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
 };
 template <>
 struct NtTiles<2, 2, NT_BF16> {
