@@ -373,10 +373,14 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  * their element type (calls are faster where p and the rows are 16-byte aligned).  A matrix of no rows is
  * allowed where rows are a batch, and queues nothing (or zeros, for sums over the batch).  Outputs
  * must not overlap inputs unless stated.  These calls need no loaded network and leave it, its bounds
- * and the other calls' workspace alone; they keep one workspace per stream, which grows as needed
- * (VCR_ERR_OOM beyond VCR_OPT_WORKSPACE_CAP_BYTES).  A call may be recorded into a HIP graph by the
+ * and the other calls' workspace alone; they keep one workspace for every stream they were given, which grows
+ * as needed (VCR_ERR_OOM beyond VCR_OPT_WORKSPACE_CAP_BYTES) and is kept until vcr_destroy.  A call may be recorded into a HIP graph by the
  * caller once it has run with the same sizes on that stream (else VCR_ERR_STATE). */
 enum { VCR_F32 = 0, VCR_BF16 = 1 };
+
+/* Longest contraction of a product here (the shared dimension; for gradients also the rows of dy, for
+ * vcr_orthogonalize both dimensions): VCR_ERR_UNSUPPORTED beyond. */
+#define VCR_MAX_CONTRACTION ((int64_t)1 << 21)
 
 typedef struct {
   void *p;                  /* device */
@@ -419,8 +423,8 @@ vcr_status vcr_mx_product(vcr_ctx *ctx, const vcr_mx *a, const vcr_mx *w, const 
 vcr_status vcr_mx_linear(vcr_ctx *ctx, const vcr_mat *x, const vcr_mx *w, const float *bias, int32_t relu,
                          const vcr_mat *y);
 
-/* Gradients of vcr_mx_linear from dy (rows, n): with g = dy, or dy where y > 0 (y: the output of a call with
- * relu, of dy's type; NULL: no relu),
+/* Gradients of vcr_mx_linear from dy (rows, n): with g = dy, or dy where y > 0 and 0 elsewhere (y: the output
+ * of a call with relu, of dy's type; NULL: no relu),
  *   dx (rows, k) = g w,   dw (n, k) = g^T x   (the gradient by the weights before their quantisation, which
  *   passes it on as it is),   db (n) = sum of g over the rows, float32.
  * Outputs may be NULL; x (of dy's type) is needed for dw, w for dx.  No rows: dw and db are zero. */

@@ -10,3 +10,4 @@ vcr_status op_space(vcr_ctx *c, size_t bytes, vcr_internal::Workspace **out);
 vcr_status op_begin(vcr_ctx *c);
 vcr_status op_end(vcr_ctx *c);
 vcr_status check_mat(vcr_ctx *c, const vcr_mat *m, const char *name);
+vcr_status check_contraction(vcr_ctx *c, int64_t k);

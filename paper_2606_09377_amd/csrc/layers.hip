@@ -9,6 +9,7 @@
 // block of columns 32 g .. 32 g + 31 of row r, the first value in the low bits; scales [rows /
 // 16][cols / 512][64 lanes][4 groups of 128 columns].  Rows are padded to 16 and columns to 128 with zeros.
 #include <algorithm>
+#include <new>
 
 #include "ctx.h"
 #include "layers.h"
@@ -454,10 +455,15 @@ vcr_status op_space(vcr_ctx *c, size_t bytes, Workspace **out) {
   vcr_internal::OpSpace *sp = nullptr;
   for (auto &o : c->op_spaces)
     if (o.stream == c->stream) sp = &o;
-  if (!sp) {
-    c->op_spaces.emplace_back();
-    sp = &c->op_spaces.back();
-    sp->stream = c->stream;
+  try {   // (room for what is kept below too: no exception crosses the ABI)
+    if (!sp) {
+      c->op_spaces.emplace_back();
+      sp = &c->op_spaces.back();
+      sp->stream = c->stream;
+    }
+    c->op_retired.reserve(c->op_retired.size() + 1);
+  } catch (const std::bad_alloc &) {
+    return VCR_ERR_OOM;
   }
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(c->stream, &cap) != hipSuccess) (void)hipGetLastError();
@@ -514,6 +520,11 @@ vcr_status check_mat(vcr_ctx *c, const vcr_mat *m, const char *name) {
   if (m->rows > 0 && !m->p) return fail(c, VCR_ERR_ARG, "%s: null pointer", name);
   if ((reinterpret_cast<uintptr_t>(m->p) & (m->type == VCR_F32 ? 3 : 1)) != 0)
     return fail(c, VCR_ERR_ARG, "%s: pointer not aligned to its type", name);
+  return VCR_OK;
+}
+vcr_status check_contraction(vcr_ctx *c, int64_t k) {
+  if (k > VCR_MAX_CONTRACTION)
+    return fail(c, VCR_ERR_UNSUPPORTED, "a contraction of %lld exceeds the limit of %lld", (long long)k, (long long)VCR_MAX_CONTRACTION);
   return VCR_OK;
 }
 static vcr_status check_mx(vcr_ctx *c, const vcr_mx *m, const char *name) {
@@ -599,6 +610,7 @@ vcr_status vcr_mx_product(vcr_ctx *c, const vcr_mx *a, const vcr_mx *w, const fl
   if (a->cols != w->cols || y->rows != a->rows || y->cols != w->rows)
     return fail(c, VCR_ERR_SHAPE, "y (%lld x %lld) is not a (%lld x %lld) times the transpose of w (%lld x %lld)", (long long)y->rows,
                 (long long)y->cols, (long long)a->rows, (long long)a->cols, (long long)w->rows, (long long)w->cols);
+  TRY(check_contraction(c, a->cols));
   TRY(op_begin(c));
   if (y->rows == 0) return VCR_OK;
   if (few_rows(X4, y->rows)) {
@@ -629,6 +641,7 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
   if (x->cols != w->cols || y->rows != x->rows || y->cols != w->rows)
     return fail(c, VCR_ERR_SHAPE, "y (%lld x %lld) is not x (%lld x %lld) times the transpose of w (%lld x %lld)", (long long)y->rows,
                 (long long)y->cols, (long long)x->rows, (long long)x->cols, (long long)w->rows, (long long)w->cols);
+  TRY(check_contraction(c, x->cols));
   TRY(op_begin(c));
   if (y->rows == 0) return VCR_OK;
   const DevMat d = dev(x);
@@ -684,6 +697,8 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
   if (dx && (w->rows != N || dx->rows != M || dx->cols != w->cols)) return fail(c, VCR_ERR_SHAPE, "dx is not dy times w");
   if (dw && (x->rows != M || dw->rows != N || dw->cols != x->cols)) return fail(c, VCR_ERR_SHAPE, "dw is not the transpose of dy times x");
   if (dw && x->type != dy->type) return fail(c, VCR_ERR_ARG, "x and dy differ in type");
+  if (dx) TRY(check_contraction(c, N));
+  if (dw) TRY(check_contraction(c, M));
   TRY(op_begin(c));
   const DevMat g = dev(dy), mask = dev(y);
   const int P = g.bf16 ? 1 : 3;

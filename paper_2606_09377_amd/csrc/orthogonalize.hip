@@ -203,6 +203,7 @@ extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t co
   if (g->rows * g->cols > VCR_MAX_LAYER_WEIGHTS)
     return fail(c, VCR_ERR_SHAPE, "%lld x %lld exceeds the limit of %lld weights", (long long)g->rows, (long long)g->cols,
                 (long long)VCR_MAX_LAYER_WEIGHTS);
+  if ((st = check_contraction(c, std::max(g->rows, g->cols))) != VCR_OK) return st;
   auto span = [](const vcr_mat *m) { return m->rows > 0 ? (m->rows - 1) * m->ld + m->cols : 0; };
   if (count > 1 && (g_stride < span(g) || out_stride < span(out) || (base && base_stride < span(base))))
     return fail(c, VCR_ERR_SHAPE, "matrices of a batch overlap");

@@ -534,12 +534,14 @@ class Ctx:
         for t in (base, out):
             if t is not None and t.shape != g.shape:
                 raise ValueError(f"expected shape {tuple(g.shape)}, got {tuple(t.shape)}")
-        count = g.shape[0] if g.dim() == 3 else 1
-
-        def one(t):
-            return (_mat(t), 0) if t.dim() == 2 else (_mat(t[0] if count else t.view(0, t.shape[2])), t.stride(0))
         if g.dim() not in (2, 3):
             raise ValueError("expected a tensor of 2 or 3 dimensions")
+        count = g.shape[0] if g.dim() == 3 else 1
+        if count == 0:
+            return out
+
+        def one(t):
+            return (_mat(t), 0) if t.dim() == 2 else (_mat(t[0]), t.stride(0))
         gm, om = one(g), one(out)
         bm = (None, 0) if base is None else one(base)
         o = VcrNsOpts(int(steps), *(float(v) for v in coefficients), float(eps), float(gain), float(keep))

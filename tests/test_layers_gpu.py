@@ -199,6 +199,29 @@ def test_gradients_are_the_differences(ctx):
             assert abs(d - grad.flat[i]) <= 1e-6 * max(1.0, np.abs(grad).max()), (i, d, grad.flat[i])
 
 
+@pytest.mark.parametrize("m,k,n", [(1, 40000, 40), (5, 33000, 100), (8, 20000, 50), (40, 40000, 33), (7, 100, 70000)])
+def test_long_contractions_and_many_columns(ctx, m, k, n):
+    """Contractions that do not fit LDS together, or are divided among workgroups; columns in many rounds."""
+    rng = np.random.default_rng(k)
+    w, wv = weights(rng, n, k)
+    for dtype in ("float32", "bfloat16"):
+        x = dev(rng.standard_normal((m, k)), dtype)
+        near(ctx.mx_linear(x, w), *o64.linear(host(x), wv), k, dtype)
+    q = ctx.mx_quantize(x)
+    near(ctx.mx_product(q, w), *o64.linear(host(ctx.mx_dequantize(q)), wv), k)
+    dy = dev(rng.standard_normal((m, n)))
+    near(ctx.mx_linear_grad(dy, None, w, need=(True, False, False))[0], host(dy) @ wv, np.abs(host(dy)) @ np.abs(wv), n)
+
+
+def test_large_gradients(ctx):
+    rng = np.random.default_rng(77)
+    m, k, n = 130, 2200, 2300
+    w, wv = weights(rng, n, k)
+    x, dy = dev(rng.standard_normal((m, k))), dev(rng.standard_normal((m, n)))
+    for got, (want, mag), K in zip(ctx.mx_linear_grad(dy, x, w), o64.linear_grad(host(dy), host(x), wv), (n, m, m)):
+        near(got, want, mag, K)
+
+
 @pytest.mark.parametrize("m", [1, 40, 300])
 def test_non_finite_and_extreme_operands(ctx, m):
     """Infinite, NaN, huge and tiny float32 rows give what float32 products give."""

@@ -71,6 +71,10 @@ def test_refusals(vc):
         assert call(x(3, 40), mx(0, 40), mat(3, 7)) == SHAPE
         assert call(x(3, 40), mx(7, 40), mat(3, 7), p + 2) == ARG
 
+        far = vc.VCR_ERR_UNSUPPORTED   # longer contractions than the kernels address
+        assert call(x(3, 1 << 21), mx(7, 1 << 21), mat(3, 7)) == STATE
+        assert call(x(3, (1 << 21) + 1), mx(7, (1 << 21) + 1), mat(3, 7)) == far
+
     def grad(dy, y, x, w, dx, dw, db=p):
         r = lambda v: None if v is None else ref(v)  # noqa: E731
         return lib.vcr_mx_linear_grad(h, r(dy), r(y), r(x), r(w), r(dx), r(dw), db)
@@ -81,6 +85,11 @@ def test_refusals(vc):
                          (2, mat(4, 40), SHAPE), (2, mat(3, 40, kind=1), ARG), (3, mx(8, 40), SHAPE),
                          (4, mat(3, 41), SHAPE), (5, mat(7, 41), SHAPE), (5, mat(8, 40), SHAPE)):
         assert grad(*ok[:i], bad, *ok[i + 1:]) == want, (i, lib.vcr_last_error(h))
+
+    n = (1 << 21) + 1
+    assert grad(mat(3, n), None, None, mx(n, 40), mat(3, 40), None) == far
+    assert grad(mat(n, 3), None, mat(n, 40), None, None, mat(3, 40)) == far
+    assert grad(mat(n, 3), None, None, None, None, None) == STATE
 
     def orth(g, o, base=None, out=None, count=1, gs=0, bs=0, os_=0):
         r = lambda v: None if v is None else ref(v)  # noqa: E731
@@ -98,6 +107,7 @@ def test_refusals(vc):
     assert orth(mat(5, 7), opts()) == SHAPE and orth(mat(5, 6), opts(), mat(6, 6)) == SHAPE
     assert orth(mat(5, 6), opts(), count=-1) == ARG and orth(mat(5, 6), opts(), count=70000) == ARG
     assert orth(mat(1 << 20, 1 << 20), opts(), out=mat(1 << 20, 1 << 20)) == SHAPE
+    assert orth(mat(4, n), opts(), out=mat(4, n)) == far
 
 
 def test_oracle_grid():
