@@ -7,9 +7,9 @@
 // A and Q are symmetric: of their 16 x 16 blocks those on and below the diagonal are computed and
 // stored twice.  A step is 3 m^2 n + m^3 multiply-adds that way (of 4 m^2 n + 2 m^3).  All three products
 // contract the contiguous axes of operands in the layout of nt.h: X (rows m) and its transpose (rows
-// n) are both kept, written by the epilogue that makes them.  float32 updates take three bf16 parts
-// (float32's accuracy), bf16 ones two: a singular value of 2^-9 is raised by a^5 = 485 in five steps, and
-// the rounding of one part, 2^-9 of the largest, with it.
+// n) are both kept, written by the epilogue that makes them.  float32 results take three bf16 parts
+// (float32's accuracy), bf16 ones two: what one step rounds, the later ones raise by up to a = 3.4 each with the smallest
+// singular values, so that one part's 2^-9 would be far above the result's own rounding, and two parts' 2^-17 is below it.
 #include <algorithm>
 #include <cmath>
 
@@ -211,7 +211,7 @@ extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t co
   if (count == 0 || g->rows == 0) return VCR_OK;
   const bool tr = g->rows > g->cols, bf = g->type == VCR_BF16;
   const int64_t mp = blocks_of(std::min(g->rows, g->cols), 32) * 32, np = blocks_of(std::max(g->rows, g->cols), 32) * 32;
-  const int P = bf ? 2 : 3;
+  const int P = out->type == VCR_BF16 ? 2 : 3;
   Workspace size;
   (void)ns_carve(size, mp, np, count, P);
   Workspace *ws = nullptr;
@@ -233,7 +233,12 @@ extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t co
   e.out_bf16 = out->type == VCR_BF16;
   e.vec = (reinterpret_cast<uintptr_t>(out->p) & (e.out_bf16 ? 7 : 15)) == 0 && out->ld % 4 == 0 && out_stride % 4 == 0;
   e.transposed = tr;
-  if (bf) HIP_TRY(c, (ns_run<2, true>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream)));
-  else HIP_TRY(c, (ns_run<3, false>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream)));
+  auto run = [&](auto parts, auto g16) {
+    return ns_run<decltype(parts)::value, decltype(g16)::value>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream);
+  };
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 3> Three;
+  HIP_TRY(c, P == 2 ? (bf ? run(Two{}, std::true_type{}) : run(Two{}, std::false_type{}))
+                    : (bf ? run(Three{}, std::true_type{}) : run(Three{}, std::false_type{})));
   return op_end(c);
 }

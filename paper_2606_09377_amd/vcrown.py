@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 import numpy as np
 
@@ -129,16 +130,14 @@ def load_library(path: str = LIB_PATH):
         "vcr_beta_crown_bounds": ([P, P, F32, P, I32, ctypes.POINTER(VcrSplits), ctypes.POINTER(VcrBetaOpts), P, P],
                                   I32),
         "vcr_bab_verify": ([P, P, F32, P, I32, ctypes.POINTER(VcrBabOpts), ctypes.POINTER(VcrBabResult), P], I32),
-        "vcr_mx_bytes": ([ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_uint64),
-                          ctypes.POINTER(ctypes.c_uint64)], I32),
-        "vcr_mx_quantize": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMx)], I32),
-        "vcr_mx_dequantize": ([P, ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMat)], I32),
-        "vcr_mx_product": ([P, ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMx), P, I32, ctypes.POINTER(VcrMat)], I32),
-        "vcr_mx_linear": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMx), P, I32, ctypes.POINTER(VcrMat)], I32),
-        "vcr_mx_linear_grad": ([P, ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat),
-                                ctypes.POINTER(VcrMx), ctypes.POINTER(VcrMat), ctypes.POINTER(VcrMat), P], I32),
-        "vcr_orthogonalize": ([P, ctypes.POINTER(VcrMat), I32, ctypes.c_int64, ctypes.POINTER(VcrNsOpts),
-                               ctypes.POINTER(VcrMat), ctypes.c_int64, ctypes.POINTER(VcrMat), ctypes.c_int64], I32),
+        # (descriptors are passed by address: packed bytes or byref of the structures below)
+        "vcr_mx_bytes": ([ctypes.c_int64, ctypes.c_int64, P, P], I32),
+        "vcr_mx_quantize": ([P, P, P], I32),
+        "vcr_mx_dequantize": ([P, P, P], I32),
+        "vcr_mx_product": ([P, P, P, P, I32, P], I32),
+        "vcr_mx_linear": ([P, P, P, P, I32, P], I32),
+        "vcr_mx_linear_grad": ([P, P, P, P, P, P, P, P], I32),
+        "vcr_orthogonalize": ([P, P, I32, ctypes.c_int64, P, P, ctypes.c_int64, P, ctypes.c_int64], I32),
         "vcr_crown_bounds_noalloc": ([P, P, I32, F32, P, I32, P, P], I32),
     }
     for name, (args, res) in sig.items():
@@ -168,7 +167,7 @@ class MX:
     column groups, 64, 16) and `scales` (row blocks, ceil(groups / 4), 64, 4).  Made by Ctx.mx_quantize, or by
     MX.pack from codes and scales in row order."""
 
-    __slots__ = ("rows", "cols", "device", "_codes", "_scales", "_buf", "_s", "_ref")
+    __slots__ = ("rows", "cols", "device", "_codes", "_scales", "_buf", "_c")
 
     def __init__(self, codes, scales, rows, cols):
         groups = -(-cols // 128)
@@ -182,8 +181,7 @@ class MX:
 
     def _set(self, rows, cols, device, codes, scales):
         self.rows, self.cols, self.device = rows, cols, device
-        self._s = VcrMx(codes, scales, rows, cols)
-        self._ref = ctypes.byref(self._s)
+        self._c = _MX.pack(codes, scales, rows, cols)
 
     @classmethod
     def empty(cls, rows, cols, device="cuda"):
@@ -318,9 +316,10 @@ class Ctx:
 
     def _current_stream(self):
         """_stream_sync for calls of a few microseconds: torch's current stream by its handle alone."""
-        import torch
-        if self.device >= 0 and torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
-            self.set_stream()
+        if self.device >= 0:
+            import torch
+            if torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+                self.set_stream()
 
     def crown_bounds(self, x0, eps, C, splits=None, out=None):
         """CROWN bounds on C f(x).  x0 (B, n0), C (B, m, n_out) float32 CUDA tensors.
@@ -476,9 +475,9 @@ class Ctx:
     def mx_quantize(self, x, out=None):
         """x (rows, cols), a float32 or bfloat16 CUDA tensor with contiguous rows, in 4 bits (an MX)."""
         m = _mat(x)
-        q = MX.empty(m.rows, m.cols, x.device) if out is None else out
+        q = MX.empty(*x.shape, x.device) if out is None else out
         self._current_stream()
-        self._check(self.lib.vcr_mx_quantize(self.h, ctypes.byref(m), q._ref))
+        self._check(self.lib.vcr_mx_quantize(self.h, m, q._c))
         return q
 
     def mx_dequantize(self, q, dtype=None, out=None):
@@ -486,7 +485,7 @@ class Ctx:
         import torch
         y = torch.empty((q.rows, q.cols), dtype=dtype or torch.float32, device=q.device) if out is None else out
         self._current_stream()
-        self._check(self.lib.vcr_mx_dequantize(self.h, q._ref, ctypes.byref(_mat(y))))
+        self._check(self.lib.vcr_mx_dequantize(self.h, q._c, _mat(y)))
         return y
 
     def mx_product(self, a, w, bias=None, relu=False, dtype=None, out=None):
@@ -494,18 +493,15 @@ class Ctx:
         import torch
         y = torch.empty((a.rows, w.rows), dtype=dtype or torch.float32, device=a.device) if out is None else out
         self._current_stream()
-        self._check(self.lib.vcr_mx_product(self.h, a._ref, w._ref, _bias(bias, w.rows),
-                                            1 if relu else 0, ctypes.byref(_mat(y))))
+        self._check(self.lib.vcr_mx_product(self.h, a._c, w._c, _bias(bias, w.rows), 1 if relu else 0, _mat(y)))
         return y
 
     def mx_linear(self, x, w, bias=None, relu=False, out=None):
         """act(x w^T + bias), x (rows, k) a float32 or bfloat16 tensor, w (n, k) an MX; of x's type."""
-        import torch
         m = _mat(x)
-        y = torch.empty((m.rows, w.rows), dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty((x.shape[0], w.rows)) if out is None else out
         self._current_stream()
-        self._check(self.lib.vcr_mx_linear(self.h, ctypes.byref(m), w._ref, _bias(bias, w.rows),
-                                           1 if relu else 0, ctypes.byref(_mat(y))))
+        self._check(self.lib.vcr_mx_linear(self.h, m, w._c, _bias(bias, w.rows), 1 if relu else 0, _mat(y)))
         return y
 
     def mx_linear_grad(self, dy, x, w, y=None, need=(True, True, True)):
@@ -513,24 +509,23 @@ class Ctx:
         (n, k) and db (n) float32; None where `need` says so."""
         import torch
         g = _mat(dy)
-        dx = torch.empty((g.rows, w.cols), dtype=dy.dtype, device=dy.device) if need[0] else None
-        dw = torch.empty((g.cols, x.shape[1]), dtype=torch.float32, device=dy.device) if need[1] else None
-        db = torch.empty((g.cols,), dtype=torch.float32, device=dy.device) if need[2] else None
-        ref = lambda t: None if t is None else ctypes.byref(_mat(t))  # noqa: E731
+        rows, n = dy.shape
+        dx = dy.new_empty((rows, w.cols)) if need[0] else None
+        dw = dy.new_empty((n, x.shape[1]), dtype=torch.float32) if need[1] else None
+        db = dy.new_empty((n,), dtype=torch.float32) if need[2] else None
         self._current_stream()
-        self._check(self.lib.vcr_mx_linear_grad(self.h, ctypes.byref(g), ref(y), ref(x if need[1] else None),
-                                                w._ref if need[0] else None, ref(dx), ref(dw),
-                                                None if db is None else _ptr(db)))
+        self._check(self.lib.vcr_mx_linear_grad(
+            self.h, g, None if y is None else _mat(y), _mat(x) if need[1] else None, w._c if need[0] else None,
+            None if dx is None else _mat(dx), None if dw is None else _mat(dw), None if db is None else db.data_ptr()))
         return dx, dw, db
 
     def orthogonalize(self, g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, gain=1.0, base=None,
                       keep=1.0, out=None):
         """gain X (+ keep base), X the Newton-Schulz orthogonalisation of g (m, n), or of every g[i] of (count, m,
         n): float32 or bfloat16 CUDA tensors with contiguous rows.  `out` defaults to a tensor of base's type, or
-        g's, and may be base."""
-        import torch
+        g's, and may be base; its type sets the accuracy."""
         if out is None:
-            out = torch.empty(g.shape, dtype=(g if base is None else base).dtype, device=g.device)
+            out = g.new_empty(g.shape, dtype=(g if base is None else base).dtype)
         for t in (base, out):
             if t is not None and t.shape != g.shape:
                 raise ValueError(f"expected shape {tuple(g.shape)}, got {tuple(t.shape)}")
@@ -546,9 +541,7 @@ class Ctx:
         bm = (None, 0) if base is None else one(base)
         o = VcrNsOpts(int(steps), *(float(v) for v in coefficients), float(eps), float(gain), float(keep))
         self._current_stream()
-        self._check(self.lib.vcr_orthogonalize(self.h, ctypes.byref(gm[0]), count, gm[1], ctypes.byref(o),
-                                               None if base is None else ctypes.byref(bm[0]), bm[1],
-                                               ctypes.byref(om[0]), om[1]))
+        self._check(self.lib.vcr_orthogonalize(self.h, gm[0], count, gm[1], ctypes.byref(o), bm[0], bm[1], om[0], om[1]))
         return out
 
     def layer_bounds(self, relu_id, B):
@@ -605,28 +598,35 @@ def _out_size(net):
 
 
 _TYPES = {}   # vcr_mat's types by torch's
+# vcr_mat and vcr_mx as bytes: a call of a few microseconds notices the time it takes to build the structures above
+_MAT, _MX = struct.Struct("@Piqqq"), struct.Struct("@PPqq")
 
 
 def _mat(t):
-    """A vcr_mat of a 2-d tensor."""
+    """A vcr_mat of a 2-d tensor, packed."""
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: 0, torch.bfloat16: 1})
-    kind = _TYPES.get(getattr(t, "dtype", None))
-    if kind is None or not t.is_cuda or t.dim() != 2:
-        raise ValueError("expected a float32 or bfloat16 CUDA tensor of 2 dimensions with contiguous rows")
-    (rows, cols), (ld, one) = t.shape, t.stride()
-    if one != 1 and cols > 1:
+    try:
+        kind = _TYPES[t.dtype]
+        rows, cols = t.shape
+        ld, one = t.stride()
+        cuda = t.is_cuda
+    except (AttributeError, KeyError, TypeError, ValueError):
+        cuda = False
+    if not cuda or (one != 1 and cols > 1):
         raise ValueError("expected a float32 or bfloat16 CUDA tensor of 2 dimensions with contiguous rows")
     # (a single row's stride is of no account)
-    return VcrMat(t.data_ptr(), kind, rows, cols, ld if rows > 1 else max(cols, 1))
+    return _MAT.pack(t.data_ptr(), kind, rows, cols, ld if rows > 1 else max(cols, 1))
 
 
 def _bias(b, n):
     if b is None:
         return None
-    _check_tensor(b, (n,))
-    return _ptr(b)
+    import torch
+    if not (isinstance(b, torch.Tensor) and b.dtype == torch.float32 and b.is_cuda and b.shape == (n,) and b.is_contiguous()):
+        raise ValueError(f"expected a contiguous float32 CUDA tensor of shape ({n},)")
+    return b.data_ptr()
 
 
 def _check_tensor(t, shape):

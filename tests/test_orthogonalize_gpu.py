@@ -70,12 +70,24 @@ def test_batches_strides_and_base(ctx, m, n, dtype):
     for i in range(3 if m < 1000 else 1):
         x = o64.orthogonalize(host(g[i]))
         want = 0.9 * host(base[i]) - 0.5 * x
-        tol = 0.5 * TOL[dtype] * np.linalg.norm(x) + 2.0 ** -23 * np.linalg.norm(want)
+        tol = 0.5 * TOL["float32"] * np.linalg.norm(x) + 2.0 ** -23 * np.linalg.norm(want)
         assert np.linalg.norm(host(out[i]) - want) <= tol
         assert np.linalg.norm(host(alone[i]) - want) <= tol
     same = base.clone()
     ctx.orthogonalize(g, gain=-0.5, base=same, keep=0.9, out=same)
     assert torch.equal(same, out)
+
+
+@pytest.mark.parametrize("steps", [1, 5])
+def test_results_of_the_other_type(ctx, steps):
+    import torch
+    rng = np.random.default_rng(10 + steps)
+    g = torch.as_tensor(rng.standard_normal((120, 200)), dtype=torch.float32).cuda()
+    for src, dst in (("float32", "bfloat16"), ("bfloat16", "float32")):
+        x = g.to(getattr(torch, src))
+        out = torch.empty(g.shape, dtype=getattr(torch, dst), device="cuda")
+        ctx.orthogonalize(x, steps=steps, out=out)
+        assert off(host(out), o64.orthogonalize(host(x), steps)) <= TOL[dst]
 
 
 @pytest.mark.parametrize("steps", [1, 2, 7])
