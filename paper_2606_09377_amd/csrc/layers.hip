@@ -120,12 +120,14 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t
 }
 
 // ---- operands of the bf16 products ------------------------------------------------------------
-// (a workgroup goes through the column tiles of 64 rows in the grid's order)
+// (a workgroup goes through the column tiles of 64 rows in the grid's order; the first g_tiles workgroups take g, the others,
+// if there are any, h)
 template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t col_tiles) {
+__global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t g_cols, int64_t g_tiles, PlanesArgs h, int64_t h_cols) {
   __shared__ float tile[64][65];
-  const int64_t tr = blockIdx.x / col_tiles;
-  planes_tile<P, BF>(g, 0, tr, blockIdx.x - tr * col_tiles, 1.f, tile);
+  const bool is_g = blockIdx.x < g_tiles;   // uniform
+  const int64_t at = is_g ? blockIdx.x : blockIdx.x - g_tiles, ct = is_g ? g_cols : h_cols, tr = at / ct;
+  planes_tile<P, BF>(is_g ? g : h, 0, tr, at - tr * ct, 1.f, tile);
 }
 
 // out[c] = the sum of a column over the groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
@@ -434,15 +436,23 @@ static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, c
   return hipGetLastError();
 }
 
-static hipError_t launch_planes(PlanesArgs g, hipStream_t s) {
+// h: another matrix of the same type, in the same launch (x.p null: none)
+static hipError_t launch_planes(PlanesArgs g, PlanesArgs h, hipStream_t s) {
   const int bytes = g.x.bf16 ? 2 : 4;
-  g.vec = rows_aligned(g.x.p, g.x.ld, bytes) && (!g.y.p || rows_aligned(g.y.p, g.y.ld, bytes));
-  // tiles of 64 rows and columns, those of the padding among them
-  const int64_t rt = std::max(blocks_of(g.x.rows, 64), g.cols ? blocks_of(g.col_chunks, 2) : 0);
-  const int64_t ct = std::max(blocks_of(g.x.cols, 64), g.rows ? blocks_of(g.row_chunks, 2) : 0);
-  if (rt * ct > 0x7fffffff) return hipErrorInvalidValue;
-  if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), dim3((unsigned)(rt * ct)), dim3(256), 0, s, g, ct);
-  else hipLaunchKernelGGL((k_planes<3, false>), dim3((unsigned)(rt * ct)), dim3(256), 0, s, g, ct);
+  int64_t cols[2] = {1, 1}, tiles[2] = {0, 0};
+  PlanesArgs *each[2] = {&g, &h};
+  for (int i = 0; i < 2; ++i) {
+    PlanesArgs &p = *each[i];
+    if (i == 1 && !p.rows && !p.cols) break;
+    p.vec = rows_aligned(p.x.p, p.x.ld, bytes) && (!p.y.p || rows_aligned(p.y.p, p.y.ld, bytes));
+    // tiles of 64 rows and columns, those of the padding among them
+    cols[i] = std::max(blocks_of(p.x.cols, 64), p.rows ? blocks_of(p.row_chunks, 2) : 0);
+    tiles[i] = std::max(blocks_of(p.x.rows, 64), p.cols ? blocks_of(p.col_chunks, 2) : 0) * cols[i];
+  }
+  if (tiles[0] + tiles[1] > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(tiles[0] + tiles[1]));
+  if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1]);
+  else hipLaunchKernelGGL((k_planes<3, false>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1]);
   return hipGetLastError();
 }
 
@@ -668,7 +678,7 @@ vcr_status vcr_mx_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mx *w, const fl
   pl.row_blocks = rb;
   pl.row_chunks = chunks;
   pl.grouped = 1;
-  HIP_TRY(c, launch_planes(pl, c->stream));
+  HIP_TRY(c, launch_planes(pl, PlanesArgs{}, c->stream));
   NtArgs g{};
   g.A = NtOperand{xp, nullptr, (int32_t)rb, 0};
   g.B = NtOperand{w->codes, w->scales, (int32_t)blocks_of(w->rows, 16), 0};
@@ -723,7 +733,7 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
   TRY(op_space(c, al(b_g) + al(b_wt) + al(b_gt) + al(b_xt) + al(b_sums) + al(b_part) + 6 * 256, &ws));
   uint8_t *gp = take<uint8_t>(*ws, b_g), *wt = take<uint8_t>(*ws, b_wt), *gt = take<uint8_t>(*ws, b_gt), *xt = take<uint8_t>(*ws, b_xt);
   float *sums = take<float>(*ws, b_sums / 4), *part = take<float>(*ws, b_part / 4);
-  if (has_dx || dw || db) {   // g's rows, its columns and their sums in one pass
+  if (has_dx || dw || db) {   // g's rows, its columns and their sums in one pass, and x's columns
     PlanesArgs pl{};
     pl.x = g;
     pl.y = mask;
@@ -738,7 +748,14 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
       pl.col_chunks = mch;
     }
     pl.sums = db ? sums : nullptr;
-    HIP_TRY(c, launch_planes(pl, s));
+    PlanesArgs xl{};
+    if (dw) {
+      xl.x = dev(x);
+      xl.cols = xt;
+      xl.col_blocks = kwb;
+      xl.col_chunks = mch;
+    }
+    HIP_TRY(c, launch_planes(pl, xl, s));
   }
   if (db) {
     hipLaunchKernelGGL(k_column_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, M > 0 ? mg : 0, N, db);
@@ -756,12 +773,6 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     else HIP_TRY(c, (nt_product<3, 1, NT_BF16>(a, o, part, s)));
   }
   if (dw) {
-    PlanesArgs pl{};
-    pl.x = dev(x);
-    pl.cols = xt;
-    pl.col_blocks = kwb;
-    pl.col_chunks = mch;
-    HIP_TRY(c, launch_planes(pl, s));
     NtArgs a{};
     a.A = NtOperand{gt, nullptr, (int32_t)nb, 0};
     a.B = NtOperand{xt, nullptr, (int32_t)kwb, 0};
