@@ -224,7 +224,7 @@ static int nt_parts(int64_t M, int64_t N, int64_t chunks) {
   const NtShape *sh = NtTiles<PA, PB, KIND>::shapes, &x = sh[NT_SHAPES - 1];
   const int64_t t = nt_tiles(M, N, x.bm, x.bn, false), parts = std::min<int64_t>(NT_CUS / t, chunks / 16);
   if (parts < 2) return 1;
-  return nt_us(x, t * parts, (chunks + parts - 1) / parts) + NT_LAUNCH_US < nt_plan(sh, M, N, chunks, 1, false).us ? (int)parts : 1;
+  return nt_us(x, t * parts, (chunks + parts - 1) / parts, 4.f) + NT_LAUNCH_US < nt_plan(sh, M, N, chunks, 1, false, 4.f).us ? (int)parts : 1;
 }
 template <int PA, int PB, int KIND>
 static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
@@ -236,7 +236,7 @@ template <int PA, int PB, int KIND>
 static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipStream_t s) {
   typedef NtTiles<PA, PB, KIND> TS;
   const int parts = nt_parts<PA, PB, KIND>(o.rows, o.cols, g.chunks);
-  if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, EpiOut{o}, s);
+  if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, o.bf16 ? 2.f : 4.f, EpiOut{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
   const NtShape &x = TS::shapes[NT_SHAPES - 1];
   const hipError_t e = launch_nt<typename TS::T4>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,

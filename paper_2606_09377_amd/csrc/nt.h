@@ -475,7 +475,8 @@ struct NtShape {
   float us1, us2;   // us of a chunk of a workgroup alone on its compute unit, of two together (0: only one fits)
 };
 constexpr int NT_SHAPES = 5, NT_CUS = 256;
-constexpr float NT_LAUNCH_US = 4.f, NT_ROUND_US = 2.f;   // of a launch, of a workgroup's start and end
+// of a launch, of a workgroup's start and end, and a compute unit's share of the memory's rate
+constexpr float NT_LAUNCH_US = 4.f, NT_ROUND_US = 2.f, NT_WRITE_BYTES_US = 20e3f;
 struct NtPlan {
   int main = 0, rest = -1;   // shapes
   int64_t main_tiles = 0, rest_tiles = 0;   // counted in main's shape, over the batch
@@ -488,16 +489,18 @@ inline int64_t nt_tiles(int64_t M, int64_t N, int bm, int bn, bool tri) {
   for (int64_t i = 0; i < mt; ++i) s += nt_row_tiles((int)i, bm, bn, (int)nt, true);
   return s;
 }
-inline float nt_us(const NtShape &s, int64_t tiles, int64_t chunks) {
+// out_bytes: what the epilogue writes per output; of a workgroup alone on its compute unit nothing hides it
+inline float nt_us(const NtShape &s, int64_t tiles, int64_t chunks, float out_bytes) {
   const int64_t n = (tiles + NT_CUS - 1) / NT_CUS;
-  const float one = s.us1 * (float)chunks + NT_ROUND_US, two = s.us2 * (float)chunks + NT_ROUND_US;
+  const float end = NT_ROUND_US + (s.us2 > 0.f ? .3f : 1.f) * (float)(s.bm * s.bn) * out_bytes / NT_WRITE_BYTES_US;
+  const float one = s.us1 * (float)chunks + end, two = s.us2 * (float)chunks + end;
   return NT_LAUNCH_US + (s.us2 > 0.f ? (float)(n / 2) * two + (float)(n % 2) * one : (float)n * one);
 }
-inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri) {
+inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri, float out_bytes) {
   NtPlan best;
   for (int a = 0; a < NT_SHAPES; ++a) {
     const int64_t t = nt_tiles(M, N, sh[a].bm, sh[a].bn, tri) * batch;
-    const float all = nt_us(sh[a], t, chunks);
+    const float all = nt_us(sh[a], t, chunks, out_bytes);
     if (a == 0 || all < best.us) {
       best.main = a;
       best.rest = -1;
@@ -509,7 +512,7 @@ inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, i
     if (full == 0 || full == t) continue;
     for (int b = a + 1; b < NT_SHAPES; ++b) {
       const int64_t subs = (int64_t)(sh[a].bm / sh[b].bm) * (sh[a].bn / sh[b].bn);
-      const float us = nt_us(sh[a], full, chunks) + nt_us(sh[b], (t - full) * subs, chunks);
+      const float us = nt_us(sh[a], full, chunks, out_bytes) + nt_us(sh[b], (t - full) * subs, chunks, out_bytes);
       if (us < best.us) {
         best.main = a;
         best.rest = b;
@@ -548,8 +551,8 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
 }
 // A product by the shapes of TS (T0 .. T4 and their `shapes`)
 template <class TS, class EPI>
-hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, const EPI &epi, hipStream_t s) {
-  const NtPlan p = nt_plan(TS::shapes, M, N, g.chunks, batch, g.tri);
+hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, float out_bytes, const EPI &epi, hipStream_t s) {
+  const NtPlan p = nt_plan(TS::shapes, M, N, g.chunks, batch, g.tri, out_bytes);
   auto go = [&](int shape, int64_t first, int64_t count) {
     const int bm = TS::shapes[p.main].bm, bn = TS::shapes[p.main].bn;
     switch (shape) {

@@ -162,18 +162,18 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
     a.chunks = (int32_t)(np / 32);
     a.tri = 1;
     e.dst = sp.gram;
-    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, EpiNs<P, NS_GRAM>{e}, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_GRAM>{e}, s)) != hipSuccess) return err;
     a.A = a.B = NtOperand{sp.gram, nullptr, (int32_t)(mp / 16), sg};
     a.chunks = (int32_t)(mp / 32);
     e.gram = sp.gram;
     e.dst = sp.poly;
-    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, EpiNs<P, NS_POLY>{e}, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_POLY>{e}, s)) != hipSuccess) return err;
     a.A = NtOperand{sp.poly, nullptr, (int32_t)(mp / 16), sg};
     a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx};
     a.tri = 0;
     e.dst = sp.x2;
     e.dst_t = sp.xt2;
-    err = step + 1 == steps ? launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, EpiNs<P, NS_OUT>{e}, s) : launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, EpiNs<P, NS_UPDATE>{e}, s);
+    err = step + 1 == steps ? launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, e.base.p ? 8.f : 4.f, EpiNs<P, NS_OUT>{e}, s) : launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, 4.f * P, EpiNs<P, NS_UPDATE>{e}, s);
     if (err != hipSuccess) return err;
     std::swap(sp.x, sp.x2);
     std::swap(sp.xt, sp.xt2);
