@@ -11,7 +11,10 @@
 // (float32's accuracy), bf16 ones two: what one step rounds, the later ones raise by up to a = 3.4 each with the smallest
 // singular values, so that one part's 2^-9 would be far above the result's own rounding, and two parts' 2^-17 is below it.
 //
-// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 24.4 ms: 33 TFLOP of partial products
+// A bf16 update is exact in one part, times a power of two: the first step multiplies one part where the later ones take
+// two or three (8192 x 8192: 24.4 to 22.6 ms).
+//
+// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 22.6 ms: 31 TFLOP of partial products
 // at 1.37 PFLOP/s), by the operands the epilogues write and the tiles' last rounds at 1024 (five float32 1024 x 1024 in 0.75 ms: a
 // step's three launches take 43, 46 and 62 us, of which 12 write X twice), and by the starts and ends of fifteen launches of 12
 // to 21 us on 777 x 1500.
@@ -54,11 +57,19 @@ __device__ __forceinline__ float ns_scale(const double *part, int batch, float e
   return (float)(1.0 / (sqrt(s) + (double)eps));
 }
 
-// X's parts from G, its rows' and its columns' (bf16 8192 x 8192, 671 MB with what it writes, in 145 us)
-template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps) {
+// X's parts from G, its rows' and its columns' (bf16 8192 x 8192, 403 MB with what it writes, in
+// 93 us).  RAW: G as it is, times the
+// power of two that brings its norm near 1: exact in one part for a bf16 G, so that the first step multiplies one part; the rest
+// of the factor is left to its epilogues (scale[batch]).
+template <int P, bool BF, bool RAW>
+__global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps, float *scale) {
   __shared__ float tile[64][65];
-  const float sc = ns_scale(part, blockIdx.y, eps);
+  float sc = ns_scale(part, blockIdx.y, eps);
+  if constexpr (RAW) {
+    const float two = __builtin_bit_cast(float, max(__builtin_bit_cast(uint32_t, sc) & 0x7f800000u, 0x00800000u));
+    if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = sc / two;
+    sc = two;
+  }
   const int64_t tr = blockIdx.x / col_tiles, bytes = g.row_blocks * g.row_chunks * P * FRAG;   // of either
   g.rows += blockIdx.y * bytes;
   g.cols += blockIdx.y * bytes;
@@ -79,13 +90,19 @@ struct NsEpilogue {
   int64_t out_rows, out_cols, out_ld, out_stride;
   float keep, gain;
   int32_t out_bf16, vec, transposed;
+  const float *scale;   // FIRST: of X in its product (gram: of both factors)
 };
-template <int P, int MODE>
+template <int P, int MODE, bool FIRST = false>
 struct EpiNs : NsEpilogue {
   __device__ __forceinline__ void store(int batch, int, int m, int n, f32v4 v, int lane) const {
     const int bm = m >> 4, bn = n >> 4, r = lane & 15;
     // after a transposition the lane holds row nt, columns mt .. mt + 3
     const int nt = n + (r & 3), mt = (m & ~3);
+    if constexpr (FIRST && MODE != NS_POLY) {
+      const float s = scale[batch];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = MODE == NS_GRAM ? v[i] * s * s : v[i] * s;
+    }
     if constexpr (MODE <= NS_POLY) {
       if (bm * 16 >= mp || bn > bm) return;   // wave-uniform
       const int64_t off = (int64_t)batch * (mp / 16) * (mp / 32) * P * FRAG;
@@ -121,12 +138,14 @@ struct EpiNs : NsEpilogue {
 
 struct NsSpace {
   double *norm;
+  float *scale;
   uint8_t *x, *xt, *x2, *xt2, *gram, *poly;
 };
 static NsSpace ns_carve(Workspace &w, int64_t mp, int64_t np, int batch, int P) {
   NsSpace s;
   const size_t bx = (size_t)batch * mp * np * 2 * P, bg = (size_t)batch * mp * mp * 2 * P;
   s.norm = take<double>(w, (size_t)batch * NORM_PARTS);
+  s.scale = take<float>(w, (size_t)batch);
   s.x = take<uint8_t>(w, bx);
   s.xt = take<uint8_t>(w, bx);
   s.x2 = take<uint8_t>(w, bx);
@@ -156,32 +175,42 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
   pl.col_blocks = cp / 16;
   pl.col_chunks = rp / 32;
   const int64_t ct = blocks_of(cp, 64);
-  hipLaunchKernelGGL((k_ns_planes<P, BF>), dim3((unsigned)(blocks_of(rp, 64) * ct), batch), dim3(256), 0, s, pl, ct, sp.norm, eps);
+  constexpr int P0 = BF ? 1 : P;   // parts of the first step's X
+  hipLaunchKernelGGL((k_ns_planes<P0, BF, BF>), dim3((unsigned)(blocks_of(rp, 64) * ct), batch), dim3(256), 0, s, pl, ct, sp.norm, eps, sp.scale);
   if ((err = hipGetLastError()) != hipSuccess) return err;
   e.mp = (int32_t)mp;
   e.np = (int32_t)np;
-  const int64_t sx = mp * np * 2 * P, sg = mp * mp * 2 * P;
-  for (int step = 0; step < steps; ++step) {
+  e.scale = sp.scale;
+  const int64_t sg = mp * mp * 2 * P;
+  auto step = [&](auto first, bool last) {   // first: of a bf16 G, whose X has one part
+    constexpr bool FIRST = decltype(first)::value;
+    constexpr int PX = FIRST ? P0 : P;
+    const int64_t sx0 = mp * np * 2 * PX;
+    hipError_t err;
     NtArgs a{};
-    a.A = a.B = NtOperand{sp.x, nullptr, (int32_t)(mp / 16), sx};
+    a.A = a.B = NtOperand{sp.x, nullptr, (int32_t)(mp / 16), sx0};
     a.chunks = (int32_t)(np / 32);
     a.tri = 1;
     e.dst = sp.gram;
-    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_GRAM>{e}, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<PX, PX, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_GRAM, FIRST>{e}, s)) != hipSuccess) return err;
     a.A = a.B = NtOperand{sp.gram, nullptr, (int32_t)(mp / 16), sg};
     a.chunks = (int32_t)(mp / 32);
     e.gram = sp.gram;
     e.dst = sp.poly;
     if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_POLY>{e}, s)) != hipSuccess) return err;
     a.A = NtOperand{sp.poly, nullptr, (int32_t)(mp / 16), sg};
-    a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx};
+    a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx0};
     a.tri = 0;
     e.dst = sp.x2;
     e.dst_t = sp.xt2;
-    err = step + 1 == steps ? launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, e.base.p ? 8.f : 4.f, EpiNs<P, NS_OUT>{e}, s) : launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, np, batch, 4.f * P, EpiNs<P, NS_UPDATE>{e}, s);
-    if (err != hipSuccess) return err;
     std::swap(sp.x, sp.x2);
     std::swap(sp.xt, sp.xt2);
+    return last ? launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, e.base.p ? 8.f : 4.f, EpiNs<P, NS_OUT, FIRST>{e}, s)
+                : launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, 4.f * P, EpiNs<P, NS_UPDATE, FIRST>{e}, s);
+  };
+  for (int i = 0; i < steps; ++i) {
+    err = BF && i == 0 ? step(std::integral_constant<bool, BF>{}, i + 1 == steps) : step(std::false_type{}, i + 1 == steps);
+    if (err != hipSuccess) return err;
   }
   return hipSuccess;
 }

@@ -114,3 +114,9 @@ def test_zero_tiny_huge_and_non_finite(ctx):
         h = g.copy()
         h[3, 4] = v
         assert torch.isnan(ctx.orthogonalize(torch.as_tensor(h).cuda())).all()
+        assert torch.isnan(ctx.orthogonalize(torch.as_tensor(h).bfloat16().cuda())).all()
+    assert not ctx.orthogonalize(z.bfloat16()).any()
+    for s in (1e-37, 1e-30, 1e30, 1e37):   # the norm's power of two is taken out of a bf16 update exactly
+        b = torch.as_tensor(g * np.float32(s)).bfloat16().cuda()
+        out = ctx.orthogonalize(b, eps=0.0, out=torch.empty((40, 60), device="cuda"))
+        assert off(host(out), o64.orthogonalize(host(b), eps=0.0)) <= TOL["float32"]
