@@ -30,7 +30,8 @@ __device__ __forceinline__ int64_t mx_scale_at(int64_t rb, int64_t group, int64_
 
 // Quantisation.  A workgroup takes 16 rows by 512 columns: a wave reads a row's 512 at once, a thread 8 of
 // them, four threads a block; the codes go through LDS into the storage order.  Bound by memory: 8192 x 8192
-// float32, 304 MB, in 55 us, 5.5 TB/s, the rate of a large copy.
+// float32, 304 MB, in 55 us, 5.5 TB/s, the rate of a large copy (67 to 78 us where the memory is still taking in the 268 MB
+// that a call before wrote: read back and quantised in turn, both take 124).
 template <bool BF>
 __global__ __launch_bounds__(256) void k_mx_quantize(DevMat x, int vec, uint8_t *codes, uint8_t *scales) {
   __shared__ uint32_t cs[4][4][16][4];   // [group][block][row][words]
