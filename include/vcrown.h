@@ -375,7 +375,8 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  * must not overlap inputs unless stated.  These calls need no loaded network and leave it, its bounds
  * and the other calls' workspace alone; they keep one workspace for every stream they were given, which grows
  * as needed (VCR_ERR_OOM beyond VCR_OPT_WORKSPACE_CAP_BYTES) and is kept until vcr_destroy.  A call may be recorded into a HIP graph by the
- * caller once it has run with the same sizes on that stream (else VCR_ERR_STATE). */
+ * caller once it has run with the same sizes on that stream (else VCR_ERR_STATE); the graph keeps that stream's
+ * workspace, so its replays are to be ordered with each other and with the calls on that stream. */
 enum { VCR_F32 = 0, VCR_BF16 = 1 };
 
 /* Longest contraction of a product here (the shared dimension; for gradients also the rows of dy, for
