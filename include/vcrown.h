@@ -435,8 +435,7 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *ctx, const vcr_mat *dy, const vcr_mat *y,
 /* Newton-Schulz orthogonalisation: X = g / (|g|_F + eps), then `steps` times, with A = X X^T (X^T X for more
  * rows than columns), X <- (a I + b A + c A A) X (from the right); out = gain X, or keep base + gain X.  With a =
  * 3.4445, b = -4.7750, c = 2.0315 five steps bring singular values above about 2^-9 of the norm
- * into [0.7, 1.2].  A float32 out is computed to float32's accuracy, a bf16 one with 16 bits of every
- * factor, whatever g's type. */
+ * into [0.7, 1.2].  X and the products are held to float32's accuracy, whatever the types. */
 typedef struct {
   int32_t steps;            /* in [1, 100] */
   float a, b, c;

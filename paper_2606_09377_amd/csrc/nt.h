@@ -16,8 +16,6 @@
 // (A parts, B parts), in order of their size:
 //   (1, 1)  h h
 //   (3, 1)  l h, m h | h h        B is exact in one part (4-bit values times powers of two)
-//   (2, 1)  m h, h h
-//   (2, 2)  h m, m h, h h         16 bits of both
 //   (3, 3)  h l, l h, m m, h m, m h | h h      float32's products (2^-24)
 // Where a bar stands, the small products have an accumulator of their own, added at the end: summed into
 // the large one they are cut off at its precision, always downwards (split_bf16.h).
@@ -75,7 +73,7 @@ template <int KIND_, int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int P
 struct NtTile {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, PA = PA_, PB = PB_, KS = KS_, NS = NS_;
   static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED;
-  static constexpr int PRODUCTS = PA == 3 ? (PB == 3 ? 6 : 3) : PA == 2 ? PB + 1 : 1;
+  static constexpr int PRODUCTS = PA == 3 ? (PB == 3 ? 6 : 3) : 1;
   static constexpr int KW = KS / WK;   // chunks of a stage that a wave multiplies
   static constexpr int NW = WM * WN * WK, T = 64 * NW;
   static constexpr int BM = 16 * MB * WM, BN = 16 * NB * WN;
@@ -295,10 +293,9 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
         hi[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(c.b[j][0]), wide(c.a[i][0]), hi[i][j], 4, 4, 0, c.bs[j], 0, c.as[i]);
     } else {
       // (A part, B part) and accumulator of product p
-      constexpr int pa33[6] = {0, 2, 1, 0, 1, 0}, pb33[6] = {2, 0, 1, 1, 0, 0}, pa31[3] = {2, 1, 0}, pa22[3] = {0, 1, 0}, pb22[3] = {1, 0, 0};
-      constexpr int pa21[2] = {1, 0};
-      const int pa = T::PRODUCTS == 6 ? pa33[p] : PA == 3 ? pa31[p] : T::PRODUCTS == 3 ? pa22[p] : PA == 2 ? pa21[p] : 0;
-      const int pb = T::PRODUCTS == 6 ? pb33[p] : PA == 2 && PB == 2 ? pb22[p] : 0;
+      constexpr int pa33[6] = {0, 2, 1, 0, 1, 0}, pb33[6] = {2, 0, 1, 1, 0, 0}, pa31[3] = {2, 1, 0};
+      const int pa = T::PRODUCTS == 6 ? pa33[p] : PA == 3 ? pa31[p] : 0;
+      const int pb = T::PRODUCTS == 6 ? pb33[p] : 0;
       const bool small = T::TWO && p + 1 < T::PRODUCTS;
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
@@ -611,25 +608,6 @@ struct NtTiles<3, 3, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 1, 1, 4, 1, 3, 3, 1, 4> T3;
   typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
   static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
-};
-template <>
-struct NtTiles<2, 2, NT_BF16> {
-  typedef NtTile<NT_BF16, 4, 4, 4, 2, 1, 2, 2, 1, 3> T0;
-  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 2, 2, 1, 4> T1;
-  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 2, 2, 1, 4> T2;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 2, 2, 2, 3> T3;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 4, 2, 2, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, 1.f, 0.f}, {128, 128, .533f, 0.f}, {64, 64, .197f, .372f}, {32, 64, .155f, .265f}, {32, 64, .137f, 0.f}};
-};
-
-template <>
-struct NtTiles<2, 1, NT_BF16> {
-  typedef NtTile<NT_BF16, 4, 4, 4, 2, 1, 2, 1, 1, 3> T0;
-  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 2, 1, 1, 4> T1;
-  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 2, 1, 1, 4> T2;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 2, 1, 2, 4> T3;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 4, 2, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 128, .69f, 0.f}, {128, 128, .39f, 0.f}, {64, 64, .162f, .273f}, {32, 64, .079f, .175f}, {32, 64, .08f, 0.f}};
 };
 template <>
 struct NtTiles<1, 1, NT_MIXED> {

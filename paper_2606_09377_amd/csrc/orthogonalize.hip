@@ -7,15 +7,15 @@
 // A and Q are symmetric: of their 16 x 16 blocks those on and below the diagonal are computed and
 // stored twice.  A step is 3 m^2 n + m^3 multiply-adds that way (of 4 m^2 n + 2 m^3).  All three products
 // contract the contiguous axes of operands in the layout of nt.h: X (rows m) and its transpose (rows
-// n) are both kept, written by the epilogue that makes them.  float32 results take three bf16 parts
-// (float32's accuracy), bf16 ones two: what one step rounds, the later ones raise by up to a = 3.4 each with the smallest
-// singular values, so that one part's 2^-9 would be far above the result's own rounding, and two parts' 2^-17 is below it.
+// n) are both kept, written by the epilogue that makes them.  X, A and Q are held in three bf16 parts, float32's accuracy, whatever
+// the result's type: what one step rounds, the later ones raise by up to a = 3.4 each in the directions that the update has little
+// or nothing of.  (With two parts, 2^-17, a bf16 result of a 300 x 500 update of rank 1 is off by 2.8e-3 after five steps and
+// 6e-2 after eight, where its own rounding is 1.7e-3.)
 //
-// A bf16 update is exact in one part, times a power of two: the first step multiplies one part where the later ones take
-// two or three (8192 x 8192: 24.4 to 22.6 ms).
+// A bf16 update is exact in one part, times a power of two: the first step multiplies one part where the later ones take three.
 //
-// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 22.6 ms: 31 TFLOP of partial products
-// at 1.37 PFLOP/s), by the operands the epilogues write and the tiles' last rounds at 1024 (five float32 1024 x 1024 in 0.75 ms: a
+// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 44.0 ms: 60 TFLOP of partial products
+// at 1.36 PFLOP/s), by the operands the epilogues write and the tiles' last rounds at 1024 (five float32 1024 x 1024 in 0.75 ms: a
 // step's three launches take 43, 46 and 62 us, of which 12 write X twice), and by the starts and ends of fifteen launches of 12
 // to 21 us on 777 x 1500.
 #include <algorithm>
@@ -27,6 +27,8 @@
 namespace vcr {
 
 constexpr int NORM_PARTS = 1024;   // partial sums of a matrix's squares
+constexpr int P = 3;               // parts of X, A and Q
+constexpr int first_parts(bool bf16) { return bf16 ? 1 : P; }   // of the first step's X
 
 // Sums of squares in 64 bits (float32's range does not hold the squares of all its values): a wave per stretch of 512
 // columns of a row.  Bound by memory: a bf16 8192 x 8192 update, 134 MB, in 32 us.
@@ -58,22 +60,22 @@ __device__ __forceinline__ float ns_scale(const double *part, int batch, float e
 }
 
 // X's parts from G, its rows' and its columns' (bf16 8192 x 8192, 403 MB with what it writes, in
-// 93 us).  RAW: G as it is, times the
-// power of two that brings its norm near 1: exact in one part for a bf16 G, so that the first step multiplies one part; the rest
-// of the factor is left to its epilogues (scale[batch]).
-template <int P, bool BF, bool RAW>
+// 93 us).  A bf16 G as it is, times the power of two that brings its norm near 1: exact in one part, so that the first step
+// multiplies one part; the rest of the factor is left to its epilogues (scale[batch]).
+template <bool BF>
 __global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps, float *scale) {
+  constexpr int P0 = first_parts(BF);
   __shared__ float tile[64][65];
   float sc = ns_scale(part, blockIdx.y, eps);
-  if constexpr (RAW) {
+  if constexpr (BF) {
     const float two = __builtin_bit_cast(float, max(__builtin_bit_cast(uint32_t, sc) & 0x7f800000u, 0x00800000u));
     if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = sc / two;
     sc = two;
   }
-  const int64_t tr = blockIdx.x / col_tiles, bytes = g.row_blocks * g.row_chunks * P * FRAG;   // of either
+  const int64_t tr = blockIdx.x / col_tiles, bytes = g.row_blocks * g.row_chunks * P0 * FRAG;   // of either
   g.rows += blockIdx.y * bytes;
   g.cols += blockIdx.y * bytes;
-  planes_tile<P, BF>(g, (int64_t)blockIdx.y * g.x.stride, tr, blockIdx.x - tr * col_tiles, sc, tile);
+  planes_tile<P0, BF>(g, (int64_t)blockIdx.y * g.x.stride, tr, blockIdx.x - tr * col_tiles, sc, tile);
 }
 
 enum NsMode : int32_t { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2, NS_OUT = 3 };
@@ -92,7 +94,7 @@ struct NsEpilogue {
   int32_t out_bf16, vec, transposed;
   const float *scale;   // FIRST: of X in its product (gram: of both factors)
 };
-template <int P, int MODE, bool FIRST = false>
+template <int MODE, bool FIRST = false>
 struct EpiNs : NsEpilogue {
   __device__ __forceinline__ void store(int batch, int, int m, int n, f32v4 v, int lane) const {
     const int bm = m >> 4, bn = n >> 4, r = lane & 15;
@@ -141,7 +143,7 @@ struct NsSpace {
   float *scale;
   uint8_t *x, *xt, *x2, *xt2, *gram, *poly;
 };
-static NsSpace ns_carve(Workspace &w, int64_t mp, int64_t np, int batch, int P) {
+static NsSpace ns_carve(Workspace &w, int64_t mp, int64_t np, int batch) {
   NsSpace s;
   const size_t bx = (size_t)batch * mp * np * 2 * P, bg = (size_t)batch * mp * mp * 2 * P;
   s.norm = take<double>(w, (size_t)batch * NORM_PARTS);
@@ -155,7 +157,7 @@ static NsSpace ns_carve(Workspace &w, int64_t mp, int64_t np, int batch, int P) 
   return s;
 }
 
-template <int P, bool BF>
+template <bool BF>
 static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, bool transposed, int steps, NsEpilogue e, float eps,
                          NsSpace sp, hipStream_t s) {
   const int vec = rows_aligned(g.p, g.ld, BF ? 2 : 4) && (g.stride * (BF ? 2 : 4)) % 16 == 0;
@@ -175,8 +177,8 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
   pl.col_blocks = cp / 16;
   pl.col_chunks = rp / 32;
   const int64_t ct = blocks_of(cp, 64);
-  constexpr int P0 = BF ? 1 : P;   // parts of the first step's X
-  hipLaunchKernelGGL((k_ns_planes<P0, BF, BF>), dim3((unsigned)(blocks_of(rp, 64) * ct), batch), dim3(256), 0, s, pl, ct, sp.norm, eps, sp.scale);
+  constexpr int P0 = first_parts(BF);
+  hipLaunchKernelGGL((k_ns_planes<BF>), dim3((unsigned)(blocks_of(rp, 64) * ct), batch), dim3(256), 0, s, pl, ct, sp.norm, eps, sp.scale);
   if ((err = hipGetLastError()) != hipSuccess) return err;
   e.mp = (int32_t)mp;
   e.np = (int32_t)np;
@@ -192,12 +194,12 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
     a.chunks = (int32_t)(np / 32);
     a.tri = 1;
     e.dst = sp.gram;
-    if ((err = launch_nt_plan<NtTiles<PX, PX, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_GRAM, FIRST>{e}, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<PX, PX, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<NS_GRAM, FIRST>{e}, s)) != hipSuccess) return err;
     a.A = a.B = NtOperand{sp.gram, nullptr, (int32_t)(mp / 16), sg};
     a.chunks = (int32_t)(mp / 32);
     e.gram = sp.gram;
     e.dst = sp.poly;
-    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<P, NS_POLY>{e}, s)) != hipSuccess) return err;
+    if ((err = launch_nt_plan<NtTiles<P, P, NT_BF16>>(a, mp, mp, batch, 4.f * P, EpiNs<NS_POLY>{e}, s)) != hipSuccess) return err;
     a.A = NtOperand{sp.poly, nullptr, (int32_t)(mp / 16), sg};
     a.B = NtOperand{sp.xt, nullptr, (int32_t)(np / 16), sx0};
     a.tri = 0;
@@ -205,8 +207,8 @@ static hipError_t ns_run(const DevMat &g, int batch, int64_t mp, int64_t np, boo
     e.dst_t = sp.xt2;
     std::swap(sp.x, sp.x2);
     std::swap(sp.xt, sp.xt2);
-    return last ? launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, e.base.p ? 8.f : 4.f, EpiNs<P, NS_OUT, FIRST>{e}, s)
-                : launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, 4.f * P, EpiNs<P, NS_UPDATE, FIRST>{e}, s);
+    return last ? launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, e.base.p ? 8.f : 4.f, EpiNs<NS_OUT, FIRST>{e}, s)
+                : launch_nt_plan<NtTiles<P, PX, NT_BF16>>(a, mp, np, batch, 4.f * P, EpiNs<NS_UPDATE, FIRST>{e}, s);
   };
   for (int i = 0; i < steps; ++i) {
     err = BF && i == 0 ? step(std::integral_constant<bool, BF>{}, i + 1 == steps) : step(std::false_type{}, i + 1 == steps);
@@ -245,12 +247,11 @@ extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t co
   if (count == 0 || g->rows == 0) return VCR_OK;
   const bool tr = g->rows > g->cols, bf = g->type == VCR_BF16;
   const int64_t mp = blocks_of(std::min(g->rows, g->cols), 32) * 32, np = blocks_of(std::max(g->rows, g->cols), 32) * 32;
-  const int P = out->type == VCR_BF16 ? 2 : 3;
   Workspace size;
-  (void)ns_carve(size, mp, np, count, P);
+  (void)ns_carve(size, mp, np, count);
   Workspace *ws = nullptr;
   if ((st = op_space(c, size.used, &ws)) != VCR_OK) return st;
-  const NsSpace sp = ns_carve(*ws, mp, np, count, P);
+  const NsSpace sp = ns_carve(*ws, mp, np, count);
   const DevMat d{g->p, bf, g->rows, g->cols, g->ld, g_stride};
   NsEpilogue e{};
   e.a = o->a;
@@ -267,12 +268,7 @@ extern "C" vcr_status vcr_orthogonalize(vcr_ctx *c, const vcr_mat *g, int32_t co
   e.out_bf16 = out->type == VCR_BF16;
   e.vec = (reinterpret_cast<uintptr_t>(out->p) & (e.out_bf16 ? 7 : 15)) == 0 && out->ld % 4 == 0 && out_stride % 4 == 0;
   e.transposed = tr;
-  auto run = [&](auto parts, auto g16) {
-    return ns_run<decltype(parts)::value, decltype(g16)::value>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream);
-  };
-  typedef std::integral_constant<int, 2> Two;
-  typedef std::integral_constant<int, 3> Three;
-  HIP_TRY(c, P == 2 ? (bf ? run(Two{}, std::true_type{}) : run(Two{}, std::false_type{}))
-                    : (bf ? run(Three{}, std::true_type{}) : run(Three{}, std::false_type{})));
+  HIP_TRY(c, bf ? ns_run<true>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream)
+                : ns_run<false>(d, count, mp, np, tr, o->steps, e, o->eps, sp, c->stream));
   return op_end(c);
 }

@@ -523,7 +523,7 @@ class Ctx:
                       keep=1.0, out=None):
         """gain X (+ keep base), X the Newton-Schulz orthogonalisation of g (m, n), or of every g[i] of (count, m,
         n): float32 or bfloat16 CUDA tensors with contiguous rows.  `out` defaults to a tensor of base's type, or
-        g's, and may be base; its type sets the accuracy."""
+        g's, and may be base."""
         if out is None:
             out = g.new_empty(g.shape, dtype=(g if base is None else base).dtype)
         for t in (base, out):

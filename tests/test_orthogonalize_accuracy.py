@@ -1,0 +1,98 @@
+"""How near the orthogonalised update stays to 64 bits, at an accuracy that fewer bits of its factors would miss.
+
+Bound.  X_0 = g / |g|, X_(i+1) = (a I + b A + c A A) X_i.  What is rounded in X_i, e |X_i| in the Frobenius norm, falls
+mostly into directions in which the update has little or nothing, and those grow by a in every later step:
+e sum_i |X_i| a^(steps - i) in all, with |X_i| of the 64-bit steps.  e: factors of 24 bits (2^-25 in the mean square) in three
+products a step, sums of some tens of additions rounded or cut to 24 bits (together some 2^-24): 2^-23 is allowed.  A bf16
+result adds its own rounding, which is known: that of the 64-bit result.
+
+The same steps with factors of 16 bits (two bf16 parts) are modelled below, and are outside these bounds where a matrix
+has small singular values."""
+import functools
+
+import numpy as np
+import pytest
+
+from oracle import layers64 as o64
+
+A, B, C, EPS = 3.4445, -4.7750, 2.0315, 1e-7
+
+
+def bf16(x):
+    import torch
+    return torch.as_tensor(np.asarray(x, dtype=np.float32)).bfloat16().double().numpy()
+
+
+def low_rank(m, n, r, bits=24):
+    rng = np.random.default_rng(m + n + r)
+    g = (rng.standard_normal((m, r)) @ rng.standard_normal((r, n))).astype(np.float32)
+    return bf16(g) if bits == 8 else g.astype(np.float64)
+
+
+def gaussian(m, n, bits=24):
+    g = (np.random.default_rng(m + 3 * n).standard_normal((m, n)) * 1e-3).astype(np.float32)
+    return bf16(g) if bits == 8 else g.astype(np.float64)
+
+
+@functools.lru_cache(maxsize=None)
+def expected(make, shape, bits, steps):
+    """(g, the 64-bit result, its bound before the result's own rounding)"""
+    g = make(*shape, bits=bits)
+    sizes = [np.linalg.norm(o64.orthogonalize(g, i, (A, B, C), EPS)) for i in range(steps)]
+    return g, o64.orthogonalize(g, steps, (A, B, C), EPS), 2.0 ** -23 * sum(s * A ** (steps - i) for i, s in enumerate(sizes))
+
+
+def outside(got, want, bound, bf16_out):
+    """How many times the bound the error is."""
+    return np.linalg.norm(got - want) / (bound + (np.linalg.norm(bf16(want) - want) if bf16_out else 0.0))
+
+
+# (matrix, shape, bits of g, bf16 result, steps)
+CASES = [(low_rank, (300, 500, 1), 24, True, 5), (low_rank, (300, 500, 1), 24, True, 8),
+         (low_rank, (500, 300, 8), 24, True, 8), (low_rank, (300, 500, 64), 8, True, 8),
+         (low_rank, (300, 500, 1), 24, False, 5), (low_rank, (300, 500, 8), 24, False, 5),
+         *[(gaussian, s, bits, False, 5) for s in ((32, 32), (33, 65), (100, 784), (300, 257), (513, 1000), (1500, 777))
+           for bits in (24, 8)]]
+
+
+def modelled(g, parts, steps):
+    """The steps with factors of `parts` bf16 values, their products' smallest left out, in 64 bits otherwise."""
+    def split(x):
+        out, x = [], x.astype(np.float32).astype(np.float64)
+        for _ in range(parts):
+            out.append(bf16(x))
+            x = x - out[-1]
+        return out
+
+    def product(x, y):
+        return sum(x[i] @ y[j] for i in range(parts) for j in range(parts) if i + j < parts)
+    tall = g.shape[0] > g.shape[1]
+    x = split((g.T if tall else g) / (np.linalg.norm(g) + EPS))
+    for _ in range(steps):
+        gram = split(product(x, [p.T for p in x]))
+        q = split(A * np.eye(gram[0].shape[0]) + B * sum(gram) + C * product(gram, gram))
+        y = product(q, x)
+        x = split(y)
+    return y.T if tall else y
+
+
+# (a wide matrix or a small one has hardly any singular values small enough to grow in every step)
+@pytest.mark.parametrize("make,shape,bits,bf16_out,steps", [c for c in CASES if min(c[1][:2]) > 250])
+def test_bounds_tell_two_parts_from_three(make, shape, bits, bf16_out, steps):
+    g, want, bound = expected(make, shape, bits, steps)
+    far = [outside(bf16(y) if bf16_out else y, want, bound, bf16_out) for y in (modelled(g, 2, steps), modelled(g, 3, steps))]
+    assert far[0] > 1 > far[1], far
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("make,shape,bits,bf16_out,steps", CASES)
+def test_update_is_held_in_float32(make, shape, bits, bf16_out, steps):
+    import torch
+    from paper_2606_09377_amd import Ctx
+    g, want, bound = expected(make, shape, bits, steps)
+    t = torch.as_tensor(g, dtype=torch.float32).cuda().to(torch.bfloat16 if bits == 8 else torch.float32)
+    out = torch.empty(t.shape, dtype=torch.bfloat16 if bf16_out else torch.float32, device="cuda")
+    Ctx(0).orthogonalize(t, steps=steps, coefficients=(A, B, C), eps=EPS, out=out)
+    far = outside(out.double().cpu().numpy(), want, bound, bf16_out)
+    print(f"{make.__name__} {shape} {bits} bits, {steps} steps: {far:.3f} of the bound", flush=True)
+    assert far <= 1
