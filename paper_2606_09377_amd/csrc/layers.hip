@@ -454,6 +454,7 @@ static hipError_t launch_planes(PlanesArgs g, PlanesArgs h, hipStream_t s) {
     cols[i] = std::max(blocks_of(p.x.cols, 64), p.rows ? blocks_of(p.row_chunks, 2) : 0);
     tiles[i] = std::max(blocks_of(p.x.rows, 64), p.cols ? blocks_of(p.col_chunks, 2) : 0) * cols[i];
   }
+  if (tiles[0] + tiles[1] == 0) return hipSuccess;   // no rows, and no padding of columns to write
   if (tiles[0] + tiles[1] > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(tiles[0] + tiles[1]));
   if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1]);
