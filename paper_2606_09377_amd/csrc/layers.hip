@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t g_cols, in
   __shared__ float tile[64][65];
   const bool is_g = blockIdx.x < g_tiles;   // uniform
   const int64_t at = is_g ? blockIdx.x : blockIdx.x - g_tiles, ct = is_g ? g_cols : h_cols, tr = at / ct;
-  planes_tile<P, BF>(is_g ? g : h, 0, tr, at - tr * ct, 1.f, tile);
+  planes_tile<P, BF>(is_g ? g : h, 0, tr, at - tr * ct, PlanesScale{{1.f, 1.f}, 1.f}, tile);
 }
 
 // out[c] = the sum of a column over the groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group

@@ -50,13 +50,20 @@ __global__ __launch_bounds__(256) void k_ns_norm(DevMat g, int vec, double *part
   __syncthreads();
   if (threadIdx.x == 0) part[blockIdx.y * NORM_PARTS + blockIdx.x] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
-// 1 / (norm + eps), by every wave
-__device__ __forceinline__ float ns_scale(const double *part, int batch, float eps) {
+// 1 / (norm + eps) = two[0] two[1] rest, by every wave: powers of two, whose product float32 may not hold (norms of finite
+// matrices lie in 2^-149 .. 2^144), and a rest in [1, 2).  Where it is no finite number above 0 it is the rest.
+struct NsScale {
+  float two[2], rest;
+};
+__device__ __forceinline__ NsScale ns_scale(const double *part, int batch, float eps) {
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < NORM_PARTS / 64; ++i) s += part[batch * NORM_PARTS + i * 64 + (threadIdx.x & 63)];
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  return (float)(1.0 / (sqrt(s) + (double)eps));
+  const double f = 1.0 / (sqrt(s) + (double)eps);
+  if (!(f > 0.0 && f <= 0x1p200)) return NsScale{{1.f, 1.f}, (float)f};
+  const int e = ilogb(f), e0 = min(max(e, -100), 100);
+  return NsScale{{ldexpf(1.f, e0), ldexpf(1.f, e - e0)}, (float)ldexp(f, -e)};
 }
 
 // X's parts from G, its rows' and its columns' (bf16 8192 x 8192, 403 MB with what it writes, in
@@ -66,16 +73,13 @@ template <bool BF>
 __global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps, float *scale) {
   constexpr int P0 = first_parts(BF);
   __shared__ float tile[64][65];
-  float sc = ns_scale(part, blockIdx.y, eps);
-  if constexpr (BF) {
-    const float two = __builtin_bit_cast(float, max(__builtin_bit_cast(uint32_t, sc) & 0x7f800000u, 0x00800000u));
-    if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = sc / two;
-    sc = two;
-  }
+  const NsScale sc = ns_scale(part, blockIdx.y, eps);
+  if (BF && blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = sc.rest;
   const int64_t tr = blockIdx.x / col_tiles, bytes = g.row_blocks * g.row_chunks * P0 * FRAG;   // of either
   g.rows += blockIdx.y * bytes;
   g.cols += blockIdx.y * bytes;
-  planes_tile<P0, BF>(g, (int64_t)blockIdx.y * g.x.stride, tr, blockIdx.x - tr * col_tiles, sc, tile);
+  planes_tile<P0, BF>(g, (int64_t)blockIdx.y * g.x.stride, tr, blockIdx.x - tr * col_tiles,
+                      PlanesScale{{sc.two[0], sc.two[1]}, BF ? 1.f : sc.rest}, tile);
 }
 
 enum NsMode : int32_t { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2, NS_OUT = 3 };

@@ -105,7 +105,7 @@ __device__ __forceinline__ void store_slot(uint8_t *planes, int64_t frag, int l,
 
 // Operands made from a matrix, its rows and its columns in one pass (either may be null): a workgroup takes 64 x 64 values, a
 // wave 16 rows of them as the fragments of its row block, the transposed ones from LDS.  Bound by memory.
-//   x      rows x cols of it, or only those where y > 0; times scale
+//   x      rows x cols of it, or only those where y > 0; times `scale`
 //   rows   operand of x's rows, row_chunks chunks of 32 columns
 //   cols   operand of x's columns, col_chunks chunks of 32 rows
 //   sums   [64-row group][cols]: column sums (null: none)
@@ -119,8 +119,12 @@ struct PlanesArgs {
   float *sums;
   int32_t grouped;   // rows: chunks in the order of 4-bit operands (NT_MIXED); row_chunks is a multiple of 4
 };
+// A factor that float32 may not hold: powers of two, applied first (exactly), and a rest
+struct PlanesScale {
+  float two[2], rest;
+};
 template <int P, bool BF>
-__device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, float scale, float (&tile)[64][65]) {
+__device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, PlanesScale scale, float (&tile)[64][65]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, oct = lane >> 4;
   const int64_t rb = tr * 4 + wave, row = rb * 16 + r;
   float v[2][8];
@@ -135,7 +139,7 @@ __device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, i
       for (int i = 0; i < 8; ++i) v[h][i] = m[i] > 0.f ? v[h][i] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[h][i] *= scale;
+    for (int i = 0; i < 8; ++i) v[h][i] = v[h][i] * scale.two[0] * scale.two[1] * scale.rest;
     const int64_t ch = tc * 2 + h;   // 32 columns
     if (g.rows && rb < g.row_blocks && ch < g.row_chunks) {
       if (g.grouped) store_slot<P>(g.rows, rb * g.row_chunks + (ch & ~(int64_t)3) + oct, (int)(ch & 3) * 16 + r, v[h]);

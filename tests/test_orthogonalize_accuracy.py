@@ -96,3 +96,33 @@ def test_update_is_held_in_float32(make, shape, bits, bf16_out, steps):
     far = outside(out.double().cpu().numpy(), want, bound, bf16_out)
     print(f"{make.__name__} {shape} {bits} bits, {steps} steps: {far:.3f} of the bound", flush=True)
     assert far <= 1
+
+
+def signs(m, n, scale, top):
+    """Whole numbers 1 .. top of either sign, times scale."""
+    rng = np.random.default_rng(m * n)
+    return rng.integers(1, top + 1, (m, n)) * rng.choice([-1.0, 1.0], (m, n)) * scale
+
+
+# norms beyond float32's range, and those whose reciprocal is: (matrix, bf16 g)
+RANGES = [((400, 500, 2.0 ** 121, 127), True), ((400, 500, 2.0 ** 121, 127), False), ((500, 400, 2.0 ** 116, 255), True),
+          ((64, 96, 2.0 ** -149, 1000), False), ((300, 200, 2.0 ** -149, 7), False), ((8, 12, 2.0 ** -133, 1), True)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("args,bf16_in", RANGES)
+def test_norms_at_the_ends_of_the_range(args, bf16_in):
+    """Finite matrices of any size and scale: the norm is taken out exactly."""
+    import torch
+    from paper_2606_09377_amd import Ctx
+    g = signs(*args)
+    t = torch.as_tensor(g, dtype=torch.float32).to(torch.bfloat16 if bf16_in else torch.float32)
+    assert np.array_equal(t.double().numpy(), g) and np.isfinite(g).all()
+    sizes = [np.linalg.norm(o64.orthogonalize(g, i, (A, B, C), 0.0)) for i in range(1, 5)]
+    want = o64.orthogonalize(g, 5, (A, B, C), 0.0)
+    bound = 2.0 ** -23 * sum(s * A ** (5 - i) for i, s in enumerate([1.0] + sizes))
+    t = t.cuda()
+    out = Ctx(0).orthogonalize(t, coefficients=(A, B, C), eps=0.0, out=torch.empty(t.shape, device="cuda"))
+    far = outside(out.double().cpu().numpy(), want, bound, False)
+    print(f"{args}: {far:.3f} of the bound", flush=True)
+    assert far <= 1
