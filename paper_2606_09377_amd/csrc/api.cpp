@@ -134,7 +134,7 @@ vcr_status ensure_ws(vcr_ctx *c, size_t bytes) {
   c->ws.base = static_cast<char *>(p);
   c->ws.cap = bytes;
   c->ws.used = 0;
-  c->peak_ws = std::max<uint64_t>(c->peak_ws, bytes);
+  c->peak_ws = std::max(c->peak_ws, held_workspace(c));
   // the A buffers' padding rows/columns are read by the GEMM: start from zeros
   HIP_TRY(c, launch_fill(reinterpret_cast<float *>(p), (int64_t)(bytes / 4), 0.f, c->stream));
   return VCR_OK;
@@ -389,7 +389,7 @@ void vcr_destroy(vcr_ctx *c) {
     if (!c->op_spaces.empty()) (void)hipDeviceSynchronize();   // calls on any stream may still use their room
     for (auto &o : c->op_spaces)
       if (o.w.base) (void)hipFree(o.w.base);
-    for (void *p : c->op_retired) (void)hipFree(p);
+    for (auto &w : c->op_retired) (void)hipFree(w.base);
     if (c->d_counters) (void)hipFree(c->d_counters);
     if (c->bab_buf) (void)hipFree(c->bab_buf);
     if (c->root_cache) (void)hipFree(c->root_cache);
@@ -1743,8 +1743,7 @@ vcr_status vcr_get_stats(vcr_ctx *c, vcr_stats *out) {
   out->ms_last_call = c->ms_last;
   out->gemm_flops_last_call = c->flops_last;
   out->peak_workspace_bytes = c->peak_ws;
-  out->workspace_bytes = c->ws.cap;
-  for (const auto &o : c->op_spaces) out->workspace_bytes += o.w.cap;
+  out->workspace_bytes = held_workspace(c);
   out->n_chunks_last_call = c->chunks_last;
   out->n_relu = (int32_t)c->relu_n.size();
   out->net_bytes = c->net_bytes;

@@ -83,7 +83,7 @@ struct vcr_ctx {
   Workspace ws;
   uint64_t peak_ws = 0;
   std::vector<vcr_internal::OpSpace> op_spaces;
-  std::vector<void *> op_retired;
+  std::vector<vcr_internal::Workspace> op_retired;   // held rooms that larger ones took the place of
   // split weight operands: what the loaded network would have split, and the one allocation that
   // holds them (null while there is none)
   std::vector<SplitItem> split_items;
@@ -197,6 +197,14 @@ T *take(vcr_ctx *c, size_t count) {
 }
 
 vcr_status ensure_ws(vcr_ctx *c, size_t bytes);
+
+// Device workspace the context holds: the bounds calls' and the layers' calls' on every stream
+inline uint64_t held_workspace(const vcr_ctx *c) {
+  uint64_t b = c->ws.cap;
+  for (const auto &o : c->op_spaces) b += o.w.cap;
+  for (const auto &w : c->op_retired) b += w.cap;
+  return b;
+}
 
 // The split copies of the dense operands of the loaded network (c->split_items; none are made for
 // other VCR_OPT_PRODUCTS than VCR_PRODUCTS_SPLIT).  They cost 6 bytes a weight and layout beside the

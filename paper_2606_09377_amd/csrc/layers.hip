@@ -494,7 +494,7 @@ vcr_status op_space(vcr_ctx *c, size_t bytes, Workspace **out) {
       return fail(c, VCR_ERR_STATE, "no workspace can be made while the stream is recorded: make the call once before");
     if (sp->w.base) {
       if (sp->held) {
-        c->op_retired.push_back(sp->w.base);   // a recorded graph uses it
+        c->op_retired.push_back(sp->w);   // a recorded graph uses it
       } else {
         HIP_TRY(c, hipStreamSynchronize(c->stream));
         (void)hipFree(sp->w.base);
@@ -508,9 +508,7 @@ vcr_status op_space(vcr_ctx *c, size_t bytes, Workspace **out) {
       return fail(c, VCR_ERR_OOM, "hipMalloc(%llu) failed: %s", (unsigned long long)bytes, hipGetErrorString(e));
     sp->w.base = static_cast<char *>(p);
     sp->w.cap = bytes;
-    uint64_t all = c->ws.cap;
-    for (auto &o : c->op_spaces) all += o.w.cap;
-    c->peak_ws = std::max<uint64_t>(c->peak_ws, all);
+    c->peak_ws = std::max(c->peak_ws, held_workspace(c));
   }
   sp->held |= capturing;
   return VCR_OK;

@@ -29,3 +29,40 @@ def test_gradients_of_no_rows(ctx, dtype, need):
         assert dx is None or dx.shape == (0, 40)
         assert dw is None or (dw.shape == (150, 40) and not dw.any())
         assert db is None or (db.shape == (150,) and not db.any())
+
+
+def test_statistics_count_every_workspace():
+    """The peak is at least what is held, and rooms kept for a recorded graph are held."""
+    import torch
+    from paper_2606_09377_amd import Ctx
+    from workloads import random_mlp
+    c = Ctx(0)
+
+    def held():
+        s = c.stats()
+        assert s["peak_workspace_bytes"] >= s["workspace_bytes"], s
+        return s["workspace_bytes"]
+    w = c.mx_quantize(torch.randn((640, 640), device="cuda"))
+    x = torch.randn((600, 640), device="cuda")
+    c.mx_linear(x, w)
+    room = held()
+    assert room > 0
+    wl = random_mlp(7, [40, 150, 130, 10], 3, 0.05)   # a bounds call that holds less than the layer call
+    c.load_net(wl.net)
+    c.crown_bounds(torch.from_numpy(wl.x0).cuda(), wl.eps, torch.from_numpy(wl.C).cuda())
+    both = held()
+    assert both > room
+    # a room that a graph was recorded with is kept beside the larger one that takes its place
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        c.mx_linear(x, w)
+    torch.cuda.synchronize()
+    one = held() - both
+    assert one > 0
+    with torch.cuda.graph(graph, stream=side):
+        c.mx_linear(x, w)
+    with torch.cuda.stream(side):
+        c.mx_linear(torch.randn((2000, 640), device="cuda"), w)
+    torch.cuda.synchronize()
+    assert held() >= both + 3 * one
