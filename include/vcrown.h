@@ -101,7 +101,8 @@ enum {
   VCR_OPT_CLIP_HI = 3,              /* default 1.0 */
   VCR_OPT_INTERSECT_IBP = 4,        /* 1 (default): intersect CROWN intermediate bounds with IBP */
   VCR_OPT_WORKSPACE_CAP_BYTES = 5,  /* device workspace cap; 0 (default) = no cap.  Inputs
-                                       (or domains) are processed in chunks that fit. */
+                                       (or domains) are processed in chunks that fit.  The calls on
+                                       layers (below) have the same cap once more for theirs. */
   VCR_OPT_SYNC_CHECK = 6,           /* 1: synchronise after each call and report device errors
                                        and invalid split domains as the call's status */
   VCR_OPT_TIME_GEMM = 7,            /* 1: bracket every backward-step GEMM launch (dense and
@@ -374,9 +375,11 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  * allowed where rows are a batch, and queues nothing (or zeros, for sums over the batch).  Outputs
  * must not overlap inputs unless stated.  These calls need no loaded network and leave it, its bounds
  * and the other calls' workspace alone; they keep one workspace for every stream they were given, which grows
- * as needed (VCR_ERR_OOM beyond VCR_OPT_WORKSPACE_CAP_BYTES) and is kept until vcr_destroy.  A call may be recorded into a HIP graph by the
- * caller once it has run with the same sizes on that stream (else VCR_ERR_STATE); the graph keeps that stream's
- * workspace, so its replays are to be ordered with each other and with the calls on that stream. */
+ * as needed and is kept until vcr_destroy.  VCR_OPT_WORKSPACE_CAP_BYTES holds for all of these workspaces together, apart
+ * from the bounds calls' own: under it a call that needs more room waits for the device and takes the place of those of other
+ * streams, and VCR_ERR_OOM is what does not fit even so.  A call may be recorded into a HIP graph by the
+ * caller once it has run with the same sizes on that stream, and while it has that workspace (else VCR_ERR_STATE); the graph keeps
+ * that stream's workspace, so its replays are to be ordered with each other and with the calls on that stream. */
 enum { VCR_F32 = 0, VCR_BF16 = 1 };
 
 /* Longest contraction of a product here (the shared dimension; for gradients also the rows of dy, for

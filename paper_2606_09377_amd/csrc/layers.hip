@@ -487,11 +487,26 @@ vcr_status op_space(vcr_ctx *c, size_t bytes, Workspace **out) {
   sp->w.used = 0;
   *out = &sp->w;
   if (sp->w.cap < bytes) {
-    if (c->ws_cap > 0 && bytes > c->ws_cap)
-      return fail(c, VCR_ERR_OOM, "the call needs %llu bytes of workspace, the cap is %llu", (unsigned long long)bytes,
-                  (unsigned long long)c->ws_cap);
+    // the cap is of all these rooms together: those that no recorded graph uses give way
+    uint64_t kept = 0, idle = 0;
+    for (auto &w : c->op_retired) kept += w.cap;
+    for (auto &o : c->op_spaces) {
+      if (o.held) kept += o.w.cap;
+      else if (&o != sp) idle += o.w.cap;   // (this stream's own is replaced)
+    }
+    if (c->ws_cap > 0 && bytes + kept > c->ws_cap)
+      return fail(c, VCR_ERR_OOM, "the call needs %llu bytes of workspace beside %llu that recorded graphs use, the cap is %llu",
+                  (unsigned long long)bytes, (unsigned long long)kept, (unsigned long long)c->ws_cap);
     if (capturing)
       return fail(c, VCR_ERR_STATE, "no workspace can be made while the stream is recorded: make the call once before");
+    if (c->ws_cap > 0 && bytes + kept + idle > c->ws_cap) {
+      HIP_TRY(c, hipDeviceSynchronize());   // (not by stream: the caller may have destroyed some)
+      for (auto &o : c->op_spaces)
+        if (&o != sp && !o.held && o.w.base) {
+          (void)hipFree(o.w.base);
+          o.w = Workspace{};
+        }
+    }
     if (sp->w.base) {
       if (sp->held) {
         c->op_retired.push_back(sp->w);   // a recorded graph uses it

@@ -66,3 +66,43 @@ def test_statistics_count_every_workspace():
         c.mx_linear(torch.randn((2000, 640), device="cuda"), w)
     torch.cuda.synchronize()
     assert held() >= both + 3 * one
+
+
+def test_cap_holds_over_all_streams():
+    """Rooms of other streams give way under the cap; those of recorded graphs stay."""
+    import torch
+    from paper_2606_09377_amd import Ctx, VcrError
+    from paper_2606_09377_amd.vcrown import OPT_WORKSPACE_CAP_BYTES, VCR_ERR_OOM
+    c = Ctx(0)
+    w = c.mx_quantize(torch.randn((640, 640), device="cuda"))
+    x = torch.randn((600, 640), device="cuda")
+    want = c.mx_linear(x, w)
+    torch.cuda.synchronize()
+    room = c.stats()["workspace_bytes"]
+    c.set_option(OPT_WORKSPACE_CAP_BYTES, room + room // 2)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for _ in range(2):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(c.mx_linear(x, w))
+            assert c.stats()["workspace_bytes"] <= room + room // 2
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[-1]):
+        y = c.mx_linear(x, w)
+    with pytest.raises(VcrError) as e:
+        with torch.cuda.stream(streams[0]):
+            c.mx_linear(x, w)
+    assert e.value.status == VCR_ERR_OOM
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+    c.set_option(OPT_WORKSPACE_CAP_BYTES, 0)
+    with torch.cuda.stream(streams[0]):
+        again = c.mx_linear(x, w)
+    torch.cuda.synchronize()
+    assert torch.equal(again, want) and c.stats()["workspace_bytes"] >= 2 * room
