@@ -33,12 +33,12 @@ __device__ __forceinline__ int64_t mx_scale_at(int64_t rb, int64_t group, int64_
 // float32, 304 MB, in 55 us, 5.5 TB/s, the rate of a large copy (67 to 78 us where the memory is still taking in the 268 MB
 // that a call before wrote: read back and quantised in turn, both take 124).
 template <bool BF>
-__global__ __launch_bounds__(256) void k_mx_quantize(DevMat x, int vec, uint8_t *codes, uint8_t *scales) {
+__global__ __launch_bounds__(256) void k_mx_quantize(DevMat x, int vec, uint8_t *codes, uint8_t *scales, int64_t first) {
   __shared__ uint32_t cs[4][4][16][4];   // [group][block][row][words]
   __shared__ uint8_t sb[16][16];         // [block of the 512 columns][row]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t groups = mx_groups(x.cols), n4 = (groups + 3) >> 2;
-  const int64_t rb = blockIdx.x / n4, c4 = blockIdx.x - rb * n4;
+  const int64_t at = first + blockIdx.x, rb = at / n4, c4 = at - rb * n4;
   const int64_t row0 = rb * 16 + wave * 4, col = c4 * 512 + lane * 8;
   float v[4][8];
   if (vec && row0 + 4 <= x.rows && c4 * 512 + 512 <= x.cols) {   // uniform: all loads at once
@@ -86,12 +86,12 @@ __device__ __forceinline__ void mx_block(const MxDev &w, int64_t rb, int64_t grp
 // The reverse, with the same division of work: 8192 x 8192 to float32 in 55 to 60 us, 5.1 to 5.5 TB/s (a thread per block, writing 32
 // values in 16-byte pieces of as many lines: 244 us).
 template <bool BF>
-__global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t ld, int vec) {
+__global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t ld, int vec, int64_t first) {
   __shared__ uint32_t cs[4][4][16][4];
   __shared__ float ss[16][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t groups = mx_groups(w.cols), n4 = (groups + 3) >> 2;
-  const int64_t rb = blockIdx.x / n4, c4 = blockIdx.x - rb * n4, grp = c4 * 4 + wave;
+  const int64_t at = first + blockIdx.x, rb = at / n4, c4 = at - rb * n4, grp = c4 * 4 + wave;
   if (grp < groups) {
     uint4 q;
     float s;
@@ -124,18 +124,20 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(MxDev w, void *y, int64_t
 // (a workgroup goes through the column tiles of 64 rows in the grid's order; the first g_tiles workgroups take g, the others,
 // if there are any, h)
 template <int P, bool BF>
-__global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t g_cols, int64_t g_tiles, PlanesArgs h, int64_t h_cols) {
+__global__ __launch_bounds__(256) void k_planes(PlanesArgs g, int64_t g_cols, int64_t g_tiles, PlanesArgs h, int64_t h_cols,
+                                               int64_t first) {
   __shared__ float tile[64][65];
-  const bool is_g = blockIdx.x < g_tiles;   // uniform
-  const int64_t at = is_g ? blockIdx.x : blockIdx.x - g_tiles, ct = is_g ? g_cols : h_cols, tr = at / ct;
+  const int64_t id = first + blockIdx.x;
+  const bool is_g = id < g_tiles;   // uniform
+  const int64_t at = is_g ? id : id - g_tiles, ct = is_g ? g_cols : h_cols, tr = at / ct;
   planes_tile<P, BF>(is_g ? g : h, 0, tr, at - tr * ct, PlanesScale{{1.f, 1.f}, 1.f}, tile);
 }
 
 // out[c] = the sum of a column over the groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
-__global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t groups, int64_t cols, float *out) {
+__global__ __launch_bounds__(256) void k_column_sums(const float *sums, int64_t groups, int64_t cols, float *out, int64_t first) {
   __shared__ float part[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t c = (first + blockIdx.x) * 64 + lane;
   float s = 0.f;
 #pragma unroll 8
   for (int64_t p = wave; p < groups; p += 4) s += c < cols ? sums[p * cols + c] : 0.f;
@@ -454,12 +456,11 @@ static hipError_t launch_planes(PlanesArgs g, PlanesArgs h, hipStream_t s) {
     cols[i] = std::max(blocks_of(p.x.cols, 64), p.rows ? blocks_of(p.row_chunks, 2) : 0);
     tiles[i] = std::max(blocks_of(p.x.rows, 64), p.cols ? blocks_of(p.col_chunks, 2) : 0) * cols[i];
   }
-  if (tiles[0] + tiles[1] == 0) return hipSuccess;   // no rows, and no padding of columns to write
-  if (tiles[0] + tiles[1] > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(tiles[0] + tiles[1]));
-  if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1]);
-  else hipLaunchKernelGGL((k_planes<3, false>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1]);
-  return hipGetLastError();
+  // (none of them: no rows, and no padding of columns to write)
+  return launch_stretches(tiles[0] + tiles[1], [&](int64_t first, dim3 grid) {
+    if (g.x.bf16) hipLaunchKernelGGL((k_planes<1, true>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1], first);
+    else hipLaunchKernelGGL((k_planes<3, false>), grid, dim3(256), 0, s, g, cols[0], tiles[0], h, cols[1], first);
+  });
 }
 
 }  // namespace vcr
@@ -607,9 +608,11 @@ vcr_status vcr_mx_quantize(vcr_ctx *c, const vcr_mat *x, const vcr_mx *q) {
   const DevMat d = dev(x);
   const int vec = rows_aligned(d.p, d.ld, d.bf16 ? 2 : 4);
   const int64_t wg = blocks_of(x->rows, 16) * blocks_of(mx_groups(x->cols), 4);
-  if (d.bf16) hipLaunchKernelGGL((k_mx_quantize<true>), dim3((unsigned)wg), dim3(256), 0, c->stream, d, vec, q->codes, q->scales);
-  else hipLaunchKernelGGL((k_mx_quantize<false>), dim3((unsigned)wg), dim3(256), 0, c->stream, d, vec, q->codes, q->scales);
-  HIP_TRY(c, hipGetLastError());
+  const hipError_t launched = launch_stretches(wg, [&](int64_t first, dim3 grid) {
+    if (d.bf16) hipLaunchKernelGGL((k_mx_quantize<true>), grid, dim3(256), 0, c->stream, d, vec, q->codes, q->scales, first);
+    else hipLaunchKernelGGL((k_mx_quantize<false>), grid, dim3(256), 0, c->stream, d, vec, q->codes, q->scales, first);
+  });
+  HIP_TRY(c, launched);
   return op_end(c);
 }
 
@@ -623,9 +626,11 @@ vcr_status vcr_mx_dequantize(vcr_ctx *c, const vcr_mx *q, const vcr_mat *y) {
   const OutMat o = out_mat(y, nullptr, 0);
   const int64_t wg = blocks_of(y->rows, 16) * blocks_of(mx_groups(y->cols), 4);
   const int vec = o.bf16 && rows_aligned(y->p, y->ld, 2) ? 2 : o.vec;   // 16-byte rows of bf16: 8 columns a store
-  if (o.bf16) hipLaunchKernelGGL((k_mx_dequantize<true>), dim3((unsigned)wg), dim3(256), 0, c->stream, dev(q), y->p, y->ld, vec);
-  else hipLaunchKernelGGL((k_mx_dequantize<false>), dim3((unsigned)wg), dim3(256), 0, c->stream, dev(q), y->p, y->ld, o.vec);
-  HIP_TRY(c, hipGetLastError());
+  const hipError_t launched = launch_stretches(wg, [&](int64_t first, dim3 grid) {
+    if (o.bf16) hipLaunchKernelGGL((k_mx_dequantize<true>), grid, dim3(256), 0, c->stream, dev(q), y->p, y->ld, vec, first);
+    else hipLaunchKernelGGL((k_mx_dequantize<false>), grid, dim3(256), 0, c->stream, dev(q), y->p, y->ld, o.vec, first);
+  });
+  HIP_TRY(c, launched);
   return op_end(c);
 }
 
@@ -777,8 +782,10 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
     HIP_TRY(c, launch_planes(pl, xl, s));
   }
   if (db) {
-    hipLaunchKernelGGL(k_column_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, M > 0 ? mg : 0, N, db);
-    HIP_TRY(c, hipGetLastError());
+    const hipError_t launched = launch_stretches(blocks_of(N, 64), [&](int64_t first, dim3 grid) {
+      hipLaunchKernelGGL(k_column_sums, grid, dim3(256), 0, s, sums, M > 0 ? mg : 0, N, db, first);
+    });
+    HIP_TRY(c, launched);
   }
   if (has_dx) {
     hipLaunchKernelGGL(k_mx_planes_t, dim3((unsigned)(nch * blocks_of(mx_groups(kx), 4))), dim3(256), 0, s, dev(w), nch, kxb, wt);

@@ -8,6 +8,18 @@ namespace vcr {
 
 inline int64_t blocks_of(int64_t n, int64_t b) { return (n + b - 1) / b; }
 
+// go(first, count) for stretches of `wgs` workgroups whose threads a launch can count (32 bits)
+template <class F>
+hipError_t launch_stretches(int64_t wgs, F &&go) {
+  constexpr int64_t MOST = 1 << 22;
+  for (int64_t first = 0; first < wgs; first += MOST) {
+    go(first, dim3((unsigned)std::min(MOST, wgs - first)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // A row-major matrix on the device: type 0 float32, 1 bf16 (VCR_F32, VCR_BF16)
 struct DevMat {
   const void *p;

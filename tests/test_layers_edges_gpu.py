@@ -106,3 +106,35 @@ def test_cap_holds_over_all_streams():
         again = c.mx_linear(x, w)
     torch.cuda.synchronize()
     assert torch.equal(again, want) and c.stats()["workspace_bytes"] >= 2 * room
+
+
+def test_more_rows_than_a_launch_has_threads_for(ctx):
+    """2^28 rows are 2^24 workgroups of 256: more threads than one launch counts."""
+    import torch
+    from oracle import layers64 as o64
+    rows, step = (1 << 28) + 72, 1 << 26   # a stretch of launches is 2^26 rows
+    g = torch.Generator("cuda").manual_seed(6)
+    x = torch.randn((rows, 3), generator=g, device="cuda")
+    q = ctx.mx_quantize(x)
+    y = torch.full((rows, 3), float("nan"), device="cuda")
+    ctx.mx_dequantize(q, out=y)
+    assert not bool(y.isnan().any())
+    for at in [0] + [i * step - 300 for i in range(1, 5)] + [rows - 500]:
+        part = slice(at, min(at + 600, rows))
+        want = o64.values(*o64.quantize(x[part].double().cpu().numpy()))
+        np.testing.assert_array_equal(y[part].double().cpu().numpy(), want)
+    del x, y, q
+    torch.cuda.empty_cache()
+
+
+def test_more_columns_than_a_launch_has_threads_for():
+    """The column sums of one row are that row, up to the largest one."""
+    import torch
+    from paper_2606_09377_amd import Ctx
+    ctx, n = Ctx(0), 1 << 30
+    dy = torch.randn((1, n), generator=torch.Generator("cuda").manual_seed(7), device="cuda")
+    db = ctx.mx_linear_grad(dy, None, None, need=(False, False, True))[2]
+    assert torch.equal(db, dy[0])
+    del dy, db
+    ctx.close()
+    torch.cuda.empty_cache()
