@@ -218,16 +218,17 @@ class MX:
         (rows, ceil(cols / 32)) in row order, as other programs store them."""
         import torch
         rows, groups = codes.shape[0], -(-cols // 128)
+        rb = -(-rows // 16)
         if tuple(codes.shape) != (rows, -(-cols // 2)) or tuple(scales.shape) != (rows, -(-cols // 32)):
             raise ValueError("codes are (rows, ceil(cols / 2)), scales (rows, ceil(cols / 32))")
         pad = torch.nn.functional.pad
         if cols % 2:
             codes = torch.cat((codes[:, :-1], codes[:, -1:] & 15), 1)
-        c = pad(codes, (0, 64 * groups - codes.shape[1], 0, -rows % 16)).view(-1, 16, groups, 4, 16)
+        c = pad(codes, (0, 64 * groups - codes.shape[1], 0, -rows % 16)).view(rb, 16, groups, 4, 16)
         n4 = -(-groups // 4)
-        s = pad(scales, (0, 16 * n4 - scales.shape[1], 0, -rows % 16)).view(-1, 16, n4, 4, 4)
-        return cls(c.permute(0, 2, 3, 1, 4).reshape(-1, groups, 64, 16).contiguous(),
-                   s.permute(0, 2, 4, 1, 3).reshape(-1, n4, 64, 4).contiguous(), rows, cols)
+        s = pad(scales, (0, 16 * n4 - scales.shape[1], 0, -rows % 16)).view(rb, 16, n4, 4, 4)
+        return cls(c.permute(0, 2, 3, 1, 4).reshape(rb, groups, 64, 16).contiguous(),
+                   s.permute(0, 2, 4, 1, 3).reshape(rb, n4, 64, 4).contiguous(), rows, cols)
 
     def unpack(self):
         """(codes, scales) in row order (the reverse of pack)."""

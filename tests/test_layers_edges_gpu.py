@@ -138,3 +138,22 @@ def test_more_columns_than_a_launch_has_threads_for():
     del dy, db
     ctx.close()
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 40), (1, 1), (17, 130)])
+def test_pack_and_unpack(ctx, rows, cols):
+    """Codes and scales in row order and back, no rows among them."""
+    import torch
+    from paper_2606_09377_amd import MX
+    codes = torch.randint(0, 256, (rows, -(-cols // 2)), dtype=torch.uint8, device="cuda")
+    if cols % 2:
+        codes[:, -1] &= 15
+    scales = torch.randint(100, 150, (rows, -(-cols // 32)), dtype=torch.uint8, device="cuda")
+    q = MX.pack(codes, scales, cols)
+    assert (q.rows, q.cols) == (rows, cols)
+    c, s = q.unpack()
+    assert torch.equal(c, codes) and torch.equal(s, scales)
+    x = torch.randn((3, cols), device="cuda")
+    assert ctx.mx_dequantize(q).shape == (rows, cols)
+    if rows:
+        assert ctx.mx_linear(x, q).shape == (3, rows)
