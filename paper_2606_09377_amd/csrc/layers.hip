@@ -222,28 +222,19 @@ __global__ __launch_bounds__(256) void k_join(const float *p, int parts, int64_t
 // ---- products by tiles ------------------------------------------------------------------------
 // (nt.h; in 4 bits 4096 x 8192 x 8192 in 156 us, 3.5 PFLOP/s; bf16 rows with 4-bit weights 256 x 8192 x 8192 in 38 us; the gradients
 // of 4096 x 8192 x 8192 in bf16 at 1.4 to 1.5 PFLOP/s, where a library product of that size reaches 1.35 to 1.55.)
-// Parts of the contraction: few tiles over a long contraction leave compute units idle.  Parts of 16 chunks and more are
-// then summed by their own workgroups (the smallest shape) and joined in order, where that pays for the second launch.
-template <int PA, int PB, int KIND>
-static int nt_parts(int64_t M, int64_t N, int64_t chunks) {
-  const NtShape *sh = NtTiles<PA, PB, KIND>::shapes, &x = sh[NT_SHAPES - 1];
-  const int64_t t = nt_tiles(M, N, x.bm, x.bn, false), parts = std::min<int64_t>(NT_CUS / t, chunks / 16);
-  if (parts < 2) return 1;
-  return nt_us(x, t * parts, (chunks + parts - 1) / parts, 4.f) + NT_LAUNCH_US < nt_plan(sh, M, N, chunks, 1, false, 4.f).us ? (int)parts : 1;
-}
 template <int PA, int PB, int KIND>
 static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
-  const int parts = nt_parts<PA, PB, KIND>(M, N, chunks);
+  const int parts = nt_parts<NtTiles<PA, PB, KIND>>(M, N, chunks);
   return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
 }
 // D = A B^T into o; part: room for part_bytes
 template <int PA, int PB, int KIND>
 static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipStream_t s) {
   typedef NtTiles<PA, PB, KIND> TS;
-  const int parts = nt_parts<PA, PB, KIND>(o.rows, o.cols, g.chunks);
+  const int parts = nt_parts<TS>(o.rows, o.cols, g.chunks);
   if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, o.bf16 ? 2.f : 4.f, EpiOut{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
-  const NtShape &x = TS::shapes[NT_SHAPES - 1];
+  const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
   const hipError_t e = launch_nt<typename TS::T4>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,
                                                   EpiPart{part, o.rows, ld}, s);
   if (e != hipSuccess) return e;

@@ -477,7 +477,7 @@ struct NtShape {
   int bm, bn;
   float us1, us2;   // us of a chunk of a workgroup alone on its compute unit, of two together (0: only one fits)
 };
-constexpr int NT_SHAPES = 5, NT_CUS = 256;
+constexpr int NT_CUS = 256;
 // of a launch, of a workgroup's start and end, and a compute unit's share of the memory's rate
 constexpr float NT_LAUNCH_US = 4.f, NT_ROUND_US = 2.f, NT_WRITE_BYTES_US = 20e3f;
 struct NtPlan {
@@ -499,9 +499,14 @@ inline float nt_us(const NtShape &s, int64_t tiles, int64_t chunks, float out_by
   const float one = s.us1 * (float)chunks + end, two = s.us2 * (float)chunks + end;
   return NT_LAUNCH_US + (s.us2 > 0.f ? (float)(n / 2) * two + (float)(n % 2) * one : (float)n * one);
 }
-inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri, float out_bytes) {
+// (TS: a class of products, with its `shapes`)
+template <class TS>
+constexpr int nt_shapes = sizeof(TS::shapes) / sizeof(NtShape);
+template <class TS>
+NtPlan nt_plan(int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri, float out_bytes) {
+  constexpr const NtShape *sh = TS::shapes;
   NtPlan best;
-  for (int a = 0; a < NT_SHAPES; ++a) {
+  for (int a = 0; a < nt_shapes<TS>; ++a) {
     const int64_t t = nt_tiles(M, N, sh[a].bm, sh[a].bn, tri) * batch;
     const float all = nt_us(sh[a], t, chunks, out_bytes);
     if (a == 0 || all < best.us) {
@@ -513,7 +518,7 @@ inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, i
     }
     const int64_t round = sh[a].us2 > 0.f ? 2 * NT_CUS : NT_CUS, full = t / round * round;
     if (full == 0 || full == t) continue;
-    for (int b = a + 1; b < NT_SHAPES; ++b) {
+    for (int b = a + 1; b < nt_shapes<TS>; ++b) {
       const int64_t subs = (int64_t)(sh[a].bm / sh[b].bm) * (sh[a].bn / sh[b].bn);
       const float us = nt_us(sh[a], full, chunks, out_bytes) + nt_us(sh[b], (t - full) * subs, chunks, out_bytes);
       if (us < best.us) {
@@ -526,6 +531,15 @@ inline NtPlan nt_plan(const NtShape *sh, int64_t M, int64_t N, int64_t chunks, i
     }
   }
   return best;
+}
+// Parts of the contraction: few tiles over a long contraction leave compute units idle.  Parts of 16 chunks and more are
+// then summed by their own workgroups (the smallest shape) and joined in order, where that pays for the second launch.
+template <class TS>
+int nt_parts(int64_t M, int64_t N, int64_t chunks) {
+  const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
+  const int64_t t = nt_tiles(M, N, x.bm, x.bn, false), parts = std::min<int64_t>(NT_CUS / t, chunks / 16);
+  if (parts < 2) return 1;
+  return nt_us(x, t * parts, (chunks + parts - 1) / parts, 4.f) + NT_LAUNCH_US < nt_plan<TS>(M, N, chunks, 1, false, 4.f).us ? (int)parts : 1;
 }
 
 // `count` tiles of shape (bm, bn) from `first` on, by kernels of shape T
@@ -555,7 +569,7 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
 // A product by the shapes of TS (T0 .. T4 and their `shapes`)
 template <class TS, class EPI>
 hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, float out_bytes, const EPI &epi, hipStream_t s) {
-  const NtPlan p = nt_plan(TS::shapes, M, N, g.chunks, batch, g.tri, out_bytes);
+  const NtPlan p = nt_plan<TS>(M, N, g.chunks, batch, g.tri, out_bytes);
   auto go = [&](int shape, int64_t first, int64_t count) {
     const int bm = TS::shapes[p.main].bm, bn = TS::shapes[p.main].bn;
     switch (shape) {
@@ -570,7 +584,8 @@ hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, 
   return e != hipSuccess || p.rest < 0 ? e : go(p.rest, p.main_tiles, p.rest_tiles);
 }
 
-// The shapes of products of PA and PB parts; their times were measured over 24 and 72 chunks of 256 and 512 tiles
+// The shapes of products of PA and PB parts; their times were measured over 24 and 72 chunks of 256 and 512 tiles.  T0 .. T3 and
+// T4, the last and smallest one again where a class has fewer.
 template <int PA, int PB, int KIND>
 struct NtTiles;
 template <>
@@ -580,7 +595,7 @@ struct NtTiles<1, 1, NT_FP4> {
   typedef NtTile<NT_FP4, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
   typedef NtTile<NT_FP4, 2, 2, 2, 2, 2, 1, 1, 4, 3> T3;
   typedef NtTile<NT_FP4, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .98f, 0.f}, {128, 128, .406f, .562f}, {64, 128, .235f, 0.f}, {64, 64, .113f, 0.f}, {32, 64, .084f, .167f}};
+  static constexpr NtShape shapes[] = {{256, 256, .98f, 0.f}, {128, 128, .406f, .562f}, {64, 128, .235f, 0.f}, {64, 64, .113f, 0.f}, {32, 64, .084f, .167f}};
 };
 template <>
 struct NtTiles<1, 1, NT_BF16> {
@@ -589,16 +604,17 @@ struct NtTiles<1, 1, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
   typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
   typedef NtTile<NT_BF16, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
+  static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
 template <>
 struct NtTiles<3, 1, NT_BF16> {
-  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 3, 1, 1, 3> T0;
-  typedef NtTile<NT_BF16, 2, 4, 2, 2, 1, 3, 1, 1, 4> T1;
-  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 1, 1, 4> T2;
-  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 1, 2, 4> T3;
-  typedef NtTile<NT_BF16, 2, 1, 1, 2, 2, 3, 1, 2, 4> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, .568f, 0.f}, {64, 128, .316f, .532f}, {64, 64, .197f, .366f}, {32, 64, .114f, .221f}, {32, 32, .078f, .157f}};
+  // (128 x 128 takes .568 us where two of 64 x 128 on a compute unit take .532)
+  typedef NtTile<NT_BF16, 2, 4, 2, 2, 1, 3, 1, 1, 4> T0;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 1, 1, 4> T1;
+  typedef NtTile<NT_BF16, 2, 2, 1, 2, 2, 3, 1, 2, 4> T2;
+  typedef NtTile<NT_BF16, 2, 1, 1, 2, 2, 3, 1, 2, 4> T3;
+  typedef T3 T4;
+  static constexpr NtShape shapes[] = {{64, 128, .316f, .532f}, {64, 64, .197f, .366f}, {32, 64, .114f, .221f}, {32, 32, .078f, .157f}};
 };
 template <>
 struct NtTiles<3, 3, NT_BF16> {
@@ -607,7 +623,7 @@ struct NtTiles<3, 3, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 3, 1, 3> T2;
   typedef NtTile<NT_BF16, 2, 1, 1, 4, 1, 3, 3, 1, 4> T3;
   typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 128, 1.f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
+  static constexpr NtShape shapes[] = {{128, 128, 1.f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
 };
 template <>
 struct NtTiles<1, 1, NT_MIXED> {
@@ -616,7 +632,7 @@ struct NtTiles<1, 1, NT_MIXED> {
   typedef NtTile<NT_MIXED, 4, 2, 1, 4, 1, 1, 1, 4, 3> T2;
   typedef NtTile<NT_MIXED, 4, 1, 1, 4, 1, 1, 1, 4, 3> T3;
   typedef NtTile<NT_MIXED, 2, 1, 1, 4, 1, 1, 1, 4, 4> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{128, 256, .366f, 0.f}, {64, 128, .126f, 0.f}, {64, 128, .148f, .234f}, {64, 64, .101f, .149f}, {32, 64, .078f, .107f}};
+  static constexpr NtShape shapes[] = {{128, 256, .366f, 0.f}, {64, 128, .126f, 0.f}, {64, 128, .148f, .234f}, {64, 64, .101f, .149f}, {32, 64, .078f, .107f}};
 };
 template <>
 struct NtTiles<3, 1, NT_MIXED> {
@@ -625,7 +641,7 @@ struct NtTiles<3, 1, NT_MIXED> {
   typedef NtTile<NT_MIXED, 2, 2, 1, 4, 1, 3, 1, 4, 2> T2;
   typedef NtTile<NT_MIXED, 2, 4, 1, 1, 4, 3, 1, 4, 2> T3;
   typedef NtTile<NT_MIXED, 2, 2, 1, 1, 4, 3, 1, 4, 3> T4;
-  static constexpr NtShape shapes[NT_SHAPES] = {{64, 256, .49f, 0.f}, {64, 128, .291f, 0.f}, {32, 128, .18f, .305f}, {32, 64, .115f, .174f}, {32, 32, .093f, .147f}};
+  static constexpr NtShape shapes[] = {{64, 256, .49f, 0.f}, {64, 128, .291f, 0.f}, {32, 128, .18f, .305f}, {32, 64, .115f, .174f}, {32, 32, .093f, .147f}};
 };
 
 }  // namespace vcr
