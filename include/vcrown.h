@@ -368,7 +368,7 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  * microscaled 4-bit floating point.  These calls make such weights, multiply by them, give the
  * gradients through them, and read them back, so that the bounds above are taken of the network as it
  * is deployed (load the values of vcr_mx_dequantize); and they orthogonalise the update of a layer's
- * weights, which keeps the spectral norms that bounds grow by in check.
+ * weights, so that a step of length r moves the layer's spectral norm by at most about 1.2 r.
  *
  * Matrices are given by vcr_mat: float32 or bf16, row-major, rows `ld` elements apart (>= cols), aligned to
  * their element type (calls are faster where p and the rows are 16-byte aligned).  A matrix of no rows is
@@ -379,7 +379,8 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  * from the bounds calls' own: under it a call that needs more room waits for the device and takes the place of those of other
  * streams, and VCR_ERR_OOM is what does not fit even so.  A call may be recorded into a HIP graph by the
  * caller once it has run with the same sizes on that stream, and while it has that workspace (else VCR_ERR_STATE); the graph keeps
- * that stream's workspace, so its replays are to be ordered with each other and with the calls on that stream. */
+ * that stream's workspace, so its replays are to be ordered with each other and with the calls on that stream.  Destroy a stream only when its work is done: the
+ * next one of the same handle takes over its workspace. */
 enum { VCR_F32 = 0, VCR_BF16 = 1 };
 
 /* Longest contraction of a product here (the shared dimension; for gradients also the rows of dy, for
@@ -423,7 +424,8 @@ vcr_status vcr_mx_product(vcr_ctx *ctx, const vcr_mx *a, const vcr_mx *w, const 
 
 /* y = act(x w^T + bias) with x (rows, k) as it is: the layer whose weights are the 4-bit ones, which
  * is the one a verified network has.  float32 x is multiplied as three bf16 values, exactly but for what of x
- * is below 2^-133 (as under "Arithmetic"), bf16 x exactly; sums are float32, their order depends on the sizes. */
+ * is below 2^-133 (as under "Arithmetic"), bf16 x exactly; sums are float32, their order depends on the sizes.  Weights
+ * above 2^127 1.5 count as infinite here and in dx, as they are read back (vcr_mx_product takes them as they are). */
 vcr_status vcr_mx_linear(vcr_ctx *ctx, const vcr_mat *x, const vcr_mx *w, const float *bias, int32_t relu,
                          const vcr_mat *y);
 
@@ -438,7 +440,7 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *ctx, const vcr_mat *dy, const vcr_mat *y,
 /* Newton-Schulz orthogonalisation: X = g / (|g|_F + eps), then `steps` times, with A = X X^T (X^T X for more
  * rows than columns), X <- (a I + b A + c A A) X (from the right); out = gain X, or keep base + gain X.  With a =
  * 3.4445, b = -4.7750, c = 2.0315 five steps bring singular values above about 2^-9 of the norm
- * into [0.7, 1.2].  X and the products are held to float32's accuracy, whatever the types. */
+ * into [0.68, 1.21], and none beyond.  X and the products are held to float32's accuracy, whatever the types. */
 typedef struct {
   int32_t steps;            /* in [1, 100] */
   float a, b, c;

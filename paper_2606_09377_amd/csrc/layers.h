@@ -4,7 +4,8 @@
 #include "ctx.h"
 
 // The context's room for a call on its current stream, at least so many bytes (nothing in it is
-// kept from call to call).  Each stream has its own, so that calls on two streams share no memory.
+// kept from call to call).  Each stream has its own, so that calls on two streams share no memory; under the
+// workspace cap, which is theirs together, idle ones of other streams are freed for it.
 vcr_status op_space(vcr_ctx *c, size_t bytes, vcr_internal::Workspace **out);
 // Before the first and after the last launch of a call
 vcr_status op_begin(vcr_ctx *c);

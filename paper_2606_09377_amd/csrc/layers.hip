@@ -398,7 +398,15 @@ struct RowsPlan {
 // bf16: 16.4 us for 8 rows here, 19.1 for 9 and 19.7 for 17 by tiles, where 16 rows took 27.8 here).
 inline bool few_rows(int X, int64_t M) { return M <= (X == X4 ? 16 : X == XBF ? 8 : 5); }
 // A workgroup of 8 waves per compute unit or more; the contraction is divided among workgroups only where there are too
-// few row blocks for that and every wave keeps 4 groups.
+// few row blocks for that and every wave keeps 4 groups.  More row blocks a workgroup share the rows' staging and reads, fewer
+// leave more workgroups.  One, two and four, us a call at 8192 columns of x, the weights not in the caches:
+//   row blocks          256               512              1024              4096            16384
+//   bf16, 1 row     8.4 10.6 13.1    14.9 12.7 17.6   27.4 23.0 22.5   66.6 68.3 66.3    218 204 196
+//   bf16, 8 rows   14.1 13.6 15.4    25.9 18.6 20.4   48.7 34.6 28.4    179  128 96.6    674 496 349
+//   float32, 1 row  9.6 11.0 13.7    16.8 13.6 18.2   31.0 24.6 23.4   71.8 72.2 69.5    232 210 199
+//   4 bits, 1 row   6.9  8.8 10.8    11.6  9.5 15.2   20.7 16.5 19.3   60.0 52.8 60.4    222 182 190
+// The two borders are for all of them together, and for counts that fill the compute units: 4-bit rows of 4096 and more row blocks would be
+// 5 to 15% faster with two, 8 rows of 1024 20% faster with four, and 384 row blocks (one bf16 row, 13.8) 20% with two.
 static RowsPlan rows_plan(int X, int64_t M, int64_t N, int64_t groups) {
   RowsPlan p{};
   const int64_t blocks = blocks_of(N, 16);

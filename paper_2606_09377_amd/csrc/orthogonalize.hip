@@ -14,8 +14,8 @@
 //
 // A bf16 update is exact in one part, times a power of two: the first step multiplies one part where the later ones take three.
 //
-// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 44.0 ms: 60 TFLOP of partial products
-// at 1.36 PFLOP/s), by the operands the epilogues write and the tiles' last rounds at 1024 (five float32 1024 x 1024 in 0.75 ms: a
+// Bound by the matrix instructions where the update is large (8192 x 8192, bf16, five steps in 44 to 45 ms: 60 TFLOP of partial
+// products at 1.33 to 1.36 PFLOP/s), by the operands the epilogues write and the tiles' last rounds at 1024 (five float32 1024 x 1024 in 0.75 ms: a
 // step's three launches take 43, 46 and 62 us, of which 12 write X twice), and by the starts and ends of fifteen launches of 12
 // to 21 us on 777 x 1500.
 #include <algorithm>
@@ -67,7 +67,7 @@ __device__ __forceinline__ NsScale ns_scale(const double *part, int batch, float
 }
 
 // X's parts from G, its rows' and its columns' (bf16 8192 x 8192, 403 MB with what it writes, in
-// 93 us).  A bf16 G as it is, times the power of two that brings its norm near 1: exact in one part, so that the first step
+// 95 to 104 us).  A bf16 G as it is, times the power of two that brings its norm near 1: exact in one part, so that the first step
 // multiplies one part; the rest of the factor is left to its epilogues (scale[batch]).
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ns_planes(PlanesArgs g, int64_t col_tiles, const double *part, float eps, float *scale) {
