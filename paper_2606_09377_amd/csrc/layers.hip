@@ -729,6 +729,7 @@ vcr_status vcr_mx_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *y, c
   if (y && y->type != dy->type) return fail(c, VCR_ERR_ARG, "y and dy differ in type");
   if (dx && (w->rows != N || dx->rows != M || dx->cols != w->cols)) return fail(c, VCR_ERR_SHAPE, "dx is not dy times w");
   if (dw && (x->rows != M || dw->rows != N || dw->cols != x->cols)) return fail(c, VCR_ERR_SHAPE, "dw is not the transpose of dy times x");
+  if (dx && dw && x->cols != w->cols) return fail(c, VCR_ERR_SHAPE, "x and w differ in columns");
   if (dw && x->type != dy->type) return fail(c, VCR_ERR_ARG, "x and dy differ in type");
   if (dx) TRY(check_contraction(c, N));
   if (dw) TRY(check_contraction(c, M));

@@ -126,3 +126,19 @@ def test_oracle_orthogonalize():
     s = np.linalg.svd(o64.orthogonalize(g), compute_uv=False)
     assert 0.6 < s.min() and s.max() < 1.3
     np.testing.assert_allclose(o64.orthogonalize(g.T), o64.orthogonalize(g).T, atol=1e-12)
+
+
+def test_gradients_of_one_layer(vc):
+    """x and w of different widths are not one layer's."""
+    ctx = vc.Ctx(-1)
+    keep = _buf()
+    p, ref = keep.ctypes.data, ctypes.byref
+
+    def mat(rows, cols):
+        return vc.VcrMat(p, 0, rows, cols, cols)
+
+    def grad(x, w):
+        return ctx.lib.vcr_mx_linear_grad(ctx.h, ref(mat(3, 7)), None, ref(mat(3, x)), ref(vc.VcrMx(p, p, 7, w)), ref(mat(3, w)),
+                                          ref(mat(7, x)), p)
+    assert grad(40, 40) == vc.VCR_ERR_STATE
+    assert grad(41, 40) == vc.VCR_ERR_SHAPE and b"w" in ctx.lib.vcr_last_error(ctx.h)
