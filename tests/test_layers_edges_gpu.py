@@ -157,3 +157,36 @@ def test_pack_and_unpack(ctx, rows, cols):
     assert ctx.mx_dequantize(q).shape == (rows, cols)
     if rows:
         assert ctx.mx_linear(x, q).shape == (3, rows)
+
+
+@pytest.mark.parametrize("m", [1, 3, 40, 300])
+@pytest.mark.parametrize("byte", [0, 1, 2, 252, 253, 254])
+def test_scales_at_the_ends(ctx, byte, m):
+    """The smallest and largest scales.  Operands are small whole numbers times powers of two: every sum is exact."""
+    import torch
+    from oracle import layers64 as o64
+    from paper_2606_09377_amd import MX
+    rng = np.random.default_rng(byte)
+    k, n = 200, 50
+    codes = rng.integers(0, 16, (n, k)).astype(np.uint8)
+    codes[:8] &= 11   # some rows without values of 4 and 6 (and 2 and 3)
+    scales = np.full((n, -(-k // 32)), byte, np.uint8)
+    w = MX.pack(torch.as_tensor(codes[:, ::2] | codes[:, 1::2] << 4).cuda(), torch.as_tensor(scales).cuda(), k)
+    wv = o64.values(codes, scales)
+    other = 2.0 ** np.clip(127 - byte, -120, 120)
+    x = rng.integers(1, 9, (m, k)) * other
+    dy = rng.integers(1, 9, (m, n)) * other
+    inf = np.abs(wv) >= 2.0 ** 128   # as bf16 or float32 values, though not as 4-bit ones
+    for dt in (torch.float32, torch.bfloat16):
+        t, g = torch.as_tensor(x, dtype=dt).cuda(), torch.as_tensor(dy, dtype=dt).cuda()
+        y = ctx.mx_linear(t, w, out=torch.empty((m, n), device="cuda")).double().cpu().numpy()
+        ok = ~inf.any(1)
+        np.testing.assert_array_equal(y[:, ok], (x @ wv.T)[:, ok])
+        assert not np.isfinite(y[:, ~ok]).any() and ok.any()
+        dx = ctx.mx_linear_grad(g.float(), None, w, need=(True, False, False))[0].double().cpu().numpy()
+        ok = ~inf.any(0)
+        np.testing.assert_array_equal(dx[:, ok], (dy @ wv)[:, ok])
+        assert not np.isfinite(dx[:, ~ok]).any()
+        q = ctx.mx_quantize(t)
+        p = ctx.mx_product(q, w).double().cpu().numpy()
+        np.testing.assert_array_equal(p, ctx.mx_dequantize(q).double().cpu().numpy() @ wv.T)
