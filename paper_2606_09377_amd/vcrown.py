@@ -297,11 +297,11 @@ class Ctx:
         self._check(self.lib.vcr_set_option(self.h, key, float(value)))
 
     def set_stream(self, stream=None):
-        """Queue work on a torch stream (default: torch's current stream)."""
+        """Queue work on a torch stream (default: torch's current stream on the context's device)."""
         import torch
-        s = torch.cuda.current_stream() if stream is None else stream
-        self._raw_stream = s.cuda_stream
+        s = torch.cuda.current_stream(self.device if self.device >= 0 else None) if stream is None else stream
         self._check(self.lib.vcr_set_stream(self.h, ctypes.c_void_p(s.cuda_stream)))
+        self._raw_stream = s.cuda_stream
 
     def load_net(self, net):
         arr, keep, chw = _net_nodes(net)

@@ -142,3 +142,22 @@ def test_gradients_of_one_layer(vc):
                                           ref(mat(7, x)), p)
     assert grad(40, 40) == vc.VCR_ERR_STATE
     assert grad(41, 40) == vc.VCR_ERR_SHAPE and b"w" in ctx.lib.vcr_last_error(ctx.h)
+
+
+def test_calls_follow_the_stream_of_their_own_device(vc, monkeypatch):
+    """Where torch's current device is another one than the context's, the context's device's current stream is taken."""
+    import types
+    import torch
+    current = {0: 0x1000, 1: 0x2000}   # device: handle of its current stream
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: current[d], raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: types.SimpleNamespace(cuda_stream=current[1 if d is None else d]))
+    given = []
+    ctx = vc.Ctx.__new__(vc.Ctx)
+    ctx.h, ctx.device, ctx._raw_stream = None, 0, 0   # (no library handle: nothing to destroy)
+    ctx.lib = types.SimpleNamespace(vcr_set_stream=lambda h, s: given.append(s.value) or 0)
+    ctx._current_stream()
+    ctx._current_stream()
+    ctx._stream_sync()
+    current[0] = 0x3000
+    ctx._current_stream()
+    assert given == [0x1000, 0x1000, 0x3000]
