@@ -372,7 +372,8 @@ vcr_status vcr_workspace_bytes(vcr_ctx *ctx, int32_t B, int32_t m, int32_t n_dom
  *
  * Matrices are given by vcr_mat: float32 or bf16, row-major, rows `ld` elements apart (>= cols), aligned to
  * their element type (calls are faster where p and the rows are 16-byte aligned).  A matrix of no rows is
- * allowed where rows are a batch, and queues nothing (or zeros, for sums over the batch).  Outputs
+ * allowed where rows are a batch, and queues nothing (or zeros, for sums over the batch).  More rows or columns than
+ * VCR_MAX_NODE_ELEMENTS, and 4-bit matrices and updates of more than VCR_MAX_LAYER_WEIGHTS values, are VCR_ERR_SHAPE.  Outputs
  * must not overlap inputs unless stated.  These calls need no loaded network and leave it, its bounds
  * and the other calls' workspace alone; they keep one workspace for every stream they were given, which grows
  * as needed and is kept until vcr_destroy.  VCR_OPT_WORKSPACE_CAP_BYTES holds for all of these workspaces together, apart
