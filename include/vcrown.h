@@ -455,6 +455,75 @@ typedef struct {
 vcr_status vcr_orthogonalize(vcr_ctx *ctx, const vcr_mat *g, int32_t count, int64_t g_stride, const vcr_ns_opts *opts,
                              const vcr_mat *base, int64_t base_stride, const vcr_mat *out, int64_t out_stride);
 
+/* ---- Layers in float, dropout and the loss ------------------------------------------------------
+ * The same layers before they are stored, with what training puts around them.  Matrices, workspaces, recording
+ * and errors are as above; matrices given together may differ in type unless stated. */
+
+/* Dropout.  The value in column c of row r is kept where the 16 random bits of that place are at least k = round(65536 p)
+ * and multiplied by 65536 / (65536 - k), else it is 0 (also where it is infinite or NaN).  So p counts in steps of 2^-16, and kept
+ * values make up for those dropped exactly.  The bits are half h = c % 8 (the low half of word h / 2 where h is even) of the Philox
+ * 4x32-10 output (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) for the counter (c / 8, r, low word of o, high
+ * word of o) and the key (low word, high word of seed), with o = offset + *step modulo 2^64.  Equal seed and o give equal
+ * masks, in every call that takes a vcr_drop and whatever the types and pitches: nothing is stored for the gradient.
+ * A call that makes its own mask takes an o of its own. */
+typedef struct {
+  float p;                  /* in [0, 1), with k < 65536; 0: nothing is dropped */
+  uint64_t seed, offset;
+  const uint64_t *step;     /* device, 8-byte aligned, or NULL (0): read when the call's work runs, so that replays of a recorded
+                               call take a new mask where the program counts it up */
+} vcr_drop;
+
+/* y = D(x) + residual (NULL: none), all of one shape; y may be x or residual itself.  The gradient by x is D(dy). */
+vcr_status vcr_dropout(vcr_ctx *ctx, const vcr_mat *x, const vcr_drop *drop, const vcr_mat *residual, const vcr_mat *y);
+
+/* Activations: z; max(z, 0); z Phi(z), Phi the normal distribution's; z / (1 + exp(-z)). */
+enum { VCR_ACT_NONE = 0, VCR_ACT_RELU = 1, VCR_ACT_GELU = 2, VCR_ACT_SILU = 3 };
+
+typedef struct {
+  const float *bias;        /* device (n), or NULL */
+  int32_t act;              /* VCR_ACT_* */
+  const vcr_drop *drop;     /* or NULL */
+  const vcr_mat *residual;  /* (rows, n), or NULL */
+  const vcr_mat *z;         /* (rows, n), or NULL */
+} vcr_linear_opts;
+
+/* Most rows of x and of w (VCR_ERR_UNSUPPORTED beyond; contractions as above) */
+#define VCR_MAX_LINEAR_ROWS ((int64_t)1 << 24)
+
+/* z = x w^T + bias, y = D(act(z)) + residual, x (rows, k) and w (n, k) of one type, y (rows, n); z is written where it is
+ * given.  opts may be NULL (y = x w^T); y may be the residual itself.  bf16 products are exact, float32 ones as under
+ * "Arithmetic"; sums are float32, in an order that depends on the sizes, and each output is rounded once to its type. */
+vcr_status vcr_linear(vcr_ctx *ctx, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts *opts, const vcr_mat *y);
+
+/* Gradients of vcr_linear from dy (rows, n): with g = D(dy) act'(z) (act'(0) = 0 for VCR_ACT_RELU),
+ *   dx (rows, k) = g w + add,   dw (n, k) = g^T x,   db (n) = sum of g over the rows, float32.
+ * Of opts, act and drop are those of the call, and z its z (VCR_ACT_RELU needs only its sign: without a residual that is
+ * y's); the rest is not read, and z is not without an activation.  dy, x and w are of one type.  The gradient by the residual is
+ * dy itself; add (rows, k), or NULL, is where another path's gradient by x joins, and may be dx itself.  With bf16 operands g is rounded to
+ * bf16 for the products (exact but for VCR_ACT_GELU and VCR_ACT_SILU: dropout's factor multiplies their sums).
+ * Outputs may be NULL; x is needed for dw, w for dx.  No rows: dw and db are zero. */
+vcr_status vcr_linear_grad(vcr_ctx *ctx, const vcr_mat *dy, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts *opts,
+                           const vcr_mat *add, const vcr_mat *dx, const vcr_mat *dw, float *db);
+
+typedef struct {
+  float smoothing;          /* s in [0, 1] */
+  float lse2;               /* c >= 0, finite */
+  int32_t mean;             /* divide by the number of rows counted (0: do not) */
+  float scale;              /* factor of dlogits, finite */
+} vcr_loss_opts;
+
+/* Cross entropy of logits x (rows, n) with one label a row (int64, device, 8-byte aligned).  With e = log sum_j exp(x_j),
+ *   loss[r] = e - (1 - s) x_t - s mean_j x_j + c e^2,
+ *   dlogits[r][j] = scale / N ((1 + 2 c e) exp(x_j - e) - (1 - s) [j = t] - s / n),
+ *   total = sum_r loss[r] / N,
+ * N the number of rows with a label of 0 or more (1 if there is none) with `mean`, else 1.  A row with a negative label does not
+ * count: its loss and dlogits are 0, and its logits are not read.  One with a label of n or more has a loss and dlogits of NaN.  Logits of
+ * -infinity have probability 0 (and make the loss infinite with smoothing); a row of nothing else, or with +infinity or
+ * NaN, gives NaN.  loss (rows), total (1) and dlogits may be NULL; dlogits may be logits itself.  Statistics are float32; sums are taken
+ * in a fixed order. */
+vcr_status vcr_cross_entropy(vcr_ctx *ctx, const vcr_mat *logits, const int64_t *label, const vcr_loss_opts *opts, float *loss,
+                             float *total, const vcr_mat *dlogits);
+
 /* Statistics; synchronises the stream. */
 vcr_status vcr_get_stats(vcr_ctx *ctx, vcr_stats *out);
 

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libvcrown.so")
 SOURCES = ["gemm.hip", "elementwise.hip", "conv.hip", "alpha.hip", "noalloc.hip", "layers.hip", "orthogonalize.hip",
-           "api.cpp", "graph.cpp"]
+           "dense.hip", "dropout.hip", "loss.hip", "api.cpp", "graph.cpp"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,293 @@
+// Layers in float: the product with its bias, activation, dropout and residual, and its gradients.  vcr_linear and
+// vcr_linear_grad of vcrown.h.
+//
+//   z = x w^T + b,  y = D(act(z)) + residual;   g = D(dy) act'(z),  dx = g w + add,  dw = g^T x,  db = sum g.
+//
+// All three products contract the contiguous axes of operands in the layout of nt.h: bf16 values in one part, float32 ones in three
+// (their six partial products keep float32's accuracy).  Dropout's factor is left out of g and multiplies the sums, so that
+// a bf16 g is dy itself or zero where the activation's slope is.
+#include <algorithm>
+
+#include "products.h"
+#include "training.h"
+
+namespace vcr {
+
+// ---- where results go -------------------------------------------------------------------------
+struct DenseOut {
+  static constexpr bool STAGED = true;
+  MatRef y, z, res;
+  const float *bias;   // or null
+  int64_t rows, cols;
+  int32_t act;
+  float factor;        // of the sums
+  DropDev drop;
+  float bytes() const { return (y.bf16 ? 2.f : 4.f) + (z.p ? z.bf16 ? 2.f : 4.f : 0.f) + (res.p ? res.bf16 ? 2.f : 4.f : 0.f); }
+  __device__ __forceinline__ void store8(int64_t m, int64_t n, float (&v)[8]) const {
+    if (m >= rows || n >= cols) return;
+    if (factor != 1.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= factor;
+    }
+    if (bias) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += n + i < cols ? bias[n + i] : 0.f;
+    }
+    if (z.p) save8(z, m, n, cols, v);
+    if (act != VCR_ACT_NONE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = act_value(act, v[i]);
+    }
+    if (drop.k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= drop.factor;
+      drop8(drop, drop_offset(drop), m, n, v);
+    }
+    if (res.p) {
+      float a[8];
+      load8(res, m, n, cols, a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += a[i];
+    }
+    save8(y, m, n, cols, v);
+  }
+};
+
+// ---- operands ---------------------------------------------------------------------------------
+// Up to three matrices of one type laid out in a launch, 64 x 64 values a workgroup; the first one may be a gradient, whose
+// values are those kept by dropout times the activation's slope.
+struct GradSource {
+  MatRef z;
+  int32_t act;
+  DropDev drop;
+};
+struct PlanesOf {
+  PlanesArgs p;
+  int64_t col_tiles, tiles;
+};
+template <int P, bool BF>
+__global__ __launch_bounds__(256) void k_dense_planes(PlanesOf a, PlanesOf b, PlanesOf c, GradSource src, int64_t first) {
+  __shared__ float tile[64][65];
+  int64_t id = first + blockIdx.x;
+  const bool is_a = id < a.tiles, is_b = !is_a && id < a.tiles + b.tiles;   // uniform
+  id -= is_a ? 0 : is_b ? a.tiles : a.tiles + b.tiles;
+  const PlanesArgs &p = is_a ? a.p : is_b ? b.p : c.p;
+  const int64_t ct = is_a ? a.col_tiles : is_b ? b.col_tiles : c.col_tiles, tr = id / ct, tc = id - tr * ct;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (tr * 4 + wave) * 16 + (lane & 15);
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t col = tc * 64 + h * 32 + (lane >> 4) * 8;
+    mat_row8<BF>(p.x, 0, row, col, p.vec, v[h]);
+    if (is_a && row < p.x.rows && col < p.x.cols) {
+      if (src.act != VCR_ACT_NONE) {
+        float z[8];
+        load8(src.z, row, col, p.x.cols, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[h][i] = src.act == VCR_ACT_RELU ? (z[i] > 0.f ? v[h][i] : 0.f) : v[h][i] * act_slope(src.act, z[i]);
+      }
+      if (src.drop.k) drop8(src.drop, drop_offset(src.drop), row, col, v[h]);
+    }
+    planes_rows<P>(p, tr, tc, h, v[h]);
+  }
+  planes_cols<P>(p, tr, tc, v, tile);
+}
+static PlanesOf planes_of(const PlanesArgs *p) {
+  PlanesOf o{};
+  if (!p) return o;
+  o.p = *p;
+  o.p.vec = rows_aligned(p->x.p, p->x.ld, p->x.bf16 ? 2 : 4);
+  // tiles of 64 rows and columns, those of the padding among them
+  o.col_tiles = std::max(blocks_of(p->x.cols, 64), p->rows ? blocks_of(p->row_chunks, 2) : 0);
+  o.tiles = std::max(blocks_of(p->x.rows, 64), p->cols ? blocks_of(p->col_chunks, 2) : 0) * o.col_tiles;
+  return o;
+}
+static hipError_t launch_dense_planes(const PlanesArgs *a, const PlanesArgs *b, const PlanesArgs *c, const GradSource &src, bool bf16, hipStream_t s) {
+  const PlanesOf pa = planes_of(a), pb = planes_of(b), pc = planes_of(c);
+  return launch_stretches(pa.tiles + pb.tiles + pc.tiles, [&](int64_t first, dim3 grid) {
+    if (bf16) hipLaunchKernelGGL((k_dense_planes<1, true>), grid, dim3(256), 0, s, pa, pb, pc, src, first);
+    else hipLaunchKernelGGL((k_dense_planes<3, false>), grid, dim3(256), 0, s, pa, pb, pc, src, first);
+  });
+}
+
+// db = factor times the sums of the columns' groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
+__global__ __launch_bounds__(256) void k_dense_sums(const float *sums, int64_t groups, int64_t cols, float factor, float *out) {
+  __shared__ float part[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  float s = 0.f;
+#pragma unroll 8
+  for (int64_t p = wave; p < groups; p += 4) s += c < cols ? sums[p * cols + c] : 0.f;
+  part[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < cols) out[c] = factor * ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+}
+
+static DevMat dev(const vcr_mat *m) { return DevMat{m->p, m->type == VCR_BF16, m->rows, m->cols, m->ld, 0}; }
+static size_t room(bool bf16, int64_t M, int64_t N, int64_t chunks) {
+  return bf16 ? part_bytes<1, 1, NT_BF16>(M, N, chunks) : part_bytes<3, 3, NT_BF16>(M, N, chunks);
+}
+static hipError_t product(bool bf16, const uint8_t *a, int64_t arb, const uint8_t *b, int64_t brb, int64_t chunks, const DenseOut &o, float *part,
+                          hipStream_t s) {
+  NtArgs g{};
+  g.A = NtOperand{a, nullptr, (int32_t)arb, 0};
+  g.B = NtOperand{b, nullptr, (int32_t)brb, 0};
+  g.chunks = (int32_t)chunks;
+  return bf16 ? nt_product<1, 1, NT_BF16>(g, o, part, s) : nt_product<3, 3, NT_BF16>(g, o, part, s);
+}
+
+}  // namespace vcr
+
+using namespace vcr;
+#define TRY(expr)                       \
+  do {                                  \
+    const vcr_status st_ = (expr);      \
+    if (st_ != VCR_OK) return st_;      \
+  } while (0)
+
+static vcr_status check_opts(vcr_ctx *c, const vcr_linear_opts *o) {
+  if (o->act < VCR_ACT_NONE || o->act > VCR_ACT_SILU) return fail(c, VCR_ERR_ARG, "act: %d is not one of VCR_ACT_*", o->act);
+  return check_drop(c, o->drop);
+}
+static vcr_status check_like(vcr_ctx *c, const vcr_mat *m, int64_t rows, int64_t cols, const char *name) {
+  TRY(check_mat(c, m, name));
+  if (m->rows != rows || m->cols != cols)
+    return fail(c, VCR_ERR_SHAPE, "%s is %lld x %lld, not %lld x %lld", name, (long long)m->rows, (long long)m->cols, (long long)rows,
+                (long long)cols);
+  return VCR_OK;
+}
+static vcr_status check_rows(vcr_ctx *c, int64_t rows) {
+  if (rows > VCR_MAX_LINEAR_ROWS)
+    return fail(c, VCR_ERR_UNSUPPORTED, "%lld rows exceed the limit of %lld", (long long)rows, (long long)VCR_MAX_LINEAR_ROWS);
+  return VCR_OK;
+}
+
+extern "C" {
+
+vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts *opts, const vcr_mat *y) {
+  if (!c) return VCR_ERR_ARG;
+  const vcr_linear_opts o = opts ? *opts : vcr_linear_opts{};
+  TRY(check_mat(c, x, "x"));
+  TRY(check_mat(c, w, "w"));
+  if (x->type != w->type) return fail(c, VCR_ERR_ARG, "x and w differ in type");
+  if (w->rows == 0) return fail(c, VCR_ERR_SHAPE, "w has no rows");
+  if (x->cols != w->cols) return fail(c, VCR_ERR_SHAPE, "x and w differ in columns");
+  TRY(check_like(c, y, x->rows, w->rows, "y"));
+  TRY(check_opts(c, &o));
+  if ((reinterpret_cast<uintptr_t>(o.bias) & 3) != 0) return fail(c, VCR_ERR_ARG, "bias: pointer not aligned to its type");
+  if (o.residual) TRY(check_like(c, o.residual, x->rows, w->rows, "residual"));
+  if (o.z) TRY(check_like(c, o.z, x->rows, w->rows, "z"));
+  TRY(check_rows(c, x->rows));
+  TRY(check_rows(c, w->rows));
+  TRY(check_contraction(c, x->cols));
+  TRY(op_begin(c));
+  const int64_t M = x->rows, N = w->rows, K = x->cols;
+  if (M == 0) return VCR_OK;
+  const bool bf16 = x->type == VCR_BF16;
+  const int P = bf16 ? 1 : 3;
+  const DenseOut out{mat_ref(y), mat_ref(o.z), mat_ref(o.residual), o.bias, M, N, o.act, 1.f, drop_dev(o.drop)};
+  const int64_t chunks = blocks_of(K, 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16);
+  const size_t xb = (size_t)mb * chunks * P * FRAG, wb = (size_t)nb * chunks * P * FRAG, pb = room(bf16, M, N, chunks);
+  Workspace *ws = nullptr;
+  TRY(op_space(c, al(xb) + al(wb) + al(pb) + 256, &ws));
+  uint8_t *xp = take<uint8_t>(*ws, xb), *wp = take<uint8_t>(*ws, wb);
+  float *part = take<float>(*ws, pb / 4);
+  PlanesArgs xl{}, wl{};
+  xl.x = dev(x);
+  xl.rows = xp;
+  xl.row_blocks = mb;
+  wl.x = dev(w);
+  wl.rows = wp;
+  wl.row_blocks = nb;
+  xl.row_chunks = wl.row_chunks = chunks;
+  HIP_TRY(c, launch_dense_planes(nullptr, &xl, &wl, GradSource{}, bf16, c->stream));
+  HIP_TRY(c, product(bf16, xp, mb, wp, nb, chunks, out, part, c->stream));
+  return op_end(c);
+}
+
+vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts *opts, const vcr_mat *add,
+                           const vcr_mat *dx, const vcr_mat *dw, float *db) {
+  if (!c) return VCR_ERR_ARG;
+  const vcr_linear_opts o = opts ? *opts : vcr_linear_opts{};
+  TRY(check_mat(c, dy, "dy"));
+  const int64_t M = dy->rows, N = dy->cols;
+  TRY(check_opts(c, &o));
+  if (o.act != VCR_ACT_NONE) {
+    if (!o.z) return fail(c, VCR_ERR_ARG, "the gradient of an activation needs z");
+    TRY(check_like(c, o.z, M, N, "z"));
+  }
+  if (dw && !x) return fail(c, VCR_ERR_ARG, "dw needs x");
+  if (dx && !w) return fail(c, VCR_ERR_ARG, "dx needs w");
+  if (x) {
+    TRY(check_mat(c, x, "x"));
+    if (x->rows != M) return fail(c, VCR_ERR_SHAPE, "x and dy differ in rows");
+    if (x->type != dy->type) return fail(c, VCR_ERR_ARG, "x and dy differ in type");
+  }
+  if (w) {
+    TRY(check_mat(c, w, "w"));
+    if (w->rows != N) return fail(c, VCR_ERR_SHAPE, "w has %lld rows, dy %lld columns", (long long)w->rows, (long long)N);
+    if (w->type != dy->type) return fail(c, VCR_ERR_ARG, "w and dy differ in type");
+  }
+  if (x && w && x->cols != w->cols) return fail(c, VCR_ERR_SHAPE, "x and w differ in columns");
+  if (dx) TRY(check_like(c, dx, M, w->cols, "dx"));
+  if (dx && add) TRY(check_like(c, add, M, w->cols, "add"));
+  if (dw) TRY(check_like(c, dw, N, x->cols, "dw"));
+  if ((reinterpret_cast<uintptr_t>(db) & 3) != 0) return fail(c, VCR_ERR_ARG, "db: pointer not aligned to its type");
+  TRY(check_rows(c, M));
+  TRY(check_rows(c, N));
+  if (dx || dw) TRY(check_rows(c, dx ? w->cols : x->cols));
+  if (dx) TRY(check_contraction(c, N));
+  if (dw) TRY(check_contraction(c, M));
+  TRY(op_begin(c));
+  const bool bf16 = dy->type == VCR_BF16, has_dx = dx && M > 0;
+  if (!has_dx && !dw && !db) return VCR_OK;
+  const int P = bf16 ? 1 : 3;
+  const hipStream_t s = c->stream;
+  const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;
+  const int64_t nch = blocks_of(N, 32), mch = blocks_of(std::max<int64_t>(M, 1), 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16),
+                kb = blocks_of(K, 16), mg = blocks_of(M, 64);
+  const size_t b_g = has_dx ? (size_t)mb * nch * P * FRAG : 0, b_wt = has_dx ? (size_t)kb * nch * P * FRAG : 0;
+  const size_t b_gt = dw ? (size_t)nb * mch * P * FRAG : 0, b_xt = dw ? (size_t)kb * mch * P * FRAG : 0;
+  const size_t b_sums = db ? (size_t)mg * N * 4 : 0;
+  const size_t b_part = std::max(has_dx ? room(bf16, M, K, nch) : 0, dw ? room(bf16, N, K, mch) : 0);
+  Workspace *ws = nullptr;
+  TRY(op_space(c, al(b_g) + al(b_wt) + al(b_gt) + al(b_xt) + al(b_sums) + al(b_part) + 6 * 256, &ws));
+  uint8_t *gp = take<uint8_t>(*ws, b_g), *wt = take<uint8_t>(*ws, b_wt), *gt = take<uint8_t>(*ws, b_gt), *xt = take<uint8_t>(*ws, b_xt);
+  float *sums = take<float>(*ws, b_sums / 4), *part = take<float>(*ws, b_part / 4);
+  const DropDev drop = drop_dev(o.drop);
+  PlanesArgs gl{}, xl{}, wl{};
+  gl.x = dev(dy);
+  if (has_dx) {
+    gl.rows = gp;
+    gl.row_blocks = mb;
+    gl.row_chunks = nch;
+    wl.x = dev(w);
+    wl.cols = wt;
+    wl.col_blocks = kb;
+    wl.col_chunks = nch;
+  }
+  if (dw) {
+    gl.cols = gt;
+    gl.col_blocks = nb;
+    xl.x = dev(x);
+    xl.cols = xt;
+    xl.col_blocks = kb;
+    gl.col_chunks = xl.col_chunks = mch;
+  }
+  gl.sums = db && M > 0 ? sums : nullptr;
+  HIP_TRY(c, launch_dense_planes(&gl, dw ? &xl : nullptr, has_dx ? &wl : nullptr, GradSource{mat_ref(o.act != VCR_ACT_NONE ? o.z : nullptr), o.act, drop},
+                                 bf16, s));
+  if (db) {
+    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, mg, N, drop.factor, db);
+    HIP_TRY(c, hipGetLastError());
+  }
+  const DropDev none = drop_dev(nullptr);
+  if (has_dx)
+    HIP_TRY(c, product(bf16, gp, mb, wt, kb, nch, DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none}, part, s));
+  if (dw)
+    HIP_TRY(c, product(bf16, gt, nb, xt, kb, mch, DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none}, part, s));
+  return op_end(c);
+}
+
+}  // extern "C"

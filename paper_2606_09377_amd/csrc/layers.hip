@@ -13,7 +13,7 @@
 
 #include "ctx.h"
 #include "layers.h"
-#include "planes.h"
+#include "products.h"
 
 namespace vcr {
 
@@ -187,6 +187,7 @@ struct OutMat {
   int64_t rows, cols, ld;
   const float *bias;   // or null
   int32_t relu;
+  float bytes() const { return bf16 ? 2.f : 4.f; }
   __device__ __forceinline__ void put(int64_t m, int64_t n, f32v4 v) const {
     if (bias) {
 #pragma unroll
@@ -199,48 +200,9 @@ struct OutMat {
     store_row4(p, bf16, ld, rows, cols, vec, m, n, v);
   }
 };
-struct EpiOut {
-  OutMat o;
-  __device__ __forceinline__ void store(int, int, int m, int n, f32v4 v, int) const { o.put(m, n, v); }
-};
-// sums over one part of the contraction, [parts][rows][ld]
-struct EpiPart {
-  float *p;
-  int64_t rows, ld;
-  __device__ __forceinline__ void store(int, int z, int m, int n, f32v4 v, int) const {
-    if (m < rows && n < ld) *reinterpret_cast<f32v4 *>(p + (z * rows + m) * ld + n) = v;
-  }
-};
-__global__ __launch_bounds__(256) void k_join(const float *p, int parts, int64_t rows, int64_t ld, OutMat o) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = ld / 4, m = id / per, n = (id - m * per) * 4;
-  if (m >= rows) return;
-  f32v4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < parts; ++z) v += *reinterpret_cast<const f32v4 *>(p + (z * rows + m) * ld + n);
-  o.put(m, n, v);
-}
-
 // ---- products by tiles ------------------------------------------------------------------------
 // (nt.h; in 4 bits 4096 x 8192 x 8192 in 156 us, 3.5 PFLOP/s; bf16 rows with 4-bit weights 256 x 8192 x 8192 in 38 us; the gradients
 // of 4096 x 8192 x 8192 in bf16 at 1.4 to 1.5 PFLOP/s, where a library product of that size reaches 1.35 to 1.55.)
-template <int PA, int PB, int KIND>
-static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
-  const int parts = nt_parts<NtTiles<PA, PB, KIND>>(M, N, chunks);
-  return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
-}
-// D = A B^T into o; part: room for part_bytes
-template <int PA, int PB, int KIND>
-static hipError_t nt_product(const NtArgs &g, const OutMat &o, float *part, hipStream_t s) {
-  typedef NtTiles<PA, PB, KIND> TS;
-  const int parts = nt_parts<TS>(o.rows, o.cols, g.chunks);
-  if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, o.bf16 ? 2.f : 4.f, EpiOut{o}, s);
-  const int64_t ld = blocks_of(o.cols, 4) * 4;
-  const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
-  const hipError_t e = launch_nt<typename TS::T4>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,
-                                                  EpiPart{part, o.rows, ld}, s);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, parts, o.rows, ld, o);
-  return hipGetLastError();
-}
 
 // ---- few rows ---------------------------------------------------------------------------------
 // y = act(x w^T + bias) for few rows x: bound by reading the weights once.  A workgroup takes RB row blocks of weights;
@@ -438,7 +400,7 @@ static hipError_t launch_rows(const DevMat &x, const MxDev &a, const MxDev &w, c
   hipError_t e = p.rb == 4 ? go(k_rows<X, 4>) : p.rb == 2 ? go(k_rows<X, 2>) : go(k_rows<X, 1>);
   if (e != hipSuccess || !part) return e;
   const int64_t ld = blocks_of(o.cols, 16) * 16;
-  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
+  hipLaunchKernelGGL((k_join<OutMat>), dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
   return hipGetLastError();
 }
 

@@ -156,6 +156,20 @@ __device__ __forceinline__ void nt_tile(const NtArgs &g, int id, int total, int 
 // EPI: a struct with store(batch, part of the contraction, m, n, values of n .. n + 3, lane): called by
 // whole waves for every block, with the lane's row m and first column n; the other lanes of a block hold
 // its other rows and columns.
+// One with STAGED has store8(m, n, values of n .. n + 7) instead: the tile goes through LDS, so that a wave has whole
+// stretches of rows (an epilogue that reads other matrices, or writes two, then moves whole lines, and its code is there once
+// and not for every block of a wave).
+template <class EPI, class = void>
+struct nt_staged : std::false_type {};
+template <class EPI>
+struct nt_staged<EPI, std::enable_if_t<EPI::STAGED>> : std::true_type {};
+// Row blocks of a wave that go through LDS together (rows of BN + 4 floats)
+template <class T>
+constexpr int nt_stage_blocks() {
+  int n = T::MB;
+  while (n > 1 && (n * T::WM * 16 * (T::BN + 4) * 4 > T::LDS || T::MB % n)) --n;
+  return n;
+}
 template <class T, class EPI>
 __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2) void k_nt(const NtArgs g, const EPI epi) {
   constexpr int MB = T::MB, NB = T::NB, NW = T::NW, KS = T::KS, NS = T::NS, PA = T::PA, PB = T::PB;
@@ -440,9 +454,61 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     return v;
   };
   auto put = [&](int i, int j, f32v4 v) {
-    epi.store(batch, blockIdx.y, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
+    if constexpr (!nt_staged<EPI>::value) epi.store(batch, blockIdx.y, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
   };
-  if constexpr (T::WK == 1) {
+  if constexpr (nt_staged<EPI>::value) {
+    constexpr int PITCH = T::BN + 4;
+    float *tile = reinterpret_cast<float *>(lds);
+    auto rows_out = [&](int per, int i0) {   // the tile's rows i0 .. i0 + per of every wave, as they lie in LDS
+      __syncthreads();
+      for (int at = threadIdx.x; at < T::WM * per * (T::BN / 8); at += T::T) {
+        const int q = at / (T::BN / 8), c = at - q * (T::BN / 8), w = q / per, r = q - w * per;
+        const float *s = tile + q * PITCH + c * 8;
+        const f32v4 a = *reinterpret_cast<const f32v4 *>(s), b = *reinterpret_cast<const f32v4 *>(s + 4);
+        float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        epi.store8(16 * (rb0 + w * MB) + i0 + r, 16 * cb0 + c * 8, v);
+      }
+    };
+    if constexpr (T::WK == 1) {
+      constexpr int IB = nt_stage_blocks<T>();
+      static_assert(IB * T::WM * 16 * PITCH * 4 <= T::LDS, "rows of a tile in LDS");
+#pragma unroll
+      for (int p = 0; p < MB / IB; ++p) {
+        barrier_only();   // what LDS held has been read
+#pragma unroll
+        for (int i = 0; i < IB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            *reinterpret_cast<f32v4 *>(tile + ((wm * IB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = joined(p * IB + i, j);
+        rows_out(16 * IB, p * IB * 16);
+      }
+    } else {
+      constexpr int B = MB * NB, PER = (B + T::WK - 1) / T::WK;
+      static_assert(T::BM * PITCH * 4 <= T::LDS, "the tile in LDS");
+      f32v4 *red = reinterpret_cast<f32v4 *>(lds) + (wm + T::WM * wn) * T::WK * B * 64 + lane;
+      barrier_only();   // the last stage has been read
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) red[(wk * B + i * NB + j) * 64] = joined(i, j);
+      __syncthreads();
+      f32v4 sum[PER];   // of blocks wk, wk + WK, ..
+#pragma unroll
+      for (int n = 0; n < PER; ++n) {
+        const int blk = min(n * T::WK + wk, B - 1);
+        sum[n] = red[blk * 64];
+#pragma unroll
+        for (int q = 1; q < T::WK; ++q) sum[n] += red[(q * B + blk) * 64];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < PER; ++n) {
+        const int blk = n * T::WK + wk, i = blk / NB, j = blk - i * NB;
+        if (blk < B) *reinterpret_cast<f32v4 *>(tile + ((wm * MB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = sum[n];
+      }
+      rows_out(16 * MB, 0);
+    }
+  } else if constexpr (T::WK == 1) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll

@@ -135,30 +135,19 @@ struct PlanesArgs {
 struct PlanesScale {
   float two[2], rest;
 };
-template <int P, bool BF>
-__device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, PlanesScale scale, float (&tile)[64][65]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, oct = lane >> 4;
-  const int64_t rb = tr * 4 + wave, row = rb * 16 + r;
-  float v[2][8];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t col = tc * 64 + h * 32 + oct * 8;
-    mat_row8<BF>(g.x, base, row, col, g.vec, v[h]);
-    if (g.y.p) {
-      float m[8];
-      mat_row8<BF>(g.y, base, row, col, g.vec, m);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[h][i] = m[i] > 0.f ? v[h][i] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[h][i] = v[h][i] * scale.two[0] * scale.two[1] * scale.rest;
-    const int64_t ch = tc * 2 + h;   // 32 columns
-    if (g.rows && rb < g.row_blocks && ch < g.row_chunks) {
-      if (g.grouped) store_slot<P>(g.rows, rb * g.row_chunks + (ch & ~(int64_t)3) + oct, (int)(ch & 3) * 16 + r, v[h]);
-      else store_slot<P>(g.rows, rb * g.row_chunks + ch, lane, v[h]);
-    }
-  }
+// The tile's operands and sums of the values of a lane: row 16 (4 tr + wave) + lane % 16, columns 64 tc + 32 h + 8 (lane / 16) ..
+template <int P>
+__device__ __forceinline__ void planes_rows(const PlanesArgs &g, int64_t tr, int64_t tc, int h, const float (&v)[8]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rb = tr * 4 + wave, ch = tc * 2 + h;   // 32 columns
+  if (!g.rows || rb >= g.row_blocks || ch >= g.row_chunks) return;
+  if (g.grouped) store_slot<P>(g.rows, rb * g.row_chunks + (ch & ~(int64_t)3) + (lane >> 4), (int)(ch & 3) * 16 + (lane & 15), v);
+  else store_slot<P>(g.rows, rb * g.row_chunks + ch, lane, v);
+}
+template <int P>
+__device__ __forceinline__ void planes_cols(const PlanesArgs &g, int64_t tr, int64_t tc, const float (&v)[2][8], float (&tile)[64][65]) {
   if (!g.cols && !g.sums) return;   // uniform
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, oct = lane >> 4;
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -183,6 +172,27 @@ __device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, i
     const int64_t col = tc * 64 + wave * 16 + r;
     if (oct == 0 && col < g.x.cols) g.sums[tr * g.x.cols + col] = s;
   }
+}
+template <int P, bool BF>
+__device__ __forceinline__ void planes_tile(const PlanesArgs &g, int64_t base, int64_t tr, int64_t tc, PlanesScale scale, float (&tile)[64][65]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (tr * 4 + wave) * 16 + (lane & 15);
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t col = tc * 64 + h * 32 + (lane >> 4) * 8;
+    mat_row8<BF>(g.x, base, row, col, g.vec, v[h]);
+    if (g.y.p) {
+      float m[8];
+      mat_row8<BF>(g.y, base, row, col, g.vec, m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[h][i] = m[i] > 0.f ? v[h][i] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[h][i] = v[h][i] * scale.two[0] * scale.two[1] * scale.rest;
+    planes_rows<P>(g, tr, tc, h, v[h]);
+  }
+  planes_cols<P>(g, tr, tc, v, tile);
 }
 
 // Four consecutive k of one row, into an operand of P parts with so many chunks

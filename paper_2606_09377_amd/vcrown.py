@@ -28,6 +28,7 @@ LAMBDA_RULES = {"adaptive": 0, "zero": 1, "one": 2, "same_slope": 3}
 # values of OPT_PRODUCTS (how the networks loaded from then on multiply)
 PRODUCTS = {"split": 0, "float32": 1, "split_no_copies": 2}
 MAX_SPLITS = 64   # VCR_MAX_SPLITS
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}   # VCR_ACT_*
 
 
 class VcrNode(ctypes.Structure):
@@ -94,6 +95,19 @@ class VcrNsOpts(ctypes.Structure):
                 ("eps", ctypes.c_float), ("gain", ctypes.c_float), ("keep", ctypes.c_float)]
 
 
+class VcrDrop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class VcrLinearOpts(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("act", ctypes.c_int32), ("drop", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("z", ctypes.c_void_p)]
+
+
+class VcrLossOpts(ctypes.Structure):
+    _fields_ = [("smoothing", ctypes.c_float), ("lse2", ctypes.c_float), ("mean", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class VcrError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 7 else status}: {msg}")
@@ -138,6 +152,10 @@ def load_library(path: str = LIB_PATH):
         "vcr_mx_linear": ([P, P, P, P, I32, P], I32),
         "vcr_mx_linear_grad": ([P, P, P, P, P, P, P, P], I32),
         "vcr_orthogonalize": ([P, P, I32, ctypes.c_int64, P, P, ctypes.c_int64, P, ctypes.c_int64], I32),
+        "vcr_dropout": ([P, P, P, P, P], I32),
+        "vcr_linear": ([P, P, P, P, P], I32),
+        "vcr_linear_grad": ([P, P, P, P, P, P, P, P, P], I32),
+        "vcr_cross_entropy": ([P, P, P, P, P, P, P], I32),
         "vcr_crown_bounds_noalloc": ([P, P, I32, F32, P, I32, P, P], I32),
     }
     for name, (args, res) in sig.items():
@@ -236,6 +254,23 @@ class MX:
         c = self.codes.view(rb, groups, 4, 16, 16).permute(0, 3, 1, 2, 4).reshape(rb * 16, groups * 64)
         s = self.scales.view(rb, n4, 4, 16, 4).permute(0, 3, 1, 4, 2).reshape(rb * 16, n4 * 16)
         return (c[:self.rows, :-(-self.cols // 2)].contiguous(), s[:self.rows, :-(-self.cols // 32)].contiguous())
+
+
+class Dropout:
+    """Which values dropout keeps (vcr_drop): each with probability 1 - p, in steps of 2^-16, by random bits that seed, offset
+    + step and a value's place give.  `step`: an int64 CUDA tensor of one element, read when a call's work runs (so that replays of
+    a recorded call take new masks), or None.  The same seed, offset and step give the same mask: a gradient takes the object
+    of its call, another call an offset of its own."""
+
+    __slots__ = ("p", "seed", "offset", "step", "_c")
+
+    def __init__(self, p, seed=0, offset=0, step=None):
+        if step is not None:
+            import torch
+            if not (isinstance(step, torch.Tensor) and step.dtype == torch.int64 and step.is_cuda and step.numel() == 1):
+                raise ValueError("expected an int64 CUDA tensor of one element")
+        self.p, self.seed, self.offset, self.step = p, seed, offset, step
+        self._c = _DROP.pack(p, seed & (2 ** 64 - 1), offset & (2 ** 64 - 1), 0 if step is None else step.data_ptr())
 
 
 def _net_nodes(net):
@@ -545,6 +580,76 @@ class Ctx:
         self._check(self.lib.vcr_orthogonalize(self.h, gm[0], count, gm[1], ctypes.byref(o), bm[0], bm[1], om[0], om[1]))
         return out
 
+    # ---- layers in float, dropout and the loss ----
+    def _here(self, *tensors):
+        """Tensors of the context's device."""
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"expected tensors of device {self.device}")
+
+    def dropout(self, x, drop, residual=None, dtype=None, out=None):
+        """Dropout of x (rows, cols), a float32 or bfloat16 CUDA tensor with contiguous rows, plus `residual`: of x's type
+        unless `dtype` says so.  drop: a Dropout.  The gradient by x is the same call on dy, without the residual.  `out`
+        may be x or the residual."""
+        m = _mat(x)
+        y = x.new_empty(x.shape, dtype=dtype or x.dtype) if out is None else out
+        self._here(x, residual, y, drop.step)
+        self._current_stream()
+        self._check(self.lib.vcr_dropout(self.h, m, drop._c, None if residual is None else _mat(residual), _mat(y)))
+        return y
+
+    def linear(self, x, w, bias=None, act="none", dropout=None, residual=None, keep_z=False, dtype=None, out=None):
+        """dropout(act(z)) + residual with z = x w^T + bias: x (rows, k) and w (n, k) float32 or bfloat16 CUDA tensors of one
+        type with contiguous rows, bias float32, act one of "none", "relu", "gelu", "silu".  Of x's type unless `dtype` says so.
+        With keep_z (y, z), z as the gradient takes it, of x's type.  `out` may be the residual."""
+        xm, wm = _mat(x), _mat(w)
+        y = x.new_empty((x.shape[0], w.shape[0]), dtype=dtype or x.dtype) if out is None else out
+        z = x.new_empty(y.shape) if keep_z else None
+        self._here(x, w, bias, residual, y, None if dropout is None else dropout.step)
+        o, keep = _linear_opts(_bias(bias, w.shape[0]), act, dropout, residual, z)
+        self._current_stream()
+        self._check(self.lib.vcr_linear(self.h, xm, wm, o, _mat(y)))
+        del keep
+        return (y, z) if keep_z else y
+
+    def linear_grad(self, dy, x, w, z=None, act="none", dropout=None, add=None, need=(True, True, True), dw_dtype=None):
+        """(dx, dw, db) of linear from dy (rows, n), all of one type: dx (rows, k), plus `add`, and dw (n, k) of that type (dw: of
+        `dw_dtype`), db (n) float32; None where `need` says so.  z: linear's, for an activation (with "relu" and no
+        residual its result will do); act and dropout as they were.  The gradient by the residual is dy."""
+        g = _mat(dy)
+        rows, n = dy.shape
+        dx = dy.new_empty((rows, w.shape[1])) if need[0] else None
+        dw = dy.new_empty((n, x.shape[1]), dtype=dw_dtype or dy.dtype) if need[1] else None
+        db = dy.new_empty((n,), dtype=_f32()) if need[2] else None
+        self._here(dy, x, w, z, add, None if dropout is None else dropout.step)
+        o, keep = _linear_opts(None, act, dropout, None, z)
+        self._current_stream()
+        self._check(self.lib.vcr_linear_grad(
+            self.h, g, _mat(x) if need[1] else None, _mat(w) if need[0] else None, o, None if add is None or not need[0] else _mat(add),
+            None if dx is None else _mat(dx), None if dw is None else _mat(dw), None if db is None else db.data_ptr()))
+        del keep
+        return dx, dw, db
+
+    def cross_entropy(self, logits, label, smoothing=0.0, lse2=0.0, mean=True, scale=1.0, grad=True, out=None):
+        """(total, loss, dlogits) of logits (rows, n), a float32 or bfloat16 CUDA tensor with contiguous rows, and label (rows),
+        int64, a negative one for a row that does not count: the rows' cross entropies plus lse2 times their squared log sum of
+        exponentials, their sum (divided by the number of rows that count, with `mean`) and scale times its gradient,
+        of the logits' type (None without `grad`).  `out`: dlogits, which may be the logits."""
+        import torch
+        m = _mat(logits)
+        rows = logits.shape[0]
+        if not (isinstance(label, torch.Tensor) and label.dtype == torch.int64 and label.is_cuda and label.shape == (rows,) and
+                label.is_contiguous()):
+            raise ValueError(f"expected a contiguous int64 CUDA tensor of shape ({rows},)")
+        sums = logits.new_empty((rows + 1,), dtype=torch.float32)   # the total, then the rows'
+        d = (logits.new_empty(logits.shape) if out is None else out) if grad else None
+        self._here(logits, label, d)
+        at = sums.data_ptr()
+        self._current_stream()
+        self._check(self.lib.vcr_cross_entropy(self.h, m, label.data_ptr(), _LOSS.pack(smoothing, lse2, 1 if mean else 0, scale), at + 4, at,
+                                               None if d is None else _mat(d)))
+        return sums[0], sums[1:], d
+
     def layer_bounds(self, relu_id, B):
         import torch
         n = self.relu_sizes[relu_id]
@@ -601,6 +706,7 @@ def _out_size(net):
 _TYPES = {}   # vcr_mat's types by torch's
 # vcr_mat and vcr_mx as bytes: a call of a few microseconds notices the time it takes to build the structures above
 _MAT, _MX = struct.Struct("@Piqqq"), struct.Struct("@PPqq")
+_DROP, _LINEAR, _LOSS = struct.Struct("@fQQP"), struct.Struct("@PiPPP"), struct.Struct("@ffif")
 
 
 def _mat(t):
@@ -628,6 +734,27 @@ def _bias(b, n):
     if not (isinstance(b, torch.Tensor) and b.dtype == torch.float32 and b.is_cuda and b.shape == (n,) and b.is_contiguous()):
         raise ValueError(f"expected a contiguous float32 CUDA tensor of shape ({n},)")
     return b.data_ptr()
+
+
+def _f32():
+    import torch
+    return torch.float32
+
+
+def _at(packed):
+    """(address, what holds it) of a packed structure that another one points to."""
+    buf = ctypes.create_string_buffer(packed, len(packed))
+    return ctypes.addressof(buf), buf
+
+
+def _linear_opts(bias, act, dropout, residual, z):
+    """A packed vcr_linear_opts and what it points to."""
+    if act not in ACTS:
+        raise ValueError(f"act is one of {sorted(ACTS)}")
+    drop, k0 = (None, None) if dropout is None else _at(dropout._c)
+    res, k1 = (None, None) if residual is None else _at(_mat(residual))
+    zz, k2 = (None, None) if z is None else _at(_mat(z))
+    return _LINEAR.pack(bias or 0, ACTS[act], drop or 0, res or 0, zz or 0), (k0, k1, k2)
 
 
 def _check_tensor(t, shape):
