@@ -27,10 +27,15 @@ __device__ __forceinline__ void unpack8(const uint4 &q, float (&v)[8]) {
     v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
   }
 }
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float f32v2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32v2{a, b}), bf16x2));
+}
 __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = bf16_round(v[2 * i]) | (uint32_t)bf16_round(v[2 * i + 1]) << 16;
+  for (int i = 0; i < 4; ++i) w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // Columns c .. c + 7 of row r, those below cols (the others are 0, or left as they are)

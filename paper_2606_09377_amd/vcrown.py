@@ -637,18 +637,20 @@ class Ctx:
         of the logits' type (None without `grad`).  `out`: dlogits, which may be the logits."""
         import torch
         m = _mat(logits)
-        rows = logits.shape[0]
-        if not (isinstance(label, torch.Tensor) and label.dtype == torch.int64 and label.is_cuda and label.shape == (rows,) and
-                label.is_contiguous()):
-            raise ValueError(f"expected a contiguous int64 CUDA tensor of shape ({rows},)")
-        sums = logits.new_empty((rows + 1,), dtype=torch.float32)   # the total, then the rows'
-        d = (logits.new_empty(logits.shape) if out is None else out) if grad else None
-        self._here(logits, label, d)
-        at = sums.data_ptr()
+        rows, here = logits.shape[0], self.device
+        if not (isinstance(label, torch.Tensor) and label.dtype == torch.int64 and label.shape == (rows,) and label.is_contiguous() and
+                label.get_device() == here and logits.get_device() == here):
+            raise ValueError(f"expected logits and a contiguous int64 tensor of shape ({rows},) on device {here}")
+        loss, total = logits.new_empty((rows,), dtype=torch.float32), logits.new_empty((), dtype=torch.float32)
+        d = None
+        if grad:
+            d = torch.empty_like(logits) if out is None else out
+            if d.get_device() != here:
+                raise ValueError(f"expected tensors of device {here}")
         self._current_stream()
-        self._check(self.lib.vcr_cross_entropy(self.h, m, label.data_ptr(), _LOSS.pack(smoothing, lse2, 1 if mean else 0, scale), at + 4, at,
-                                               None if d is None else _mat(d)))
-        return sums[0], sums[1:], d
+        self._check(self.lib.vcr_cross_entropy(self.h, m, label.data_ptr(), _LOSS.pack(smoothing, lse2, 1 if mean else 0, scale), loss.data_ptr(),
+                                               total.data_ptr(), None if d is None else m if d is logits else _mat(d)))
+        return total, loss, d
 
     def layer_bounds(self, relu_id, B):
         import torch
