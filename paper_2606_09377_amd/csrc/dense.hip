@@ -124,6 +124,200 @@ __global__ __launch_bounds__(256) void k_dense_sums(const float *sums, int64_t g
   if (wave == 0 && c < cols) out[c] = factor * ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
 }
 
+// ---- few rows ---------------------------------------------------------------------------------
+// y for up to 64 rows of x, from x and w as they are stored: bound by reading the weights once.  A workgroup takes NB row blocks of w (16
+// rows), its 8 waves go through groups of U chunks of 32 columns in turn, each with the next group's loads in flight, and their sums are added in LDS in wave order.
+// A lane reads its row's eight columns of a chunk as the matrix instruction takes them, of w and of x alike (x comes from L2: laid out
+// in LDS it would have to wait there for the slowest wave); float32 values are split into their parts in registers.  Rows beyond
+// the last read that one, and their results are not stored.
+template <bool BF>
+struct Raw8 {   // eight columns of a row as stored
+  uint4 q[BF ? 1 : 2];
+};
+template <bool BF>
+__device__ __forceinline__ Raw8<BF> raw_load(const uint8_t *p) {   // (rows may be aligned to their element alone)
+  Raw8<BF> r;
+  __builtin_memcpy(&r, __builtin_assume_aligned(p, BF ? 2 : 4), sizeof(r));
+  return r;
+}
+template <bool BF>
+__device__ __forceinline__ Raw8<BF> raw_edge(const uint8_t *p, int n) {   // the first n of them, zeros beyond
+  Raw8<BF> r;
+  uint32_t *w = reinterpret_cast<uint32_t *>(&r);
+#pragma unroll
+  for (int i = 0; i < (BF ? 4 : 8); ++i) {
+    if constexpr (BF) {
+      const uint16_t *s = reinterpret_cast<const uint16_t *>(p) + 2 * i;
+      w[i] = (2 * i < n ? s[0] : 0u) | (2 * i + 1 < n ? (uint32_t)s[1] << 16 : 0u);
+    } else {
+      w[i] = i < n ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
+    }
+  }
+  return r;
+}
+template <bool BF>
+struct Parts8 {
+  bf16x8 p[BF ? 1 : 3];
+};
+template <bool BF>
+__device__ __forceinline__ Parts8<BF> raw_parts(const Raw8<BF> &r) {
+  Parts8<BF> o;
+  if constexpr (BF) {
+    o.p[0] = __builtin_bit_cast(bf16x8, r.q[0]);
+  } else {
+    const float v[8] = {__builtin_bit_cast(float, r.q[0].x), __builtin_bit_cast(float, r.q[0].y), __builtin_bit_cast(float, r.q[0].z),
+                        __builtin_bit_cast(float, r.q[0].w), __builtin_bit_cast(float, r.q[1].x), __builtin_bit_cast(float, r.q[1].y),
+                        __builtin_bit_cast(float, r.q[1].z), __builtin_bit_cast(float, r.q[1].w)};
+    uint32_t w[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) parts_of<3>(v[2 * i], v[2 * i + 1], w[i]);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) o.p[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]));
+  }
+  return o;
+}
+template <bool BF, int MT, int NB, int U>
+__global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut o, float *part, int z_groups) {
+  constexpr int ES = BF ? 2 : 4;
+  __shared__ f32v4 red[8][MT * NB][64];
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * NB);
+  const int M = (int)x.rows, K = (int)w.cols, whole = K / (32 * U), groups = (K + 32 * U - 1) / (32 * U);
+  const int g0 = blockIdx.y * z_groups, g1 = min(groups, g0 + z_groups), gw = min(whole, g1);
+  const uint8_t *wp[NB], *xp[MT];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) wp[b] = static_cast<const uint8_t *>(w.p) + (min(n0 + 16 * b + r16, w.rows - 1) * w.ld + 8 * g4) * ES;
+#pragma unroll
+  for (int t = 0; t < MT; ++t) xp[t] = static_cast<const uint8_t *>(x.p) + (min(16 * t + r16, M - 1) * x.ld + 8 * g4) * ES;
+  struct Group {
+    Raw8<BF> w[U][NB], x[U][MT];
+  };
+  auto load = [&](Group &q, int gi) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = ((int64_t)gi * U + u) * (32 * ES);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) q.w[u][b] = raw_load<BF>(wp[b] + at);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) q.x[u][t] = raw_load<BF>(xp[t] + at);
+    }
+  };
+  f32v4 hi[MT][NB], lo[BF ? 1 : MT][BF ? 1 : NB];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      hi[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (!BF) lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+    }
+  auto multiply = [&](const Raw8<BF> (&rw)[NB], const Raw8<BF> (&rx)[MT]) {
+    Parts8<BF> a[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) a[t] = raw_parts<BF>(rx[t]);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const Parts8<BF> v = raw_parts<BF>(rw[b]);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        if constexpr (BF) {
+          hi[t][b] = mfma_bf16(v.p[0], a[t].p[0], hi[t][b]);
+        } else {   // (nt.h: the small products, in order of their size, in an accumulator of their own)
+          constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+          for (int p = 0; p < 5; ++p) lo[t][b] = mfma_bf16(v.p[pb[p]], a[t].p[pa[p]], lo[t][b]);
+          hi[t][b] = mfma_bf16(v.p[0], a[t].p[0], hi[t][b]);
+        }
+      }
+    }
+  };
+  auto use = [&](const Group &q) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) multiply(q.w[u], q.x[u]);
+  };
+  Group q[2];
+  int gi = g0 + wave;
+  if (gi < gw) load(q[0], gi);
+  for (; gi < gw; gi += 16) {
+    if (gi + 8 < gw) load(q[1], gi + 8);
+    use(q[0]);
+    if (gi + 16 < gw) load(q[0], gi + 16);
+    if (gi + 8 < gw) use(q[1]);
+  }
+  if (groups > whole && g1 == groups && wave == (whole - g0) % 8) {   // the columns beyond whole groups
+    for (int c = whole * U; c * 32 < K; ++c) {
+      const int n = max(0, min(8, K - 32 * c - 8 * g4));
+      const int64_t at = (int64_t)c * (32 * ES);
+      Raw8<BF> ew[NB], ex[MT];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) ew[b] = raw_edge<BF>(wp[b] + at, n);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) ex[t] = raw_edge<BF>(xp[t] + at, n);
+      multiply(ew, ex);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      f32v4 v = hi[t][b];
+      if constexpr (!BF) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < __builtin_huge_valf() ? v[i] + lo[t][b][i] : v[i];
+      }
+      red[wave][t * NB + b][lane] = v;
+    }
+  __syncthreads();
+  for (int it = threadIdx.x; it < M * NB * 2; it += 512) {
+    const int m = it / (NB * 2), oct = it - m * (NB * 2), blk = (m >> 4) * NB + (oct >> 1), l = (m & 15) + 32 * (oct & 1);
+    f32v4 a = red[0][blk][l], b = red[0][blk][l + 16];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) a += red[k][blk][l], b += red[k][blk][l + 16];
+    const int64_t n = n0 + oct * 8;
+    if (part) {
+      f32v4 *d = reinterpret_cast<f32v4 *>(part + ((int64_t)blockIdx.y * M + m) * (gridDim.x * (16 * NB)) + n);
+      d[0] = a;
+      d[1] = b;
+    } else {
+      float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      o.store8(m, n, v);
+    }
+  }
+}
+struct DenseRows {
+  int nb, u, parts, z_groups;
+  int64_t wgs;
+  size_t part_bytes;
+};
+static DenseRows dense_rows(bool bf16, int64_t M, int64_t N, int64_t K) {
+  DenseRows p{};
+  const int64_t blocks = blocks_of(N, 16);
+  const char *e = getenv("DR");
+  p.nb = e ? atoi(e) : blocks >= 512 ? 2 : 1;
+  p.u = bf16 ? (M <= 16 ? 4 : 2) : M <= 16 ? 2 : 1;
+  p.wgs = blocks_of(blocks, p.nb);
+  const int64_t groups = blocks_of(K, 32 * p.u), bytes = 16 * p.nb * K * (bf16 ? 2 : 4);
+  const int64_t z = std::max<int64_t>(1, std::min<int64_t>({256 / p.wgs, bytes >> 18, groups / 16}));
+  p.z_groups = (int)blocks_of(groups, z);
+  p.parts = (int)blocks_of(groups, p.z_groups);
+  p.part_bytes = p.parts > 1 ? (size_t)p.parts * M * p.wgs * p.nb * 64 : 0;
+  return p;
+}
+template <bool BF>
+static hipError_t launch_dense_rows(const DevMat &x, const DevMat &w, const DenseRows &p, const DenseOut &o, float *part, hipStream_t s) {
+  if (p.parts == 1) part = nullptr;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.wgs, (unsigned)p.parts), dim3(512), 0, s, x, w, o, part, p.z_groups); };
+  constexpr int U1 = BF ? 4 : 2, U2 = BF ? 2 : 1;
+  if (x.rows <= 16) p.nb == 2 ? go(k_dense_rows<BF, 1, 2, U1>) : go(k_dense_rows<BF, 1, 1, U1>);
+  else if (x.rows <= 32) p.nb == 2 ? go(k_dense_rows<BF, 2, 2, U2>) : go(k_dense_rows<BF, 2, 1, U2>);
+  else p.nb == 2 ? go(k_dense_rows<BF, 4, 2, U2>) : go(k_dense_rows<BF, 4, 1, U2>);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !part) return e;
+  const int64_t ld = p.wgs * p.nb * 16;
+  hipLaunchKernelGGL((k_join<DenseOut>), dim3((unsigned)blocks_of(o.rows * (ld / 8), 256)), dim3(256), 0, s, part, p.parts, o.rows, ld, o);
+  return hipGetLastError();
+}
+
 static DevMat dev(const vcr_mat *m) { return DevMat{m->p, m->type == VCR_BF16, m->rows, m->cols, m->ld, 0}; }
 static size_t room(bool bf16, int64_t M, int64_t N, int64_t chunks) {
   return bf16 ? part_bytes<1, 1, NT_BF16>(M, N, chunks) : part_bytes<3, 3, NT_BF16>(M, N, chunks);
@@ -135,6 +329,11 @@ static hipError_t product(bool bf16, const uint8_t *a, int64_t arb, const uint8_
   g.B = NtOperand{b, nullptr, (int32_t)brb, 0};
   g.chunks = (int32_t)chunks;
   return bf16 ? nt_product<1, 1, NT_BF16>(g, o, part, s) : nt_product<3, 3, NT_BF16>(g, o, part, s);
+}
+
+// bf16 operands that the tiles take as they are (nt.h)
+static bool rows_product(const vcr_mat *x, const vcr_mat *w) {
+  return x->cols % 8 == 0 && rows_aligned(x->p, x->ld, 2) && rows_aligned(w->p, w->ld, 2) && std::max(x->ld, w->ld) < (int64_t)1 << 22;
 }
 
 }  // namespace vcr
@@ -187,7 +386,28 @@ vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_
   const bool bf16 = x->type == VCR_BF16;
   const int P = bf16 ? 1 : 3;
   const DenseOut out{mat_ref(y), mat_ref(o.z), mat_ref(o.residual), o.bias, M, N, o.act, 1.f, drop_dev(o.drop)};
+  if (M <= (getenv("DRM") ? atoi(getenv("DRM")) : 64)) {
+    const DenseRows p = dense_rows(bf16, M, N, K);
+    Workspace *ws = nullptr;
+    TRY(op_space(c, p.part_bytes, &ws));
+    float *part = reinterpret_cast<float *>(ws->base);
+    if (bf16) HIP_TRY(c, launch_dense_rows<true>(dev(x), dev(w), p, out, part, c->stream));
+    else HIP_TRY(c, launch_dense_rows<false>(dev(x), dev(w), p, out, part, c->stream));
+    return op_end(c);
+  }
   const int64_t chunks = blocks_of(K, 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16);
+  if (bf16 && rows_product(x, w) && !getenv("NOROWS")) {
+    const size_t pb = part_bytes<1, 1, NT_ROWS>(M, N, chunks);
+    Workspace *ws = nullptr;
+    TRY(op_space(c, pb, &ws));
+    NtArgs g{};
+    g.A = NtOperand{static_cast<const uint8_t *>(x->p), nullptr, (int32_t)mb, 0, x->ld * 2, M};
+    g.B = NtOperand{static_cast<const uint8_t *>(w->p), nullptr, (int32_t)nb, 0, w->ld * 2, N};
+    g.chunks = (int32_t)chunks;
+    g.cols = (int32_t)K;
+    HIP_TRY(c, (nt_product<1, 1, NT_ROWS>(g, out, reinterpret_cast<float *>(ws->base), c->stream)));
+    return op_end(c);
+  }
   const size_t xb = (size_t)mb * chunks * P * FRAG, wb = (size_t)nb * chunks * P * FRAG, pb = room(bf16, M, N, chunks);
   Workspace *ws = nullptr;
   TRY(op_space(c, al(xb) + al(wb) + al(pb) + 256, &ws));

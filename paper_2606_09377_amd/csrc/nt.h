@@ -12,6 +12,12 @@
 // first to fourth eight columns of each of its blocks of 32, so that the 16 bytes a lane has of a 4-bit fragment
 // are its columns of four instructions in turn; they become bf16 in registers, exactly, where they are multiplied.
 //
+// bf16 operands may also be as a program has them (NT_ROWS): rows of a pitch, 16-byte aligned, of a multiple of 8 columns.  A wave-wide load
+// then takes 16 / KS rows' 64 KS bytes, whole lines from two chunks a stage on, into LDS rows of 64 KS bytes, whose 16-byte pieces change
+// places within their row by the row's number (the permutation is applied to the addresses that are read from memory), so that the 16 lanes that LDS
+// serves together read from all banks.  Rows beyond the last one and pieces beyond the last column are read in the place of those, and the
+// columns zeroed in registers.
+//
 // Parts.  float32 values are three bf16 parts h + m + l (split_bf16.h); P parts keep 8 P bits.  Products of
 // (A parts, B parts), in order of their size:
 //   (1, 1)  h h
@@ -56,6 +62,7 @@ struct NtOperand {
   const uint8_t *scales;
   int32_t row_blocks;
   int64_t stride;   // bytes from one matrix of a batch to the next
+  int64_t pitch, rows;   // NT_ROWS: bytes from one row to the next, rows
 };
 struct NtArgs {
   NtOperand A, B;
@@ -65,14 +72,16 @@ struct NtArgs {
   // Tiles are counted in a shape of bm x bn, n_mt x n_nt of them and `tiles` in use per matrix of a batch.  A
   // launch takes those from `first` on, each as sub_m x sub_n of its own.
   int32_t bm, bn, n_mt, n_nt, tiles, first, sub_m, sub_n;
+  int32_t cols;         // NT_ROWS: columns of the contraction
 };
 
-enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2 };   // both bf16, both 4-bit, A bf16 (grouped) and B 4-bit
+enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2, NT_ROWS = 3 };   // both bf16, both 4-bit, A bf16 (grouped) and B 4-bit, both rows of bf16
 
 template <int KIND_, int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_>
 struct NtTile {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, PA = PA_, PB = PB_, KS = KS_, NS = NS_;
-  static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED;
+  static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED, ROWS = KIND_ == NT_ROWS;
+  static constexpr int PIECES = 4 * KS_;   // NT_ROWS: 16-byte pieces of a stage's row
   static constexpr int PRODUCTS = PA == 3 ? (PB == 3 ? 6 : 3) : 1;
   static constexpr int KW = KS / WK;   // chunks of a stage that a wave multiplies
   static constexpr int NW = WM * WN * WK, T = 64 * NW;
@@ -89,6 +98,9 @@ struct NtTile {
   static_assert(!MIXED || (KS == 4 && PB == 1), "a stage is a group");
   static_assert(KS % WK == 0 && (WK == 1 || NW * MB * NB * 1024 <= LDS), "waves that share a block");
   static_assert(KW == 1 || KW % 2 == 0, "register sets alternate");
+  static_assert(!ROWS || (PA == 1 && PB == 1 && (KS & (KS - 1)) == 0 && KS <= 4), "rows of one part");
+  // NT_ROWS: where piece p of row r (of 16) lies in its row
+  static __device__ __forceinline__ int place(int r, int p) { return p ^ (r / (4 / KS) & (PIECES - 1)); }
 };
 
 // 16 (wide) or 4 bytes a lane, at a 32-bit offset from a wave-uniform base, into LDS at lane times that many (dma16's form)
@@ -190,13 +202,18 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   // formed once (32 bits: launch_nt).  Row blocks beyond the last one read that.  (Forming the addresses anew for every
   // load cost a wave that has its SIMD to itself as much time as its products.)
   const int b_chunks = T::MIXED ? g.chunks / 4 : g.chunks, bk0 = T::MIXED ? kc0 / 4 : kc0;   // B's fragments of a row block
-  const uint8_t *a_base = g.A.p + batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG;
-  const uint8_t *b_base = g.B.p + batch * g.B.stride + ((int64_t)cb0 * b_chunks + bk0) * PB * FRAG;
+  const uint8_t *a_base = g.A.p + (T::ROWS ? 16 * rb0 * g.A.pitch + (int64_t)kc0 * 64 : batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG);
+  const uint8_t *b_base = g.B.p + (T::ROWS ? 16 * cb0 * g.B.pitch + (int64_t)kc0 * 64 : batch * g.B.stride + ((int64_t)cb0 * b_chunks + bk0) * PB * FRAG);
   uint32_t f_off[T::FQ];
 #pragma unroll
   for (int q = 0; q < T::FQ; ++q) {
     const int f = min(q * NW + wave, T::FA + T::FB - 1);
-    if (f < T::FA) {   // wave-uniform
+    if constexpr (T::ROWS) {
+      const int g0 = f < T::FA ? f : f - T::FA, r = g0 % KS * (16 / KS) + lane / T::PIECES, row = g0 / KS * 16 + r;
+      const NtOperand &o = f < T::FA ? g.A : g.B;
+      const int64_t first = 16 * (int64_t)(f < T::FA ? rb0 : cb0);
+      f_off[q] = (uint32_t)((min(first + row, o.rows - 1) - first) * o.pitch) + T::place(r, lane % T::PIECES) * 16;
+    } else if (f < T::FA) {   // wave-uniform
       const int i = f / (KS * PA);
       f_off[q] = ((uint32_t)min(i, g.A.row_blocks - 1 - rb0) * g.chunks * PA + (f - i * (KS * PA))) * FRAG + lane * 16;
     } else {
@@ -221,10 +238,11 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     const uint8_t *a, *b;
     uint32_t lds;
     int at4, over;   // over: chunks of the stage beyond the contraction
+    int first;       // NT_ROWS: its first piece
   };
   auto stage = [&](int kt, int buf) {
-    return Stage{a_base + (int64_t)kt * (KS * PA * FRAG), b_base + (int64_t)kt * (T::BF * FRAG), lds0 + buf * T::STAGE,
-                 (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS)};
+    return Stage{a_base + (int64_t)kt * (T::ROWS ? KS * 64 : KS * PA * FRAG), b_base + (int64_t)kt * (T::ROWS ? KS * 64 : T::BF * FRAG), lds0 + buf * T::STAGE,
+                 (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS), (kc0 + kt * KS) * 4};
   };
   auto load = [&](const Stage &s, int q, auto last) {   // load q < LOADS of this wave
     if (q < T::FQ) {
@@ -232,8 +250,13 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       const bool is_a = (q + 1) * NW <= T::FA || (q * NW < T::FA && f < T::FA);
       uint32_t off = f_off[q];
       if constexpr (decltype(last)::value) {   // the contraction's last chunk is read in the place of those beyond it
-        const int P = is_a ? PA : PB, kc = (is_a ? f : f - T::FA) % (KS * P) / P;
-        off -= max(0, kc - (KS - s.over - 1)) * (P * FRAG);
+        if constexpr (T::ROWS) {   // (of columns: its last piece)
+          const int r = (is_a ? f : f - T::FA) % KS * (16 / KS) + lane / T::PIECES;
+          off -= max(0, s.first + T::place(r, lane % T::PIECES) - ((g.cols >> 3) - 1)) * 16;
+        } else {
+          const int P = is_a ? PA : PB, kc = (is_a ? f : f - T::FA) % (KS * P) / P;
+          off -= max(0, kc - (KS - s.over - 1)) * (P * FRAG);
+        }
       }
       nt_dma(is_a ? s.a : s.b, off, s.lds + f * FRAG, true);
     } else if constexpr (SCALES) {
@@ -243,7 +266,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   };
   auto issue = [&](int kt, int buf) {
     const Stage s = stage(kt, buf);
-    if (KS == 1 || T::MIXED || s.over <= 0) {
+    if (!T::ROWS && (KS == 1 || T::MIXED || s.over <= 0)) {
 #pragma unroll
       for (int q = 0; q < T::LOADS; ++q) load(s, q, std::false_type{});
     } else {
@@ -270,7 +293,12 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   struct Codes {
     uint32_t w[NB][CW], s[NB];
   };
+  auto row_at = [&](int blk, int kc) { return blk * (KS * FRAG) + (lane & 15) * (KS * 64) + T::place(lane & 15, kc * 4 + (lane >> 4)) * 16; };
   auto read_a = [&](Chunk &c, int kt, const uint8_t *st, int kc, int i, int p) {
+    if constexpr (T::ROWS) {
+      c.a[i][p] = *reinterpret_cast<const bf16x8 *>(st + row_at(wm * MB + i, kc));
+      return;
+    }
     c.a[i][p] = *reinterpret_cast<const bf16x8 *>(st + (((wm * MB + i) * KS + kc) * PA + p) * FRAG + lane * 16);
     if constexpr (T::FP4) {
       const uint32_t *s = reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG) + lane;
@@ -278,6 +306,10 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     }
   };
   auto read_b = [&](Chunk &c, int kt, const uint8_t *st, int kc, int j, int p) {
+    if constexpr (T::ROWS) {
+      c.b[j][p] = *reinterpret_cast<const bf16x8 *>(st + T::FA * FRAG + row_at(wn * NB + j, kc));
+      return;
+    }
     c.b[j][p] = *reinterpret_cast<const bf16x8 *>(st + (T::FA + ((wn * NB + j) * KS + kc) * PB + p) * FRAG + lane * 16);
     if constexpr (T::FP4) {
       const uint32_t *s = reinterpret_cast<const uint32_t *>(st + (T::FA + T::FB) * FRAG) + lane;
@@ -394,10 +426,19 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     const int left = kc1 - kc0 - kt * KS;
 #pragma unroll
     for (int k = 0; k < KW; ++k) {
-      const Chunk &now = set[(SP * KW + k) & 1];
+      Chunk &now = set[(SP * KW + k) & 1];
       Chunk &next = set[(SP * KW + k + 1) & 1];
       const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
       arrived();
+      if constexpr (T::ROWS) {   // columns beyond the last one (which may be anything, in both operands)
+        const int col = (kc0 + kt * KS + k * T::WK + wk) * 32 + (lane >> 4) * 8;
+        if (col >= g.cols) {
+#pragma unroll
+          for (int i = 0; i < MB; ++i) now.a[i][0] = bf16x8{};
+#pragma unroll
+          for (int j = 0; j < NB; ++j) now.b[j][0] = bf16x8{};
+        }
+      }
       if (k + 1 == KW && nkt < KT) {
         landed(nkt, NS - 2);
         barrier_only();
@@ -623,7 +664,9 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
   g.sub_n = bn / T::BN;
   const int64_t grid = count * g.sub_m * g.sub_n;
   // (a tile's row blocks are reached by 32-bit offsets)
-  if ((int64_t)g.chunks * 3 * FRAG * (std::max(T::BM, T::BN) / 16) > 0xffffffffll) return hipErrorInvalidValue;
+  if (T::ROWS ? std::max(g.A.pitch, g.B.pitch) * std::max(T::BM, T::BN) > 0xffffffffll
+              : (int64_t)g.chunks * 3 * FRAG * (std::max(T::BM, T::BN) / 16) > 0xffffffffll)
+    return hipErrorInvalidValue;
   if (mt <= 0 || nt <= 0 || g.chunks <= 0 || tiles > 0x7fffffff || grid <= 0 || grid > 0x7fffffff || first + count > 0x7fffffff ||
       g.sub_m * T::BM != bm || g.sub_n * T::BN != bn || parts <= 0 || parts > 65535)
     return hipErrorInvalidValue;
@@ -670,6 +713,15 @@ struct NtTiles<1, 1, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
   typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
   typedef NtTile<NT_BF16, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
+  static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
+};
+template <>
+struct NtTiles<1, 1, NT_ROWS> {
+  typedef NtTile<NT_ROWS, 8, 4, 2, 4, 1, 1, 1, 2, 2> T0;
+  typedef NtTile<NT_ROWS, 4, 4, 2, 2, 1, 1, 1, 2, 2> T1;
+  typedef NtTile<NT_ROWS, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
+  typedef NtTile<NT_ROWS, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
+  typedef NtTile<NT_ROWS, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
   static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
 template <>
