@@ -23,16 +23,36 @@ struct DenseOut {
   float factor;        // of the sums
   DropDev drop;
   float bytes() const { return (y.bf16 ? 2.f : 4.f) + (z.p ? z.bf16 ? 2.f : 4.f : 0.f) + (res.p ? res.bf16 ? 2.f : 4.f : 0.f); }
-  __device__ __forceinline__ void store8(int64_t m, int64_t n, float (&v)[8]) const {
-    if (m >= rows || n >= cols) return;
-    if (factor != 1.f) {
+  struct Col {
+    float bias[8];
+    uint64_t offset;
+  };
+  typedef Octet Pre;   // of the residual
+  __device__ __forceinline__ Col col(int64_t n) const {
+    Col c;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= factor;
-    }
+    for (int i = 0; i < 8; ++i) c.bias[i] = 0.f;
     if (bias) {
+      if (n + 8 <= cols) {
+        __builtin_memcpy(c.bias, __builtin_assume_aligned(bias + n, 4), 32);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += n + i < cols ? bias[n + i] : 0.f;
+        for (int i = 0; i < 8; ++i)
+          if (n + i < cols) c.bias[i] = bias[n + i];
+      }
     }
+    c.offset = drop.k ? drop_offset(drop) : 0;
+    return c;
+  }
+  __device__ __forceinline__ Pre pre(int64_t m, int64_t n) const {
+    Pre p{};
+    if (res.p && m < rows && n < cols) p = load_octet(res, m, n, cols);
+    return p;
+  }
+  __device__ __forceinline__ void store8(int64_t m, int64_t n, float (&v)[8], const Col &c, const Pre &p) const {
+    if (m >= rows || n >= cols) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], factor, c.bias[i]);
     if (z.p) save8(z, m, n, cols, v);
     if (act != VCR_ACT_NONE) {
 #pragma unroll
@@ -41,11 +61,11 @@ struct DenseOut {
     if (drop.k) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= drop.factor;
-      drop8(drop, drop_offset(drop), m, n, v);
+      drop8(drop, c.offset, m, n, v);
     }
     if (res.p) {
       float a[8];
-      load8(res, m, n, cols, a);
+      octet_values(res, p, a);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += a[i];
     }
@@ -280,7 +300,7 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
       d[1] = b;
     } else {
       float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      o.store8(m, n, v);
+      o.store8(m, n, v, o.col(n), o.pre(m, n));
     }
   }
 }
@@ -292,8 +312,7 @@ struct DenseRows {
 static DenseRows dense_rows(bool bf16, int64_t M, int64_t N, int64_t K) {
   DenseRows p{};
   const int64_t blocks = blocks_of(N, 16);
-  const char *e = getenv("DR");
-  p.nb = e ? atoi(e) : blocks >= 512 ? 2 : 1;
+  p.nb = M > 8 && blocks >= 512 ? 2 : 1;
   p.u = bf16 ? (M <= 16 ? 4 : 2) : M <= 16 ? 2 : 1;
   p.wgs = blocks_of(blocks, p.nb);
   const int64_t groups = blocks_of(K, 32 * p.u), bytes = 16 * p.nb * K * (bf16 ? 2 : 4);
@@ -320,7 +339,7 @@ static hipError_t launch_dense_rows(const DevMat &x, const DevMat &w, const Dens
 
 static DevMat dev(const vcr_mat *m) { return DevMat{m->p, m->type == VCR_BF16, m->rows, m->cols, m->ld, 0}; }
 static size_t room(bool bf16, int64_t M, int64_t N, int64_t chunks) {
-  return bf16 ? part_bytes<1, 1, NT_BF16>(M, N, chunks) : part_bytes<3, 3, NT_BF16>(M, N, chunks);
+  return bf16 ? part_bytes<1, 1, NT_BF16, 32>(M, N, chunks) : part_bytes<3, 3, NT_BF16, 32>(M, N, chunks);
 }
 static hipError_t product(bool bf16, const uint8_t *a, int64_t arb, const uint8_t *b, int64_t brb, int64_t chunks, const DenseOut &o, float *part,
                           hipStream_t s) {
@@ -328,9 +347,29 @@ static hipError_t product(bool bf16, const uint8_t *a, int64_t arb, const uint8_
   g.A = NtOperand{a, nullptr, (int32_t)arb, 0};
   g.B = NtOperand{b, nullptr, (int32_t)brb, 0};
   g.chunks = (int32_t)chunks;
-  return bf16 ? nt_product<1, 1, NT_BF16>(g, o, part, s) : nt_product<3, 3, NT_BF16>(g, o, part, s);
+  return bf16 ? nt_product<1, 1, NT_BF16, 32>(g, o, part, s) : nt_product<3, 3, NT_BF16, 32>(g, o, part, s);
 }
 
+// Up to 64 rows of bf16: tiles of all the rows and 32 columns, whose waves divide the contraction, with as many stages in flight as memory takes to answer
+struct SkinnyTiles {
+  typedef NtTile<NT_ROWS, 1, 2, 1, 1, 4, 1, 1, 4, 6> R16;
+  typedef NtTile<NT_ROWS, 2, 2, 1, 1, 4, 1, 1, 4, 6> R32;
+  typedef NtTile<NT_ROWS, 4, 2, 1, 1, 4, 1, 1, 4, 4> R64;
+};
+// Taken where there are about enough such tiles for the chip, so that dividing the contraction would only add a launch, or where the
+// contraction is short (this way and by the plan, us a call with weights from memory: 1 x 8192 x 8192 29.0 and 31.3, 64 x 8192 x 8192 34.4 and 36.7,
+// 64 x 4096 x 4096 16.8 and 18.1, 16 x 2048 x 2048 7.9 and 10.4; 16 x 8192 x 2048 17.6 and 12.5, 64 x 1024 x 65536 54 and 30).
+static bool skinny(int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = blocks_of(N, 32);
+  return M <= 64 && (tiles >= 128 || K <= 2048) && (tiles <= 512 || M <= 16);
+}
+static hipError_t skinny_product(const NtArgs &g, const DenseOut &o, hipStream_t s) {
+  auto go = [&](auto t) {
+    typedef decltype(t) T;
+    return launch_nt<T>(g, o.rows, o.cols, T::BM, T::BN, 0, nt_tiles(o.rows, o.cols, T::BM, T::BN, false), 1, EpiOut<DenseOut>{o}, s);
+  };
+  return o.rows <= 16 ? go(SkinnyTiles::R16{}) : o.rows <= 32 ? go(SkinnyTiles::R32{}) : go(SkinnyTiles::R64{});
+}
 // bf16 operands that the tiles take as they are (nt.h)
 static bool rows_product(const vcr_mat *x, const vcr_mat *w) {
   return x->cols % 8 == 0 && rows_aligned(x->p, x->ld, 2) && rows_aligned(w->p, w->ld, 2) && std::max(x->ld, w->ld) < (int64_t)1 << 22;
@@ -386,7 +425,8 @@ vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_
   const bool bf16 = x->type == VCR_BF16;
   const int P = bf16 ? 1 : 3;
   const DenseOut out{mat_ref(y), mat_ref(o.z), mat_ref(o.residual), o.bias, M, N, o.act, 1.f, drop_dev(o.drop)};
-  if (M <= (getenv("DRM") ? atoi(getenv("DRM")) : 64)) {
+  const bool as_stored = bf16 && rows_product(x, w);
+  if (as_stored ? M <= 8 && N * K <= (int64_t)1 << 24 : M <= 64) {
     const DenseRows p = dense_rows(bf16, M, N, K);
     Workspace *ws = nullptr;
     TRY(op_space(c, p.part_bytes, &ws));
@@ -396,16 +436,19 @@ vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_
     return op_end(c);
   }
   const int64_t chunks = blocks_of(K, 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16);
-  if (bf16 && rows_product(x, w) && !getenv("NOROWS")) {
-    const size_t pb = part_bytes<1, 1, NT_ROWS>(M, N, chunks);
-    Workspace *ws = nullptr;
-    TRY(op_space(c, pb, &ws));
+  if (as_stored) {
     NtArgs g{};
     g.A = NtOperand{static_cast<const uint8_t *>(x->p), nullptr, (int32_t)mb, 0, x->ld * 2, M};
     g.B = NtOperand{static_cast<const uint8_t *>(w->p), nullptr, (int32_t)nb, 0, w->ld * 2, N};
     g.chunks = (int32_t)chunks;
     g.cols = (int32_t)K;
-    HIP_TRY(c, (nt_product<1, 1, NT_ROWS>(g, out, reinterpret_cast<float *>(ws->base), c->stream)));
+    if (skinny(M, N, K)) {
+      HIP_TRY(c, skinny_product(g, out, c->stream));
+      return op_end(c);
+    }
+    Workspace *ws = nullptr;
+    TRY(op_space(c, part_bytes<1, 1, NT_ROWS, 32>(M, N, chunks), &ws));
+    HIP_TRY(c, (nt_product<1, 1, NT_ROWS, 32>(g, out, reinterpret_cast<float *>(ws->base), c->stream)));
     return op_end(c);
   }
   const size_t xb = (size_t)mb * chunks * P * FRAG, wb = (size_t)nb * chunks * P * FRAG, pb = room(bf16, M, N, chunks);

@@ -168,9 +168,10 @@ __device__ __forceinline__ void nt_tile(const NtArgs &g, int id, int total, int 
 // EPI: a struct with store(batch, part of the contraction, m, n, values of n .. n + 3, lane): called by
 // whole waves for every block, with the lane's row m and first column n; the other lanes of a block hold
 // its other rows and columns.
-// One with STAGED has store8(m, n, values of n .. n + 7) instead: the tile goes through LDS, so that a wave has whole
-// stretches of rows (an epilogue that reads other matrices, or writes two, then moves whole lines, and its code is there once
-// and not for every block of a wave).
+// One with STAGED is given eight columns of a row instead: the tile goes through LDS, so that a wave has whole stretches of rows
+// (an epilogue that reads other matrices, or writes two, then moves whole lines, and its code is there once and not for every
+// block of a wave).  Col col(n): what it takes of columns n .. n + 7, asked for once; Pre pre(m, n): what it reads of a row there, asked for
+// a pass ahead; store8(m, n, values, col, pre).
 template <class EPI, class = void>
 struct nt_staged : std::false_type {};
 template <class EPI>
@@ -352,12 +353,14 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     }
   };
   auto landed = [&](int kt, int later) {   // this wave's loads of stage kt, with `later` stages issued after it
-    if (later > 1 && kt + later < KT) wait_vmcnt<2 * T::LOADS>();
+    if (NS > 5 && later > 3 && kt + 4 < KT) wait_vmcnt<4 * T::LOADS>();
+    else if (NS > 4 && later > 2 && kt + 3 < KT) wait_vmcnt<3 * T::LOADS>();
+    else if (later > 1 && kt + 2 < KT) wait_vmcnt<2 * T::LOADS>();
     else if (later > 0 && kt + 1 < KT) wait_vmcnt<T::LOADS>();
     else wait_vmcnt<0>();
   };
 
-  static_assert(NS >= 2 && NS <= 4, "at most two stages in flight behind the one waited for");
+  static_assert(NS >= 2 && NS <= 6, "at most four stages in flight behind the one waited for");
   // A wave's chunks in turn: chunk k of stage kt is multiplied while the operands of the next one are read.  With the last
   // chunk of a stage, stage kt + 1 has landed; the barrier publishes it and frees stage kt, whose operands every wave has
   // in registers, for stage kt + NS.  (Two register sets, and the loop takes two stages at a time, so that none is copied.)
@@ -465,7 +468,9 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     for (int t = 0; t < NS; ++t)
       if (t < KT) issue(t, t);
     // stage 0, with up to NS - 1 behind it
-    if (NS > 3 && KT > 3) wait_vmcnt<3 * T::LOADS>();
+    if (NS > 5 && KT > 5) wait_vmcnt<5 * T::LOADS>();
+    else if (NS > 4 && KT > 4) wait_vmcnt<4 * T::LOADS>();
+    else if (NS > 3 && KT > 3) wait_vmcnt<3 * T::LOADS>();
     else if (NS > 2 && KT > 2) wait_vmcnt<2 * T::LOADS>();
     else if (KT > 1) wait_vmcnt<T::LOADS>();
     else wait_vmcnt<0>();
@@ -498,31 +503,52 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     if constexpr (!nt_staged<EPI>::value) epi.store(batch, blockIdx.y, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
   };
   if constexpr (nt_staged<EPI>::value) {
-    constexpr int PITCH = T::BN + 4;
+    constexpr int PITCH = T::BN + 4, IB = T::WK == 1 ? nt_stage_blocks<T>() : MB;   // row blocks of a wave in a pass
+    constexpr int OCTS = T::BN / 8, STEP = T::T / OCTS, HELD = T::WM * IB * 16, ITEMS = (HELD + STEP - 1) / STEP;
+    static_assert(T::T % OCTS == 0 && (HELD % STEP == 0 || ITEMS == 1), "whole rows for every thread");
     float *tile = reinterpret_cast<float *>(lds);
-    auto rows_out = [&](int per, int i0) {   // the tile's rows i0 .. i0 + per of every wave, as they lie in LDS
+    const int oct = threadIdx.x % OCTS, row0 = threadIdx.x / OCTS, n_at = 16 * cb0 + oct * 8;
+    auto row_of = [&](int pass, int it) {   // of a thread's item: its row in the tile as it lies in LDS, and in the result
+      const int q = row0 + it * STEP, w = q / (16 * IB);
+      return 16 * (rb0 + w * MB + pass * IB) + q - w * (16 * IB);
+    };
+    typename EPI::Pre pre[2][ITEMS];
+    const typename EPI::Col col = epi.col(n_at);
+    auto ahead = [&](auto pass) {
+#pragma unroll
+      for (int it = 0; it < ITEMS; ++it)
+        if (HELD % STEP == 0 || row0 < HELD) pre[decltype(pass)::value & 1][it] = epi.pre(row_of(pass, it), n_at);
+    };
+    auto rows_out = [&](auto pass) {
       __syncthreads();
-      for (int at = threadIdx.x; at < T::WM * per * (T::BN / 8); at += T::T) {
-        const int q = at / (T::BN / 8), c = at - q * (T::BN / 8), w = q / per, r = q - w * per;
-        const float *s = tile + q * PITCH + c * 8;
+      if constexpr (decltype(pass)::value + 1 < MB / IB) ahead(std::integral_constant<int, decltype(pass)::value + 1>{});
+#pragma unroll
+      for (int it = 0; it < ITEMS; ++it) {
+        if (HELD % STEP != 0 && row0 >= HELD) continue;
+        const float *s = tile + (row0 + it * STEP) * PITCH + oct * 8;
         const f32v4 a = *reinterpret_cast<const f32v4 *>(s), b = *reinterpret_cast<const f32v4 *>(s + 4);
         float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        epi.store8(16 * (rb0 + w * MB) + i0 + r, 16 * cb0 + c * 8, v);
+        epi.store8(row_of(pass, it), n_at, v, col, pre[decltype(pass)::value & 1][it]);
       }
     };
+    ahead(std::integral_constant<int, 0>{});
     if constexpr (T::WK == 1) {
-      constexpr int IB = nt_stage_blocks<T>();
       static_assert(IB * T::WM * 16 * PITCH * 4 <= T::LDS, "rows of a tile in LDS");
-#pragma unroll
-      for (int p = 0; p < MB / IB; ++p) {
+      auto pass = [&](auto at) {
+        constexpr int p = decltype(at)::value;
         barrier_only();   // what LDS held has been read
 #pragma unroll
         for (int i = 0; i < IB; ++i)
 #pragma unroll
           for (int j = 0; j < NB; ++j)
             *reinterpret_cast<f32v4 *>(tile + ((wm * IB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = joined(p * IB + i, j);
-        rows_out(16 * IB, p * IB * 16);
-      }
+        rows_out(at);
+      };
+      pass(std::integral_constant<int, 0>{});
+      if constexpr (MB / IB > 1) pass(std::integral_constant<int, 1>{});
+      if constexpr (MB / IB > 2) pass(std::integral_constant<int, 2>{});
+      if constexpr (MB / IB > 3) pass(std::integral_constant<int, 3>{});
+      static_assert(MB / IB <= 4, "passes");
     } else {
       constexpr int B = MB * NB, PER = (B + T::WK - 1) / T::WK;
       static_assert(T::BM * PITCH * 4 <= T::LDS, "the tile in LDS");
@@ -547,7 +573,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
         const int blk = n * T::WK + wk, i = blk / NB, j = blk - i * NB;
         if (blk < B) *reinterpret_cast<f32v4 *>(tile + ((wm * MB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = sum[n];
       }
-      rows_out(16 * MB, 0);
+      rows_out(std::integral_constant<int, 0>{});
     }
   } else if constexpr (T::WK == 1) {
 #pragma unroll

@@ -1,7 +1,7 @@
 // Products by the tiles of nt.h into a matrix, the contraction divided where that pays.  Part of layers.hip and dense.hip.
 //
 // OUT: where results go.  rows, cols, bytes() that an output takes, and put(m, n, values of n .. n + 3), or with STAGED
-// store8(m, n, values of n .. n + 7) (nt.h).
+// col, pre and store8 of eight columns (nt.h).
 #pragma once
 
 #include "planes.h"
@@ -16,8 +16,12 @@ struct EpiOut {
 template <class OUT>
 struct EpiOut<OUT, std::enable_if_t<OUT::STAGED>> {
   static constexpr bool STAGED = true;
+  typedef typename OUT::Col Col;
+  typedef typename OUT::Pre Pre;
   OUT o;
-  __device__ __forceinline__ void store8(int m, int n, float (&v)[8]) const { o.store8(m, n, v); }
+  __device__ __forceinline__ Col col(int n) const { return o.col(n); }
+  __device__ __forceinline__ Pre pre(int m, int n) const { return o.pre(m, n); }
+  __device__ __forceinline__ void store8(int m, int n, float (&v)[8], const Col &c, const Pre &p) const { o.store8(m, n, v, c, p); }
 };
 // sums over one part of the contraction, [parts][rows][ld]
 struct EpiPart {
@@ -37,26 +41,28 @@ static __global__ __launch_bounds__(256) void k_join(const float *p, int parts, 
   for (int q = 0; q < W; ++q) {
     v[q] = f32v4{0.f, 0.f, 0.f, 0.f};
     if (q == 0 || n + 4 * q < ld)
+#pragma unroll 4
       for (int z = 0; z < parts; ++z) v[q] += *reinterpret_cast<const f32v4 *>(p + (z * rows + m) * ld + n + 4 * q);
   }
   if constexpr (W == 1) {
     o.put(m, n, v[0]);
   } else {
     float x[8] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
-    o.store8(m, n, x);
+    o.store8(m, n, x, o.col(n), o.pre(m, n));
   }
 }
 
-template <int PA, int PB, int KIND>
+// MOST: parts of the contraction
+template <int PA, int PB, int KIND, int MOST = NT_CUS>
 static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
-  const int parts = nt_parts<NtTiles<PA, PB, KIND>>(M, N, chunks);
+  const int parts = std::min(MOST, nt_parts<NtTiles<PA, PB, KIND>>(M, N, chunks));
   return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
 }
 // D = A B^T into o; part: room for part_bytes
-template <int PA, int PB, int KIND, class OUT>
+template <int PA, int PB, int KIND, int MOST = NT_CUS, class OUT>
 static hipError_t nt_product(const NtArgs &g, const OUT &o, float *part, hipStream_t s) {
   typedef NtTiles<PA, PB, KIND> TS;
-  const int parts = nt_parts<TS>(o.rows, o.cols, g.chunks);
+  const int parts = std::min(MOST, nt_parts<TS>(o.rows, o.cols, g.chunks));
   if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, o.bytes(), EpiOut<OUT>{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
   const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
