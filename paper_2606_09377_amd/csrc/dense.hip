@@ -113,6 +113,52 @@ __global__ __launch_bounds__(256) void k_dense_planes(PlanesOf a, PlanesOf b, Pl
   }
   planes_cols<P>(p, tr, tc, v, tile);
 }
+// g = the kept values of dy times the activation's slope as rows of bf16 (out null: not stored), and the sums of its columns over every 64
+// rows, sums [group][cols] (null: none; of one group: times `factor`, what is asked for).  A workgroup takes 64 x 64 values, a
+// thread eight columns of two rows.  Bound by memory.
+__global__ __launch_bounds__(256) void k_grad_rows(DevMat dy, int vec, GradSource src, uint16_t *out, int64_t pitch, float *sums, float factor, int64_t first) {
+  __shared__ float part[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, oct = threadIdx.x & 7;
+  const int64_t ct = (dy.cols + 63) / 64, id = first + blockIdx.x, tr = id / ct, tc = id - tr * ct, col = tc * 64 + oct * 8, row0 = tr * 64 + (threadIdx.x >> 3);
+  float v[2][8], z[2][8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    mat_row8<true>(dy, 0, row0 + 32 * i, col, vec, v[i]);
+    if (src.act != VCR_ACT_NONE && row0 + 32 * i < dy.rows && col < dy.cols) load8(src.z, row0 + 32 * i, col, dy.cols, z[i]);
+  }
+  const uint64_t offset = src.drop.k ? drop_offset(src.drop) : 0;
+  float s[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s[k] = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t row = row0 + 32 * i;
+    if (row >= dy.rows || col >= dy.cols) continue;
+    if (src.act != VCR_ACT_NONE) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = src.act == VCR_ACT_RELU ? (z[i][k] > 0.f ? v[i][k] : 0.f) : v[i][k] * act_slope(src.act, z[i][k]);
+    }
+    if (src.drop.k) drop8(src.drop, offset, row, col, v[i]);
+    if (out) *reinterpret_cast<uint4 *>(out + row * pitch + col) = pack8(v[i]);   // (zeros beyond the columns, up to the pitch)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k] += v[i][k];
+  }
+  if (!sums) return;   // uniform
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {   // over a wave's 8 rows
+    s[k] += __shfl_xor(s[k], 8);
+    s[k] += __shfl_xor(s[k], 16);
+    s[k] += __shfl_xor(s[k], 32);
+  }
+  if (lane < 8) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) part[wave][lane * 8 + k] = s[k];
+  }
+  __syncthreads();
+  const int64_t c = tc * 64 + threadIdx.x;
+  if (threadIdx.x < 64 && c < dy.cols)
+    sums[tr * dy.cols + c] = factor * ((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+}
 static PlanesOf planes_of(const PlanesArgs *p) {
   PlanesOf o{};
   if (!p) return o;
@@ -370,10 +416,9 @@ static hipError_t skinny_product(const NtArgs &g, const DenseOut &o, hipStream_t
   };
   return o.rows <= 16 ? go(SkinnyTiles::R16{}) : o.rows <= 32 ? go(SkinnyTiles::R32{}) : go(SkinnyTiles::R64{});
 }
-// bf16 operands that the tiles take as they are (nt.h)
-static bool rows_product(const vcr_mat *x, const vcr_mat *w) {
-  return x->cols % 8 == 0 && rows_aligned(x->p, x->ld, 2) && rows_aligned(w->p, w->ld, 2) && std::max(x->ld, w->ld) < (int64_t)1 << 22;
-}
+// bf16 matrices that the tiles take as they are (nt.h)
+static bool rows_operand(const vcr_mat *m) { return m->cols % 8 == 0 && rows_aligned(m->p, m->ld, 2) && m->ld < (int64_t)1 << 22; }
+static bool rows_product(const vcr_mat *x, const vcr_mat *w) { return rows_operand(x) && rows_operand(w); }
 
 }  // namespace vcr
 
@@ -399,6 +444,52 @@ static vcr_status check_rows(vcr_ctx *c, int64_t rows) {
   if (rows > VCR_MAX_LINEAR_ROWS)
     return fail(c, VCR_ERR_UNSUPPORTED, "%lld rows exceed the limit of %lld", (long long)rows, (long long)VCR_MAX_LINEAR_ROWS);
   return VCR_OK;
+}
+
+// The gradients of bf16 matrices that the tiles take as they are, M > 0: g is written out where it is not dy itself
+static vcr_status grad_of_rows(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts &o, const vcr_mat *add,
+                               const vcr_mat *dx, const vcr_mat *dw, float *db) {
+  const int64_t M = dy->rows, N = dy->cols, K = dx ? w->cols : dw ? x->cols : 1, mg = blocks_of(M, 64), nch = blocks_of(N, 32), mch = blocks_of(M, 32);
+  const DropDev drop = drop_dev(o.drop), none = drop_dev(nullptr);
+  const bool store = (dx || dw) && (o.act != VCR_ACT_NONE || drop.k || !rows_operand(dy));
+  const int64_t pitch = store ? blocks_of(N, 8) * 8 : dy->ld;
+  const size_t b_g = store ? (size_t)M * pitch * 2 : 0, b_sums = db && mg > 1 ? (size_t)mg * N * 4 : 0;
+  const size_t b_part = std::max(dx ? part_bytes<1, 1, NT_RT, 32>(M, K, nch) : 0, dw ? part_bytes<1, 1, NT_TT, 32>(N, K, mch) : 0);
+  Workspace *ws = nullptr;
+  TRY(op_space(c, al(b_g) + al(b_sums) + al(b_part) + 3 * 256, &ws));
+  uint16_t *g = take<uint16_t>(*ws, b_g / 2);
+  float *sums = take<float>(*ws, b_sums / 4), *part = take<float>(*ws, b_part / 4);
+  const hipStream_t s = c->stream;
+  if (store || db) {
+    const GradSource src{mat_ref(o.act != VCR_ACT_NONE ? o.z : nullptr), o.act, drop};
+    const hipError_t e = launch_stretches(mg * blocks_of(N, 64), [&](int64_t first, dim3 grid) {
+      hipLaunchKernelGGL(k_grad_rows, grid, dim3(256), 0, s, dev(dy), rows_aligned(dy->p, dy->ld, 2), src, store ? g : nullptr, pitch,
+                         db ? mg > 1 ? sums : db : nullptr, mg > 1 ? 1.f : drop.factor, first);
+    });
+    HIP_TRY(c, e);
+  }
+  if (db && mg > 1) {
+    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, mg, N, drop.factor, db);
+    HIP_TRY(c, hipGetLastError());
+  }
+  const uint8_t *gp = store ? reinterpret_cast<const uint8_t *>(g) : static_cast<const uint8_t *>(dy->p);
+  if (dx) {
+    NtArgs a{};
+    a.A = NtOperand{gp, nullptr, (int32_t)blocks_of(M, 16), 0, pitch * 2, M};
+    a.B = NtOperand{static_cast<const uint8_t *>(w->p), nullptr, (int32_t)blocks_of(K, 16), 0, w->ld * 2, K};
+    a.chunks = (int32_t)nch;
+    a.cols = (int32_t)N;
+    HIP_TRY(c, (nt_product<1, 1, NT_RT, 32>(a, DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none}, part, s)));
+  }
+  if (dw) {
+    NtArgs a{};
+    a.A = NtOperand{gp, nullptr, (int32_t)blocks_of(N, 16), 0, pitch * 2, N};
+    a.B = NtOperand{static_cast<const uint8_t *>(x->p), nullptr, (int32_t)blocks_of(K, 16), 0, x->ld * 2, K};
+    a.chunks = (int32_t)mch;
+    a.cols = (int32_t)M;
+    HIP_TRY(c, (nt_product<1, 1, NT_TT, 32>(a, DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none}, part, s)));
+  }
+  return op_end(c);
 }
 
 extern "C" {
@@ -505,6 +596,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   TRY(op_begin(c));
   const bool bf16 = dy->type == VCR_BF16, has_dx = dx && M > 0;
   if (!has_dx && !dw && !db) return VCR_OK;
+  if (bf16 && M > 0 && (!dx || rows_operand(w)) && (!dw || rows_operand(x)) && !getenv("NOTR")) return grad_of_rows(c, dy, x, w, o, add, dx, dw, db);
   const int P = bf16 ? 1 : 3;
   const hipStream_t s = c->stream;
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;

@@ -12,11 +12,16 @@
 // first to fourth eight columns of each of its blocks of 32, so that the 16 bytes a lane has of a 4-bit fragment
 // are its columns of four instructions in turn; they become bf16 in registers, exactly, where they are multiplied.
 //
-// bf16 operands may also be as a program has them (NT_ROWS): rows of a pitch, 16-byte aligned, of a multiple of 8 columns.  A wave-wide load
-// then takes 16 / KS rows' 64 KS bytes, whole lines from two chunks a stage on, into LDS rows of 64 KS bytes, whose 16-byte pieces change
-// places within their row by the row's number (the permutation is applied to the addresses that are read from memory), so that the 16 lanes that LDS
-// serves together read from all banks.  Rows beyond the last one and pieces beyond the last column are read in the place of those, and the
-// columns zeroed in registers.
+// bf16 operands may also be as a program has them: rows of a pitch, 16-byte aligned and of a multiple of 8 columns, or of padding
+// that may be read up to one.
+//   Rows whose columns are contracted (NT_ROWS, and A of NT_RT).  A wave-wide load takes 16 / KS rows' 64 KS bytes, whole lines from two chunks a
+//   stage on, into LDS rows of 64 KS bytes, whose 16-byte pieces change places within their row by the row's number, so that the 16 lanes
+//   that LDS serves together read from all banks.
+//   Rows that are contracted (NT_TT, and B of NT_RT): operand row i is column i of the matrix.  A chunk is 32 rows' 2 BM or 2 BN bytes; a lane's
+//   eight values are two of LDS's transposing reads, each of 4 rows by 16 columns for 16 lanes, whose 32-byte pieces change places by the row's number, so
+//   that those of the 8 rows that 32 lanes read lie in different banks.
+// In both the permutation is applied to the addresses that are read from memory (a load to LDS has no other).  What lies beyond the matrix
+// is read in the place of the nearest that does not, and zeroed in registers where it would be contracted.
 //
 // Parts.  float32 values are three bf16 parts h + m + l (split_bf16.h); P parts keep 8 P bits.  Products of
 // (A parts, B parts), in order of their size:
@@ -62,7 +67,7 @@ struct NtOperand {
   const uint8_t *scales;
   int32_t row_blocks;
   int64_t stride;   // bytes from one matrix of a batch to the next
-  int64_t pitch, rows;   // NT_ROWS: bytes from one row to the next, rows
+  int64_t pitch, rows;   // as a program has them: bytes from one row of the matrix to the next, rows of the operand
 };
 struct NtArgs {
   NtOperand A, B;
@@ -72,16 +77,18 @@ struct NtArgs {
   // Tiles are counted in a shape of bm x bn, n_mt x n_nt of them and `tiles` in use per matrix of a batch.  A
   // launch takes those from `first` on, each as sub_m x sub_n of its own.
   int32_t bm, bn, n_mt, n_nt, tiles, first, sub_m, sub_n;
-  int32_t cols;         // NT_ROWS: columns of the contraction
+  int32_t cols;         // as a program has them: length of the contraction
 };
 
-enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2, NT_ROWS = 3 };   // both bf16, both 4-bit, A bf16 (grouped) and B 4-bit, both rows of bf16
+// both bf16, both 4-bit, A bf16 (grouped) and B 4-bit; bf16 as a program has them: both with contracted columns, B or both with contracted rows
+enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2, NT_ROWS = 3, NT_RT = 4, NT_TT = 5 };
 
 template <int KIND_, int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_>
 struct NtTile {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, PA = PA_, PB = PB_, KS = KS_, NS = NS_;
-  static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED, ROWS = KIND_ == NT_ROWS;
-  static constexpr int PIECES = 4 * KS_;   // NT_ROWS: 16-byte pieces of a stage's row
+  static constexpr bool FP4 = KIND_ == NT_FP4, MIXED = KIND_ == NT_MIXED, ROWS = KIND_ >= NT_ROWS;
+  static constexpr bool AT = KIND_ == NT_TT, BT = KIND_ >= NT_RT;   // contracted rows
+  static constexpr int PIECES = 4 * KS_;   // 16-byte pieces of a stage's row with contracted columns
   static constexpr int PRODUCTS = PA == 3 ? (PB == 3 ? 6 : 3) : 1;
   static constexpr int KW = KS / WK;   // chunks of a stage that a wave multiplies
   static constexpr int NW = WM * WN * WK, T = 64 * NW;
@@ -98,9 +105,13 @@ struct NtTile {
   static_assert(!MIXED || (KS == 4 && PB == 1), "a stage is a group");
   static_assert(KS % WK == 0 && (WK == 1 || NW * MB * NB * 1024 <= LDS), "waves that share a block");
   static_assert(KW == 1 || KW % 2 == 0, "register sets alternate");
-  static_assert(!ROWS || (PA == 1 && PB == 1 && (KS & (KS - 1)) == 0 && KS <= 4), "rows of one part");
-  // NT_ROWS: where piece p of row r (of 16) lies in its row
+  static_assert(!ROWS || (PA == 1 && PB == 1 && (KS & (KS - 1)) == 0 && KS <= 4 && (MB & (MB - 1)) == 0 && (NB & (NB - 1)) == 0), "rows of one part");
+  // contracted columns: where piece p of row r (of 16) lies in its row
   static __device__ __forceinline__ int place(int r, int p) { return p ^ (r / (4 / KS) & (PIECES - 1)); }
+  // contracted rows: by what the 32-byte pieces of row n of `rows` operand rows change places
+  static __device__ __forceinline__ int turn(int rows, int n) {
+    return rows >= 128 ? (n & 3) | (n >> 3 & 1) << 2 : rows == 64 ? (n >> 1 & 1) | (n >> 3 & 1) << 1 : rows == 32 ? n >> 3 & 1 : 0;
+  }
 };
 
 // 16 (wide) or 4 bytes a lane, at a 32-bit offset from a wave-uniform base, into LDS at lane times that many (dma16's form)
@@ -203,17 +214,32 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   // formed once (32 bits: launch_nt).  Row blocks beyond the last one read that.  (Forming the addresses anew for every
   // load cost a wave that has its SIMD to itself as much time as its products.)
   const int b_chunks = T::MIXED ? g.chunks / 4 : g.chunks, bk0 = T::MIXED ? kc0 / 4 : kc0;   // B's fragments of a row block
-  const uint8_t *a_base = g.A.p + (T::ROWS ? 16 * rb0 * g.A.pitch + (int64_t)kc0 * 64 : batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG);
-  const uint8_t *b_base = g.B.p + (T::ROWS ? 16 * cb0 * g.B.pitch + (int64_t)kc0 * 64 : batch * g.B.stride + ((int64_t)cb0 * b_chunks + bk0) * PB * FRAG);
+  const uint8_t *a_base = g.A.p + (T::AT ? 32 * kc0 * g.A.pitch + (int64_t)rb0 * 32 : T::ROWS ? 16 * rb0 * g.A.pitch + (int64_t)kc0 * 64 : batch * g.A.stride + ((int64_t)rb0 * g.chunks + kc0) * PA * FRAG);
+  const uint8_t *b_base = g.B.p + (T::BT ? 32 * kc0 * g.B.pitch + (int64_t)cb0 * 32 : T::ROWS ? 16 * cb0 * g.B.pitch + (int64_t)kc0 * 64 : batch * g.B.stride + ((int64_t)cb0 * b_chunks + bk0) * PB * FRAG);
   uint32_t f_off[T::FQ];
+  // contracted rows: the row of load l of br operand rows; a wave's loads of a stage are NW apart, which is a multiple of 16 rows, so that all have the
+  // lane's offset of the first, and a step apart
+  auto t_row = [&](int l, int br) { return l * (FRAG / 2 / br) + lane / (br / 8); };
+  auto t_offset = [&](const NtOperand &o, int br, int rb) {
+    const int n = t_row(wave, br), p = lane % (br / 8) ^ 2 * T::turn(br, n);
+    return (uint32_t)(n * o.pitch) + (uint32_t)min((int64_t)p, (o.rows - 1 - 16 * (int64_t)rb) / 8) * 16;
+  };
+  static_assert(!T::ROWS || (T::FA % NW == 0 && T::FB % NW == 0 && NW * (FRAG / 2 / T::BM) % 16 == 0 && NW * (FRAG / 2 / T::BN) % 16 == 0), "loads in step");
+  const uint32_t ta_off = T::AT ? t_offset(g.A, T::BM, rb0) : 0, tb_off = T::BT ? t_offset(g.B, T::BN, cb0) : 0;
+  const int64_t ta_step = T::AT ? NW * (FRAG / 2 / T::BM) * g.A.pitch : 0, tb_step = T::BT ? NW * (FRAG / 2 / T::BN) * g.B.pitch : 0;
 #pragma unroll
   for (int q = 0; q < T::FQ; ++q) {
     const int f = min(q * NW + wave, T::FA + T::FB - 1);
     if constexpr (T::ROWS) {
-      const int g0 = f < T::FA ? f : f - T::FA, r = g0 % KS * (16 / KS) + lane / T::PIECES, row = g0 / KS * 16 + r;
-      const NtOperand &o = f < T::FA ? g.A : g.B;
-      const int64_t first = 16 * (int64_t)(f < T::FA ? rb0 : cb0);
-      f_off[q] = (uint32_t)((min(first + row, o.rows - 1) - first) * o.pitch) + T::place(r, lane % T::PIECES) * 16;
+      const bool is_a = q * NW < T::FA;
+      if (is_a ? T::AT : T::BT) {
+        f_off[q] = 0;   // (t_off)
+      } else {
+        const int l = is_a ? f : f - T::FA, r = l % KS * (16 / KS) + lane / T::PIECES, row = l / KS * 16 + r;
+        const NtOperand &o = is_a ? g.A : g.B;
+        const int64_t first = 16 * (int64_t)(is_a ? rb0 : cb0);
+        f_off[q] = (uint32_t)((min(first + row, o.rows - 1) - first) * o.pitch) + T::place(r, lane % T::PIECES) * 16;
+      }
     } else if (f < T::FA) {   // wave-uniform
       const int i = f / (KS * PA);
       f_off[q] = ((uint32_t)min(i, g.A.row_blocks - 1 - rb0) * g.chunks * PA + (f - i * (KS * PA))) * FRAG + lane * 16;
@@ -239,27 +265,39 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     const uint8_t *a, *b;
     uint32_t lds;
     int at4, over;   // over: chunks of the stage beyond the contraction
-    int first;       // NT_ROWS: its first piece
+    int first;       // as a program has them: its first place in the contraction
   };
   auto stage = [&](int kt, int buf) {
-    return Stage{a_base + (int64_t)kt * (T::ROWS ? KS * 64 : KS * PA * FRAG), b_base + (int64_t)kt * (T::ROWS ? KS * 64 : T::BF * FRAG), lds0 + buf * T::STAGE,
-                 (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS), (kc0 + kt * KS) * 4};
+    return Stage{a_base + kt * (T::AT ? 32 * KS * g.A.pitch : (int64_t)(T::ROWS ? KS * 64 : KS * PA * FRAG)),
+                 b_base + kt * (T::BT ? 32 * KS * g.B.pitch : (int64_t)(T::ROWS ? KS * 64 : T::BF * FRAG)), lds0 + buf * T::STAGE,
+                 (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS), (kc0 + kt * KS) * 32};
   };
   auto load = [&](const Stage &s, int q, auto last) {   // load q < LOADS of this wave
     if (q < T::FQ) {
       const int f = min(q * NW + wave, T::FA + T::FB - 1);
       const bool is_a = (q + 1) * NW <= T::FA || (q * NW < T::FA && f < T::FA);
-      uint32_t off = f_off[q];
+      const bool rows = is_a ? T::AT : T::BT;   // contracted ones (then is_a is known for the whole q)
+      const int qi = is_a ? q : q - T::FA / NW;
+      uint32_t off = rows ? is_a ? ta_off : tb_off : f_off[q];
+      const uint8_t *base = is_a ? s.a : s.b;
+      if (T::ROWS && rows) base += qi * (is_a ? ta_step : tb_step);
       if constexpr (decltype(last)::value) {   // the contraction's last chunk is read in the place of those beyond it
-        if constexpr (T::ROWS) {   // (of columns: its last piece)
-          const int r = (is_a ? f : f - T::FA) % KS * (16 / KS) + lane / T::PIECES;
-          off -= max(0, s.first + T::place(r, lane % T::PIECES) - ((g.cols >> 3) - 1)) * 16;
+        if constexpr (T::ROWS) {   // (the last row or piece of columns)
+          const int l = is_a ? f : f - T::FA;
+          if (rows) {   // (from the stage's first row on: the lane's own may lie beyond the last)
+            const int br = is_a ? T::BM : T::BN;
+            off += (uint32_t)((min(t_row(l, br), g.cols - 1 - s.first) - t_row(wave, br)) * (is_a ? g.A.pitch : g.B.pitch));
+            base -= qi * (is_a ? ta_step : tb_step);
+          } else {
+            const int r = l % KS * (16 / KS) + lane / T::PIECES;
+            off -= max(0, s.first / 8 + T::place(r, lane % T::PIECES) - (g.cols - 1) / 8) * 16;
+          }
         } else {
           const int P = is_a ? PA : PB, kc = (is_a ? f : f - T::FA) % (KS * P) / P;
           off -= max(0, kc - (KS - s.over - 1)) * (P * FRAG);
         }
       }
-      nt_dma(is_a ? s.a : s.b, off, s.lds + f * FRAG, true);
+      nt_dma(base, off, s.lds + f * FRAG, true);
     } else if constexpr (SCALES) {
       const int i = min((q - T::FQ) * NW + wave, T::SA + T::SB - 1);
       nt_dma(s_base[q - T::FQ] + s.at4, lane * 4, s.lds + (T::FA + T::FB) * FRAG + i * 256, false);
@@ -295,7 +333,31 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     uint32_t w[NB][CW], s[NB];
   };
   auto row_at = [&](int blk, int kc) { return blk * (KS * FRAG) + (lane & 15) * (KS * 64) + T::place(lane & 15, kc * 4 + (lane >> 4)) * 16; };
+  // contracted rows of br columns: where this lane's values of the wave's first block begin (t_base; a power of two of blocks, so that
+  // block i's are at that with i's bits turned), and chunk kc of block i
+  auto t_base = [&](int br, int blk) {
+    const int n = 8 * (lane >> 4) + (lane >> 2 & 3);   // and n + 4, which turns as n
+    return (uint32_t)(n * (2 * br) + (blk ^ T::turn(br, n)) * 32 + (lane & 3) * 8);
+  };
+  uint32_t ta = T::AT ? t_base(T::BM, wm * MB) : 0, tb = T::BT ? t_base(T::BN, wn * NB) : 0;
+  auto transposed = [&](const uint8_t *st, uint32_t base, int br, int i, int kc) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef const __attribute__((address_space(3))) uint8_t *Lds;
+    const Lds at = (Lds)st + (base ^ i * 32) + kc * (64 * br);
+    s16x4 v[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + t * (8 * br)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto turned_anew = [&] {   // (the blocks' addresses are formed where they are used: kept over the loop, they would not fit the registers)
+    if constexpr (T::AT) asm volatile("" : "+v"(ta));
+    if constexpr (T::BT) asm volatile("" : "+v"(tb));
+  };
   auto read_a = [&](Chunk &c, int kt, const uint8_t *st, int kc, int i, int p) {
+    if constexpr (T::AT) {
+      c.a[i][p] = transposed(st, ta, T::BM, i, kc);
+      return;
+    }
     if constexpr (T::ROWS) {
       c.a[i][p] = *reinterpret_cast<const bf16x8 *>(st + row_at(wm * MB + i, kc));
       return;
@@ -307,6 +369,10 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     }
   };
   auto read_b = [&](Chunk &c, int kt, const uint8_t *st, int kc, int j, int p) {
+    if constexpr (T::BT) {
+      c.b[j][p] = transposed(st + T::FA * FRAG, tb, T::BN, j, kc);
+      return;
+    }
     if constexpr (T::ROWS) {
       c.b[j][p] = *reinterpret_cast<const bf16x8 *>(st + T::FA * FRAG + row_at(wn * NB + j, kc));
       return;
@@ -386,8 +452,37 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   // `now` is in registers: told to the compiler before the reads of the next set, whose end it would otherwise wait for before
   // the products of `now`
   auto arrived = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
-  auto steady = [&](int kt, auto sp) {   // stage kt (sp: its parity), kt + NS + 1 < KT
+  // as a program has them: what lies beyond the contraction in its last stage (which may be anything, in both operands) is zeroed in LDS, and the
+  // stage multiplied as the others
+  const bool whole = kc1 < g.chunks || g.cols % (32 * KS) == 0;
+  auto zero_beyond = [&](int kt) {
+    uint8_t *st = lds + kt % NS * T::STAGE;
+    const int valid = g.cols - (kc0 + kt * KS) * 32;
+    auto operand = [&](uint8_t *at, int br, bool rows) {
+      for (int it = threadIdx.x; it < br * 4 * KS; it += T::T) {   // 16-byte pieces
+        if (rows) {
+          if (it / (br / 8) >= valid) *reinterpret_cast<uint4 *>(at + it * 16) = make_uint4(0, 0, 0, 0);
+        } else {
+          const int row = it / T::PIECES, p = it % T::PIECES, left = valid - 8 * p;
+          if (left >= 8) continue;
+          uint4 *d = reinterpret_cast<uint4 *>(at + row / 16 * (KS * FRAG) + row % 16 * (KS * 64) + T::place(row % 16, p) * 16);
+          uint4 v = *d;
+          uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[q] &= left > 2 * q + 1 ? 0xffffffffu : left == 2 * q + 1 ? 0xffffu : 0u;
+          *d = v;
+        }
+      }
+    };
+    operand(st, T::BM, T::AT);
+    operand(st + T::FA * FRAG, T::BN, T::BT);
+    barrier_only();
+  };
+  // stage kt (sp: its parity), kt + NS + 1 < KT.  LOAD: stage kt + NS is loaded, and is not the last one in part; else it is loaded if there is one.  NEXT:
+  // there is a stage after this one
+  auto steady_of = [&](int kt, auto sp, auto loads, auto next_one) {
     constexpr int SP = decltype(sp)::value;
+    constexpr bool LOAD = decltype(loads)::value, NEXT = decltype(next_one)::value;
 #pragma unroll
     for (int k = 0; k < KW; ++k) {
       const Chunk &now = set[(SP * KW + k) & 1];
@@ -395,11 +490,18 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
       Codes &ncodes = codes[T::MIXED ? SP ^ 1 : 0];   // (read with a stage's first chunk)
       arrived();
+      turned_anew();
       Stage ns{};
-      if (k + 1 == KW) {
-        wait_vmcnt<(NS - 2) * T::LOADS>();
+      if (k + 1 == KW && NEXT) {
+        if constexpr (LOAD) wait_vmcnt<(NS - 2) * T::LOADS>();
+        else landed(nkt, NS - 2);
         barrier_only();
-        ns = stage(kt + NS, kt % NS);
+        if constexpr (LOAD) {
+          ns = stage(kt + NS, kt % NS);
+        } else {
+          if (kt + NS < KT) issue(kt + NS, kt % NS);
+          if (nkt + 1 == KT && !whole) zero_beyond(nkt);
+        }
       }
       if (T::MIXED && k == 0) {
 #pragma unroll
@@ -409,12 +511,14 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       // memory pipe have taken all of them.
 #pragma unroll
       for (int n = 0; n < GROUPS; ++n) {
-        if (k + 1 == KW) {
+        if (k + 1 == KW && LOAD) {
 #pragma unroll
           for (int q = n * T::LOADS / GROUPS; q < (n + 1) * T::LOADS / GROUPS; ++q) load(ns, q, std::false_type{});
         }
+        if (k + 1 < KW || NEXT) {
 #pragma unroll
-        for (int q = n * reads(nk) / GROUPS; q < (n + 1) * reads(nk) / GROUPS; ++q) read(next, ncodes, nkt, nk, q);
+          for (int q = n * reads(nk) / GROUPS; q < (n + 1) * reads(nk) / GROUPS; ++q) read(next, ncodes, nkt, nk, q);
+        }
         if (T::MIXED && k + 1 < KW) {
 #pragma unroll
           for (int j = n * NB / GROUPS; j < (n + 1) * NB / GROUPS; ++j) expand(codes[T::MIXED ? SP : 0], k + 1, j);
@@ -424,24 +528,16 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       }
     }
   };
+  auto steady = [&](int kt, auto sp) { steady_of(kt, sp, std::true_type{}, std::true_type{}); };
   auto last = [&](int kt, auto sp) {   // the same, of the last stages
     constexpr int SP = decltype(sp)::value;
     const int left = kc1 - kc0 - kt * KS;
 #pragma unroll
     for (int k = 0; k < KW; ++k) {
-      Chunk &now = set[(SP * KW + k) & 1];
+      const Chunk &now = set[(SP * KW + k) & 1];
       Chunk &next = set[(SP * KW + k + 1) & 1];
       const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
       arrived();
-      if constexpr (T::ROWS) {   // columns beyond the last one (which may be anything, in both operands)
-        const int col = (kc0 + kt * KS + k * T::WK + wk) * 32 + (lane >> 4) * 8;
-        if (col >= g.cols) {
-#pragma unroll
-          for (int i = 0; i < MB; ++i) now.a[i][0] = bf16x8{};
-#pragma unroll
-          for (int j = 0; j < NB; ++j) now.b[j][0] = bf16x8{};
-        }
-      }
       if (k + 1 == KW && nkt < KT) {
         landed(nkt, NS - 2);
         barrier_only();
@@ -475,18 +571,49 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     else if (KT > 1) wait_vmcnt<T::LOADS>();
     else wait_vmcnt<0>();
     barrier_only();
+    if constexpr (T::ROWS) {
+      if (KT == 1 && !whole) zero_beyond(0);
+    }
 #pragma unroll
     for (int n = 0; n < reads(0); ++n) read(set[0], codes[0], 0, 0, n);
   }
   int kt = 0;
-  for (; kt + NS + 2 < KT; kt += 2) {
-    steady(kt, Even{});
-    steady(kt + 1, Odd{});
-  }
+  if constexpr (T::ROWS) {
+    const int full = KT - (whole ? 0 : 1);
+    auto loaded = [&](int t, auto sp) { steady_of(t, sp, std::false_type{}, std::true_type{}); };
+    auto final = [&](int t, auto sp) { steady_of(t, sp, std::false_type{}, std::false_type{}); };
+    if constexpr (KW % 2 == 0) {   // every stage begins with the first register set
+      for (; kt + NS < full; ++kt) steady(kt, Even{});
 #pragma unroll 1
-  for (; kt < KT; kt += 2) {
-    last(kt, Even{});
-    if (kt + 1 < KT) last(kt + 1, Odd{});
+      for (; kt + 1 < KT; ++kt) loaded(kt, Even{});
+      if (KT > 0) final(kt, Even{});
+    } else {
+      for (; kt + NS + 1 < full; kt += 2) {
+        steady(kt, Even{});
+        steady(kt + 1, Odd{});
+      }
+#pragma unroll 1
+      for (; kt + 2 < KT; kt += 2) {
+        loaded(kt, Even{});
+        loaded(kt + 1, Odd{});
+      }
+      if (kt + 1 < KT) {
+        loaded(kt, Even{});
+        final(kt + 1, Odd{});
+      } else if (KT > 0) {
+        final(kt, Even{});
+      }
+    }
+  } else {
+    for (; kt + NS + 2 < KT; kt += 2) {
+      steady(kt, Even{});
+      steady(kt + 1, Odd{});
+    }
+#pragma unroll 1
+    for (; kt < KT; kt += 2) {
+      last(kt, Even{});
+      if (kt + 1 < KT) last(kt + 1, Odd{});
+    }
   }
 
   const int r16 = lane & 15, g4 = lane >> 4;
@@ -520,7 +647,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
         if (HELD % STEP == 0 || row0 < HELD) pre[decltype(pass)::value & 1][it] = epi.pre(row_of(pass, it), n_at);
     };
     auto rows_out = [&](auto pass) {
-      __syncthreads();
+      barrier_only();
       if constexpr (decltype(pass)::value + 1 < MB / IB) ahead(std::integral_constant<int, decltype(pass)::value + 1>{});
 #pragma unroll
       for (int it = 0; it < ITEMS; ++it) {
@@ -690,7 +817,7 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
   g.sub_n = bn / T::BN;
   const int64_t grid = count * g.sub_m * g.sub_n;
   // (a tile's row blocks are reached by 32-bit offsets)
-  if (T::ROWS ? std::max(g.A.pitch, g.B.pitch) * std::max(T::BM, T::BN) > 0xffffffffll
+  if (T::ROWS ? std::max(g.A.pitch, g.B.pitch) * std::max({T::BM, T::BN, 32 * T::KS}) > 0xffffffffll
               : (int64_t)g.chunks * 3 * FRAG * (std::max(T::BM, T::BN) / 16) > 0xffffffffll)
     return hipErrorInvalidValue;
   if (mt <= 0 || nt <= 0 || g.chunks <= 0 || tiles > 0x7fffffff || grid <= 0 || grid > 0x7fffffff || first + count > 0x7fffffff ||
@@ -741,15 +868,21 @@ struct NtTiles<1, 1, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
   static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
-template <>
-struct NtTiles<1, 1, NT_ROWS> {
-  typedef NtTile<NT_ROWS, 8, 4, 2, 4, 1, 1, 1, 2, 2> T0;
-  typedef NtTile<NT_ROWS, 4, 4, 2, 2, 1, 1, 1, 2, 2> T1;
-  typedef NtTile<NT_ROWS, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
-  typedef NtTile<NT_ROWS, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
-  typedef NtTile<NT_ROWS, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
+template <int KIND>
+struct NtTilesOfRows {
+  typedef NtTile<KIND, 8, 4, 2, 4, 1, 1, 1, 2, 2> T0;
+  typedef NtTile<KIND, 4, 4, 2, 2, 1, 1, 1, 2, 2> T1;
+  typedef NtTile<KIND, 2, 2, 2, 4, 1, 1, 1, 2, 4> T2;
+  typedef NtTile<KIND, 2, 2, 2, 2, 1, 1, 1, 2, 4> T3;
+  typedef NtTile<KIND, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
   static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
+template <>
+struct NtTiles<1, 1, NT_ROWS> : NtTilesOfRows<NT_ROWS> {};
+template <>
+struct NtTiles<1, 1, NT_RT> : NtTilesOfRows<NT_RT> {};
+template <>
+struct NtTiles<1, 1, NT_TT> : NtTilesOfRows<NT_TT> {};
 template <>
 struct NtTiles<3, 1, NT_BF16> {
   // (128 x 128 takes .568 us where two of 64 x 128 on a compute unit take .532)
