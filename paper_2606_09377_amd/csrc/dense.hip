@@ -27,7 +27,6 @@ struct DenseOut {
     float bias[8];
     uint64_t offset;
   };
-  typedef Octet Pre;   // of the residual
   __device__ __forceinline__ Col col(int64_t n) const {
     Col c;
 #pragma unroll
@@ -44,12 +43,7 @@ struct DenseOut {
     c.offset = drop.k ? drop_offset(drop) : 0;
     return c;
   }
-  __device__ __forceinline__ Pre pre(int64_t m, int64_t n) const {
-    Pre p{};
-    if (res.p && m < rows && n < cols) p = load_octet(res, m, n, cols);
-    return p;
-  }
-  __device__ __forceinline__ void store8(int64_t m, int64_t n, float (&v)[8], const Col &c, const Pre &p) const {
+  __device__ __forceinline__ void store8(int64_t m, int64_t n, float (&v)[8], const Col &c) const {
     if (m >= rows || n >= cols) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], factor, c.bias[i]);
@@ -65,7 +59,7 @@ struct DenseOut {
     }
     if (res.p) {
       float a[8];
-      octet_values(res, p, a);
+      load8(res, m, n, cols, a);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += a[i];
     }
@@ -346,7 +340,7 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
       d[1] = b;
     } else {
       float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      o.store8(m, n, v, o.col(n), o.pre(m, n));
+      o.store8(m, n, v, o.col(n));
     }
   }
 }
@@ -596,7 +590,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   TRY(op_begin(c));
   const bool bf16 = dy->type == VCR_BF16, has_dx = dx && M > 0;
   if (!has_dx && !dw && !db) return VCR_OK;
-  if (bf16 && M > 0 && (!dx || rows_operand(w)) && (!dw || rows_operand(x)) && !getenv("NOTR")) return grad_of_rows(c, dy, x, w, o, add, dx, dw, db);
+  if (bf16 && M > 0 && (!dx || rows_operand(w)) && (!dw || rows_operand(x))) return grad_of_rows(c, dy, x, w, o, add, dx, dw, db);
   const int P = bf16 ? 1 : 3;
   const hipStream_t s = c->stream;
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;

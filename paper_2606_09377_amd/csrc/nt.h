@@ -181,8 +181,7 @@ __device__ __forceinline__ void nt_tile(const NtArgs &g, int id, int total, int 
 // its other rows and columns.
 // One with STAGED is given eight columns of a row instead: the tile goes through LDS, so that a wave has whole stretches of rows
 // (an epilogue that reads other matrices, or writes two, then moves whole lines, and its code is there once and not for every
-// block of a wave).  Col col(n): what it takes of columns n .. n + 7, asked for once; Pre pre(m, n): what it reads of a row there, asked for
-// a pass ahead; store8(m, n, values, col, pre).
+// block of a wave).  Col col(n): what it takes of columns n .. n + 7, asked for once; store8(m, n, values, col).
 template <class EPI, class = void>
 struct nt_staged : std::false_type {};
 template <class EPI>
@@ -583,7 +582,10 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     auto loaded = [&](int t, auto sp) { steady_of(t, sp, std::false_type{}, std::true_type{}); };
     auto final = [&](int t, auto sp) { steady_of(t, sp, std::false_type{}, std::false_type{}); };
     if constexpr (KW % 2 == 0) {   // every stage begins with the first register set
-      for (; kt + NS < full; ++kt) steady(kt, Even{});
+      for (; kt + NS + 1 < full; kt += 2) {
+        steady(kt, Even{});
+        steady(kt + 1, Even{});
+      }
 #pragma unroll 1
       for (; kt + 1 < KT; ++kt) loaded(kt, Even{});
       if (KT > 0) final(kt, Even{});
@@ -639,43 +641,31 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
       const int q = row0 + it * STEP, w = q / (16 * IB);
       return 16 * (rb0 + w * MB + pass * IB) + q - w * (16 * IB);
     };
-    typename EPI::Pre pre[2][ITEMS];
     const typename EPI::Col col = epi.col(n_at);
-    auto ahead = [&](auto pass) {
-#pragma unroll
-      for (int it = 0; it < ITEMS; ++it)
-        if (HELD % STEP == 0 || row0 < HELD) pre[decltype(pass)::value & 1][it] = epi.pre(row_of(pass, it), n_at);
-    };
-    auto rows_out = [&](auto pass) {
+    auto rows_out = [&](int pass) {
       barrier_only();
-      if constexpr (decltype(pass)::value + 1 < MB / IB) ahead(std::integral_constant<int, decltype(pass)::value + 1>{});
-#pragma unroll
+      if (HELD % STEP != 0 && row0 >= HELD) return;
+      // (rolled: with the items' copies of its code an epilogue outgrows the instruction cache, 9 us a tile of 256 x 256)
+#pragma unroll 1
       for (int it = 0; it < ITEMS; ++it) {
-        if (HELD % STEP != 0 && row0 >= HELD) continue;
         const float *s = tile + (row0 + it * STEP) * PITCH + oct * 8;
         const f32v4 a = *reinterpret_cast<const f32v4 *>(s), b = *reinterpret_cast<const f32v4 *>(s + 4);
         float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        epi.store8(row_of(pass, it), n_at, v, col, pre[decltype(pass)::value & 1][it]);
+        epi.store8(row_of(pass, it), n_at, v, col);
       }
     };
-    ahead(std::integral_constant<int, 0>{});
     if constexpr (T::WK == 1) {
       static_assert(IB * T::WM * 16 * PITCH * 4 <= T::LDS, "rows of a tile in LDS");
-      auto pass = [&](auto at) {
-        constexpr int p = decltype(at)::value;
+#pragma unroll
+      for (int p = 0; p < MB / IB; ++p) {
         barrier_only();   // what LDS held has been read
 #pragma unroll
         for (int i = 0; i < IB; ++i)
 #pragma unroll
           for (int j = 0; j < NB; ++j)
             *reinterpret_cast<f32v4 *>(tile + ((wm * IB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = joined(p * IB + i, j);
-        rows_out(at);
-      };
-      pass(std::integral_constant<int, 0>{});
-      if constexpr (MB / IB > 1) pass(std::integral_constant<int, 1>{});
-      if constexpr (MB / IB > 2) pass(std::integral_constant<int, 2>{});
-      if constexpr (MB / IB > 3) pass(std::integral_constant<int, 3>{});
-      static_assert(MB / IB <= 4, "passes");
+        rows_out(p);
+      }
     } else {
       constexpr int B = MB * NB, PER = (B + T::WK - 1) / T::WK;
       static_assert(T::BM * PITCH * 4 <= T::LDS, "the tile in LDS");
@@ -700,7 +690,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
         const int blk = n * T::WK + wk, i = blk / NB, j = blk - i * NB;
         if (blk < B) *reinterpret_cast<f32v4 *>(tile + ((wm * MB + i) * 16 + r16) * PITCH + (wn * NB + j) * 16 + 4 * g4) = sum[n];
       }
-      rows_out(std::integral_constant<int, 0>{});
+      rows_out(0);
     }
   } else if constexpr (T::WK == 1) {
 #pragma unroll

@@ -1,7 +1,7 @@
 // Products by the tiles of nt.h into a matrix, the contraction divided where that pays.  Part of layers.hip and dense.hip.
 //
 // OUT: where results go.  rows, cols, bytes() that an output takes, and put(m, n, values of n .. n + 3), or with STAGED
-// col, pre and store8 of eight columns (nt.h).
+// col and store8 of eight columns (nt.h).
 #pragma once
 
 #include "planes.h"
@@ -17,11 +17,9 @@ template <class OUT>
 struct EpiOut<OUT, std::enable_if_t<OUT::STAGED>> {
   static constexpr bool STAGED = true;
   typedef typename OUT::Col Col;
-  typedef typename OUT::Pre Pre;
   OUT o;
   __device__ __forceinline__ Col col(int n) const { return o.col(n); }
-  __device__ __forceinline__ Pre pre(int m, int n) const { return o.pre(m, n); }
-  __device__ __forceinline__ void store8(int m, int n, float (&v)[8], const Col &c, const Pre &p) const { o.store8(m, n, v, c, p); }
+  __device__ __forceinline__ void store8(int m, int n, float (&v)[8], const Col &c) const { o.store8(m, n, v, c); }
 };
 // sums over one part of the contraction, [parts][rows][ld]
 struct EpiPart {
@@ -48,7 +46,7 @@ static __global__ __launch_bounds__(256) void k_join(const float *p, int parts, 
     o.put(m, n, v[0]);
   } else {
     float x[8] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
-    o.store8(m, n, x, o.col(n), o.pre(m, n));
+    o.store8(m, n, x, o.col(n));
   }
 }
 

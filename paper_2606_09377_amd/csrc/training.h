@@ -38,40 +38,23 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   for (int i = 0; i < 4; ++i) w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Columns c .. c + 7 of row r as stored, those below cols (the others are 0)
-struct Octet {
-  uint4 q[2];   // of bf16 the first
-};
-__device__ __forceinline__ Octet load_octet(const MatRef &m, int64_t r, int64_t c, int64_t cols) {
-  const int64_t at = r * m.ld + c;
-  Octet o{};
-  if (m.vec && c + 8 <= cols) {
-    const uint4 *s = m.bf16 ? reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(m.p) + at)
-                            : reinterpret_cast<const uint4 *>(static_cast<const float *>(m.p) + at);
-    o.q[0] = s[0];
-    if (!m.bf16) o.q[1] = s[1];
-    return o;
-  }
-  uint32_t *w = reinterpret_cast<uint32_t *>(&o);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (c + i >= cols) continue;
-    if (m.bf16) w[i / 2] |= (uint32_t)static_cast<const uint16_t *>(m.p)[at + i] << 16 * (i & 1);
-    else w[i] = static_cast<const uint32_t *>(m.p)[at + i];
-  }
-  return o;
-}
-__device__ __forceinline__ void octet_values(const MatRef &m, const Octet &o, float (&v)[8]) {
-  if (m.bf16) {
-    unpack8(o.q[0], v);
-  } else {
-    const uint32_t w[8] = {o.q[0].x, o.q[0].y, o.q[0].z, o.q[0].w, o.q[1].x, o.q[1].y, o.q[1].z, o.q[1].w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float, w[i]);
-  }
-}
+// Columns c .. c + 7 of row r, those below cols (the others are 0)
 __device__ __forceinline__ void load8(const MatRef &m, int64_t r, int64_t c, int64_t cols, float (&v)[8]) {
-  octet_values(m, load_octet(m, r, c, cols), v);
+  const int64_t at = r * m.ld + c;
+  if (m.vec && c + 8 <= cols) {
+    if (m.bf16) {
+      unpack8(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(m.p) + at), v);
+    } else {
+      const f32v4 *s = reinterpret_cast<const f32v4 *>(static_cast<const float *>(m.p) + at);
+      const f32v4 a = s[0], b = s[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    v[i] = c + i >= cols ? 0.f : m.bf16 ? bf16_value(static_cast<const uint16_t *>(m.p)[at + i]) : static_cast<const float *>(m.p)[at + i];
 }
 // (those below cols)
 __device__ __forceinline__ void save8(const MatRef &m, int64_t r, int64_t c, int64_t cols, const float (&v)[8]) {
