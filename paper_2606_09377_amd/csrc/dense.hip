@@ -172,16 +172,72 @@ static hipError_t launch_dense_planes(const PlanesArgs *a, const PlanesArgs *b, 
 }
 
 // db = factor times the sums of the columns' groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
-__global__ __launch_bounds__(256) void k_dense_sums(const float *sums, int64_t groups, int64_t cols, float factor, float *out) {
-  __shared__ float part[4][64];
+struct ColumnSums {
+  const float *sums;
+  int64_t groups, cols;
+  float factor;
+  float *out;   // or null
+};
+__device__ __forceinline__ void column_sums(const ColumnSums &g, int64_t block, float *lds) {   // lds: 256 floats
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t c = block * 64 + lane;
   float s = 0.f;
 #pragma unroll 8
-  for (int64_t p = wave; p < groups; p += 4) s += c < cols ? sums[p * cols + c] : 0.f;
-  part[wave][lane] = s;
+  for (int64_t p = wave; p < g.groups; p += 4) s += c < g.cols ? g.sums[p * g.cols + c] : 0.f;
+  lds[threadIdx.x] = s;
   __syncthreads();
-  if (wave == 0 && c < cols) out[c] = factor * ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+  if (wave == 0 && c < g.cols) g.out[c] = g.factor * ((lds[lane] + lds[64 + lane]) + (lds[128 + lane] + lds[192 + lane]));
+}
+__global__ __launch_bounds__(256) void k_dense_sums(ColumnSums g) {
+  __shared__ float lds[256];
+  column_sums(g, blockIdx.x, lds);
+}
+
+// ---- both gradients in one launch -------------------------------------------------------------
+// Two products of small tiles and the columns' sums, where the launches would take longer than their work: workgroups
+// of one after those of the other.
+template <class TA, class TB>
+__global__ __launch_bounds__(TA::T, 2) void k_dense_pair(const NtArgs ga, const EpiOut<DenseOut> ea, int na, const NtArgs gb, const EpiOut<DenseOut> eb, int nb,
+                                                         ColumnSums sums) {
+  static_assert(TA::T == 256 && TB::T == 256, "workgroups of both");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[TA::LDS > TB::LDS ? TA::LDS : TB::LDS];
+  const int id = blockIdx.x;
+  if (id < na) nt_run<TA>(ga, ea, lds, id, na, 0);
+  else if (id < na + nb) nt_run<TB>(gb, eb, lds, id - na, nb, 0);
+  else column_sums(sums, id - na - nb, reinterpret_cast<float *>(lds));
+}
+template <int P, int KIND>
+struct PairTile {   // 32 x 64 outputs
+  typedef typename NtTiles<P, P, KIND>::T4 T;
+};
+template <>
+struct PairTile<3, NT_BF16> {
+  typedef NtTiles<3, 3, NT_BF16>::T3 T;
+};
+// By the plan's figures for that shape, its longest chain of chunks or its work on all compute units, whichever is longer (P parts; KA, KB: kinds of dx and dw)
+template <int P, int KA, int KB>
+static bool pair_pays(const DenseOut &a, int64_t ca, const DenseOut &b, int64_t cb) {
+  const NtShape &x = NtTiles<P, P, KA>::shapes[P == 3 ? 3 : 4];
+  const int64_t na = nt_tiles(a.rows, a.cols, 32, 64, false), nb = nt_tiles(b.rows, b.cols, 32, 64, false);
+  if (na + nb > 1 << 20) return false;
+  const float chain = x.us1 * (float)std::max(ca, cb) + NT_ROUND_US;
+  const float work = (.5f * x.us2 * (float)(na * ca + nb * cb) + .5f * NT_ROUND_US * (float)(na + nb)) / NT_CUS;
+  return NT_LAUNCH_US + std::max(chain, work) <
+         product_us<P, P, KA, 32>(a.rows, a.cols, ca, a.bytes()) + product_us<P, P, KB, 32>(b.rows, b.cols, cb, b.bytes());
+}
+template <int P, int KA, int KB>
+static hipError_t launch_pair(NtArgs ga, const DenseOut &a, NtArgs gb, const DenseOut &b, const ColumnSums &sums, hipStream_t s) {
+  typedef typename PairTile<P, KA>::T TA;
+  typedef typename PairTile<P, KB>::T TB;
+  static_assert(TA::BM == 32 && TA::BN == 64 && TB::BM == 32 && TB::BN == 64, "the shape of pair_pays");
+  const int64_t na = nt_tiles(a.rows, a.cols, 32, 64, false), nb = nt_tiles(b.rows, b.cols, 32, 64, false);
+  hipError_t e = nt_args<TA>(ga, a.rows, a.cols, 32, 64, 0, na, 1);
+  if (e == hipSuccess) e = nt_args<TB>(gb, b.rows, b.cols, 32, 64, 0, nb, 1);
+  if (e != hipSuccess) return e;
+  const int64_t ns = sums.out ? blocks_of(sums.cols, 64) : 0;
+  hipLaunchKernelGGL((k_dense_pair<TA, TB>), dim3((unsigned)(na + nb + ns)), dim3(256), 0, s, ga, EpiOut<DenseOut>{a}, (int)na, gb, EpiOut<DenseOut>{b}, (int)nb,
+                     sums);
+  return hipGetLastError();
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -381,12 +437,7 @@ static DevMat dev(const vcr_mat *m) { return DevMat{m->p, m->type == VCR_BF16, m
 static size_t room(bool bf16, int64_t M, int64_t N, int64_t chunks) {
   return bf16 ? part_bytes<1, 1, NT_BF16, 32>(M, N, chunks) : part_bytes<3, 3, NT_BF16, 32>(M, N, chunks);
 }
-static hipError_t product(bool bf16, const uint8_t *a, int64_t arb, const uint8_t *b, int64_t brb, int64_t chunks, const DenseOut &o, float *part,
-                          hipStream_t s) {
-  NtArgs g{};
-  g.A = NtOperand{a, nullptr, (int32_t)arb, 0};
-  g.B = NtOperand{b, nullptr, (int32_t)brb, 0};
-  g.chunks = (int32_t)chunks;
+static hipError_t product(bool bf16, const NtArgs &g, const DenseOut &o, float *part, hipStream_t s) {
   return bf16 ? nt_product<1, 1, NT_BF16, 32>(g, o, part, s) : nt_product<3, 3, NT_BF16, 32>(g, o, part, s);
 }
 
@@ -462,27 +513,34 @@ static vcr_status grad_of_rows(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, 
     });
     HIP_TRY(c, e);
   }
-  if (db && mg > 1) {
-    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, mg, N, drop.factor, db);
-    HIP_TRY(c, hipGetLastError());
-  }
+  const ColumnSums cs{sums, mg, N, drop.factor, db && mg > 1 ? db : nullptr};
   const uint8_t *gp = store ? reinterpret_cast<const uint8_t *>(g) : static_cast<const uint8_t *>(dy->p);
+  NtArgs a{}, b{};
+  DenseOut ao{}, bo{};
   if (dx) {
-    NtArgs a{};
     a.A = NtOperand{gp, nullptr, (int32_t)blocks_of(M, 16), 0, pitch * 2, M};
     a.B = NtOperand{static_cast<const uint8_t *>(w->p), nullptr, (int32_t)blocks_of(K, 16), 0, w->ld * 2, K};
     a.chunks = (int32_t)nch;
     a.cols = (int32_t)N;
-    HIP_TRY(c, (nt_product<1, 1, NT_RT, 32>(a, DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none}, part, s)));
+    ao = DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none};
   }
   if (dw) {
-    NtArgs a{};
-    a.A = NtOperand{gp, nullptr, (int32_t)blocks_of(N, 16), 0, pitch * 2, N};
-    a.B = NtOperand{static_cast<const uint8_t *>(x->p), nullptr, (int32_t)blocks_of(K, 16), 0, x->ld * 2, K};
-    a.chunks = (int32_t)mch;
-    a.cols = (int32_t)M;
-    HIP_TRY(c, (nt_product<1, 1, NT_TT, 32>(a, DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none}, part, s)));
+    b.A = NtOperand{gp, nullptr, (int32_t)blocks_of(N, 16), 0, pitch * 2, N};
+    b.B = NtOperand{static_cast<const uint8_t *>(x->p), nullptr, (int32_t)blocks_of(K, 16), 0, x->ld * 2, K};
+    b.chunks = (int32_t)mch;
+    b.cols = (int32_t)M;
+    bo = DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none};
   }
+  if (dx && dw && pair_pays<1, NT_RT, NT_TT>(ao, nch, bo, mch)) {
+    HIP_TRY(c, (launch_pair<1, NT_RT, NT_TT>(a, ao, b, bo, cs, s)));
+    return op_end(c);
+  }
+  if (cs.out) {
+    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, cs);
+    HIP_TRY(c, hipGetLastError());
+  }
+  if (dx) HIP_TRY(c, (nt_product<1, 1, NT_RT, 32>(a, ao, part, s)));
+  if (dw) HIP_TRY(c, (nt_product<1, 1, NT_TT, 32>(b, bo, part, s)));
   return op_end(c);
 }
 
@@ -550,7 +608,11 @@ vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_
   wl.row_blocks = nb;
   xl.row_chunks = wl.row_chunks = chunks;
   HIP_TRY(c, launch_dense_planes(nullptr, &xl, &wl, GradSource{}, bf16, c->stream));
-  HIP_TRY(c, product(bf16, xp, mb, wp, nb, chunks, out, part, c->stream));
+  NtArgs g{};
+  g.A = NtOperand{xp, nullptr, (int32_t)mb, 0};
+  g.B = NtOperand{wp, nullptr, (int32_t)nb, 0};
+  g.chunks = (int32_t)chunks;
+  HIP_TRY(c, product(bf16, g, out, part, c->stream));
   return op_end(c);
 }
 
@@ -627,15 +689,32 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   gl.sums = db && M > 0 ? sums : nullptr;
   HIP_TRY(c, launch_dense_planes(&gl, dw ? &xl : nullptr, has_dx ? &wl : nullptr, GradSource{mat_ref(o.act != VCR_ACT_NONE ? o.z : nullptr), o.act, drop},
                                  bf16, s));
-  if (db) {
-    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, sums, mg, N, drop.factor, db);
+  const ColumnSums cs{sums, mg, N, drop.factor, db};
+  const DropDev none = drop_dev(nullptr);
+  NtArgs a{}, b{};
+  DenseOut ao{}, bo{};
+  if (has_dx) {
+    a.A = NtOperand{gp, nullptr, (int32_t)mb, 0};
+    a.B = NtOperand{wt, nullptr, (int32_t)kb, 0};
+    a.chunks = (int32_t)nch;
+    ao = DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none};
+  }
+  if (dw) {
+    b.A = NtOperand{gt, nullptr, (int32_t)nb, 0};
+    b.B = NtOperand{xt, nullptr, (int32_t)kb, 0};
+    b.chunks = (int32_t)mch;
+    bo = DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none};
+  }
+  if (has_dx && dw && (bf16 ? pair_pays<1, NT_BF16, NT_BF16>(ao, nch, bo, mch) : pair_pays<3, NT_BF16, NT_BF16>(ao, nch, bo, mch))) {
+    HIP_TRY(c, bf16 ? (launch_pair<1, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)) : (launch_pair<3, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)));
+    return op_end(c);
+  }
+  if (cs.out) {
+    hipLaunchKernelGGL(k_dense_sums, dim3((unsigned)blocks_of(N, 64)), dim3(256), 0, s, cs);
     HIP_TRY(c, hipGetLastError());
   }
-  const DropDev none = drop_dev(nullptr);
-  if (has_dx)
-    HIP_TRY(c, product(bf16, gp, mb, wt, kb, nch, DenseOut{mat_ref(dx), MatRef{}, mat_ref(add), nullptr, M, K, VCR_ACT_NONE, drop.factor, none}, part, s));
-  if (dw)
-    HIP_TRY(c, product(bf16, gt, nb, xt, kb, mch, DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none}, part, s));
+  if (has_dx) HIP_TRY(c, product(bf16, a, ao, part, s));
+  if (dw) HIP_TRY(c, product(bf16, b, bo, part, s));
   return op_end(c);
 }
 

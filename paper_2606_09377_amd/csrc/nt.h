@@ -193,19 +193,19 @@ constexpr int nt_stage_blocks() {
   while (n > 1 && (n * T::WM * 16 * (T::BN + 4) * 4 > T::LDS || T::MB % n)) --n;
   return n;
 }
+// The tile of workgroup `id` of `total`, over part `z` of the contraction; lds: T::LDS bytes
 template <class T, class EPI>
-__global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2) void k_nt(const NtArgs g, const EPI epi) {
+__device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t *lds, int id, int total, int z) {
   constexpr int MB = T::MB, NB = T::NB, NW = T::NW, KS = T::KS, NS = T::NS, PA = T::PA, PB = T::PB;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[T::LDS];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM % T::WN, wk = wave / (T::WM * T::WN);
   int batch, mt, nt;
-  nt_tile(g, blockIdx.x, gridDim.x, batch, mt, nt);
+  nt_tile(g, id, total, batch, mt, nt);
   const int rb0 = mt * (T::BM / 16), cb0 = nt * (T::BN / 16);
   // (parts of a larger tile may lie outside)
   if (rb0 >= g.A.row_blocks || cb0 >= g.B.row_blocks || (g.tri && cb0 >= rb0 + T::BM / 16)) return;
-  const int kc0 = blockIdx.y * g.z_chunks, kc1 = min(g.chunks, kc0 + g.z_chunks);
+  const int kc0 = z * g.z_chunks, kc1 = min(g.chunks, kc0 + g.z_chunks);
   const int KT = (kc1 - kc0 + KS - 1) / KS;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)lds;
 
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
     return v;
   };
   auto put = [&](int i, int j, f32v4 v) {
-    if constexpr (!nt_staged<EPI>::value) epi.store(batch, blockIdx.y, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
+    if constexpr (!nt_staged<EPI>::value) epi.store(batch, z, 16 * (rb0 + wm * MB + i) + r16, 16 * (cb0 + wn * NB + j) + 4 * g4, v, lane);
   };
   if constexpr (nt_staged<EPI>::value) {
     constexpr int PITCH = T::BN + 4, IB = T::WK == 1 ? nt_stage_blocks<T>() : MB;   // row blocks of a wave in a pass
@@ -718,6 +718,13 @@ __global__ __launch_bounds__(T::T, T::NW == 4 && 2 * T::LDS > 160 * 1024 ? 1 : 2
   }
 }
 
+constexpr int nt_min_blocks(int waves, int lds) { return waves == 4 && 2 * lds > 160 * 1024 ? 1 : 2; }
+template <class T, class EPI>
+__global__ __launch_bounds__(T::T, nt_min_blocks(T::NW, T::LDS)) void k_nt(const NtArgs g, const EPI epi) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[T::LDS];
+  nt_run<T>(g, epi, lds, blockIdx.x, gridDim.x, blockIdx.y);
+}
+
 // ---- which tiles -------------------------------------------------------------------------------
 // The shapes of one class of products, largest first; a tile of one is whole tiles of every later one.  A large shape
 // spends less per output, a small one wastes less of the chip's last round, and where two workgroups fit a compute unit
@@ -792,9 +799,9 @@ int nt_parts(int64_t M, int64_t N, int64_t chunks) {
   return nt_us(x, t * parts, (chunks + parts - 1) / parts, 4.f) + NT_LAUNCH_US < nt_plan<TS>(M, N, chunks, 1, false, 4.f).us ? (int)parts : 1;
 }
 
-// `count` tiles of shape (bm, bn) from `first` on, by kernels of shape T
-template <class T, class EPI>
-hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t first, int64_t count, int parts, const EPI &epi, hipStream_t s) {
+// g for `count` tiles of shape (bm, bn) from `first` on, by kernels of shape T
+template <class T>
+hipError_t nt_args(NtArgs &g, int64_t M, int64_t N, int bm, int bn, int64_t first, int64_t count, int parts) {
   const int64_t mt = (M + bm - 1) / bm, nt = (N + bn - 1) / bn;
   g.bm = bm;
   g.bn = bn;
@@ -815,7 +822,13 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
     return hipErrorInvalidValue;
   const int kt = (g.chunks + T::KS - 1) / T::KS;
   g.z_chunks = (kt + parts - 1) / parts * T::KS;
-  hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)grid, (unsigned)parts), dim3(T::T), 0, s, g, epi);
+  return hipSuccess;
+}
+template <class T, class EPI>
+hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t first, int64_t count, int parts, const EPI &epi, hipStream_t s) {
+  const hipError_t e = nt_args<T>(g, M, N, bm, bn, first, count, parts);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)(count * g.sub_m * g.sub_n), (unsigned)parts), dim3(T::T), 0, s, g, epi);
   return hipGetLastError();
 }
 // A product by the shapes of TS (T0 .. T4 and their `shapes`)

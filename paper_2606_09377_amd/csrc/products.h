@@ -56,6 +56,15 @@ static size_t part_bytes(int64_t M, int64_t N, int64_t chunks) {
   const int parts = std::min(MOST, nt_parts<NtTiles<PA, PB, KIND>>(M, N, chunks));
   return parts > 1 ? (size_t)parts * M * blocks_of(N, 4) * 16 : 0;
 }
+// What nt_product is estimated to take, us
+template <int PA, int PB, int KIND, int MOST = NT_CUS>
+static float product_us(int64_t M, int64_t N, int64_t chunks, float out_bytes) {
+  typedef NtTiles<PA, PB, KIND> TS;
+  const int parts = std::min(MOST, nt_parts<TS>(M, N, chunks));
+  if (parts == 1) return nt_plan<TS>(M, N, chunks, 1, false, out_bytes).us;
+  const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
+  return nt_us(x, nt_tiles(M, N, x.bm, x.bn, false) * parts, blocks_of(chunks, parts), 4.f) + NT_LAUNCH_US;
+}
 // D = A B^T into o; part: room for part_bytes
 template <int PA, int PB, int KIND, int MOST = NT_CUS, class OUT>
 static hipError_t nt_product(const NtArgs &g, const OUT &o, float *part, hipStream_t s) {
