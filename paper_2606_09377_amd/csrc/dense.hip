@@ -210,14 +210,10 @@ template <int P, int KIND>
 struct PairTile {   // 32 x 64 outputs
   typedef typename NtTiles<P, P, KIND>::T4 T;
 };
-template <>
-struct PairTile<3, NT_BF16> {
-  typedef NtTiles<3, 3, NT_BF16>::T3 T;
-};
 // By the plan's figures for that shape, its longest chain of chunks or its work on all compute units, whichever is longer (P parts; KA, KB: kinds of dx and dw)
 template <int P, int KA, int KB>
 static bool pair_pays(const DenseOut &a, int64_t ca, const DenseOut &b, int64_t cb) {
-  const NtShape &x = NtTiles<P, P, KA>::shapes[P == 3 ? 3 : 4];
+  const NtShape &x = NtTiles<P, P, KA>::shapes[4];
   const int64_t na = nt_tiles(a.rows, a.cols, 32, 64, false), nb = nt_tiles(b.rows, b.cols, 32, 64, false);
   if (na + nb > 1 << 20) return false;
   const float chain = x.us1 * (float)std::max(ca, cb) + NT_ROUND_US;
@@ -435,10 +431,10 @@ static hipError_t launch_dense_rows(const DevMat &x, const DevMat &w, const Dens
 
 static DevMat dev(const vcr_mat *m) { return DevMat{m->p, m->type == VCR_BF16, m->rows, m->cols, m->ld, 0}; }
 static size_t room(bool bf16, int64_t M, int64_t N, int64_t chunks) {
-  return bf16 ? part_bytes<1, 1, NT_BF16, 32>(M, N, chunks) : part_bytes<3, 3, NT_BF16, 32>(M, N, chunks);
+  return bf16 ? part_bytes<1, 1, NT_BF16, 32>(M, N, chunks) : part_bytes<3, 3, NT_BF16_DENSE, 32>(M, N, chunks);
 }
 static hipError_t product(bool bf16, const NtArgs &g, const DenseOut &o, float *part, hipStream_t s) {
-  return bf16 ? nt_product<1, 1, NT_BF16, 32>(g, o, part, s) : nt_product<3, 3, NT_BF16, 32>(g, o, part, s);
+  return bf16 ? nt_product<1, 1, NT_BF16, 32>(g, o, part, s) : nt_product<3, 3, NT_BF16_DENSE, 32>(g, o, part, s);
 }
 
 // Up to 64 rows of bf16: tiles of all the rows and 32 columns, whose waves divide the contraction, with as many stages in flight as memory takes to answer
@@ -705,8 +701,8 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
     b.chunks = (int32_t)mch;
     bo = DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none};
   }
-  if (has_dx && dw && (bf16 ? pair_pays<1, NT_BF16, NT_BF16>(ao, nch, bo, mch) : pair_pays<3, NT_BF16, NT_BF16>(ao, nch, bo, mch))) {
-    HIP_TRY(c, bf16 ? (launch_pair<1, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)) : (launch_pair<3, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)));
+  if (has_dx && dw && (bf16 ? pair_pays<1, NT_BF16, NT_BF16>(ao, nch, bo, mch) : pair_pays<3, NT_BF16_DENSE, NT_BF16_DENSE>(ao, nch, bo, mch))) {
+    HIP_TRY(c, bf16 ? (launch_pair<1, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)) : (launch_pair<3, NT_BF16_DENSE, NT_BF16_DENSE>(a, ao, b, bo, cs, s)));
     return op_end(c);
   }
   if (cs.out) {

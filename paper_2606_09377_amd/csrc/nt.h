@@ -82,6 +82,7 @@ struct NtArgs {
 
 // both bf16, both 4-bit, A bf16 (grouped) and B 4-bit; bf16 as a program has them: both with contracted columns, B or both with contracted rows
 enum NtKind : int { NT_BF16 = 0, NT_FP4 = 1, NT_MIXED = 2, NT_ROWS = 3, NT_RT = 4, NT_TT = 5 };
+enum : int { NT_BF16_DENSE = 16 };   // classes of NtTiles alone: NT_BF16 with other shapes
 
 template <int KIND_, int MB_, int NB_, int WM_, int WN_, int WK_, int PA_, int PB_, int KS_, int NS_>
 struct NtTile {
@@ -776,6 +777,7 @@ NtPlan nt_plan(int64_t M, int64_t N, int64_t chunks, int64_t batch, bool tri, fl
     const int64_t round = sh[a].us2 > 0.f ? 2 * NT_CUS : NT_CUS, full = t / round * round;
     if (full == 0 || full == t) continue;
     for (int b = a + 1; b < nt_shapes<TS>; ++b) {
+      if (sh[a].bm % sh[b].bm || sh[a].bn % sh[b].bn) continue;   // (not whole tiles of it)
       const int64_t subs = (int64_t)(sh[a].bm / sh[b].bm) * (sh[a].bn / sh[b].bn);
       const float us = nt_us(sh[a], full, chunks, out_bytes) + nt_us(sh[b], (t - full) * subs, chunks, out_bytes);
       if (us < best.us) {
@@ -831,7 +833,16 @@ hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t fir
   hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)(count * g.sub_m * g.sub_n), (unsigned)parts), dim3(T::T), 0, s, g, epi);
   return hipGetLastError();
 }
-// A product by the shapes of TS (T0 .. T4 and their `shapes`)
+// The smallest shape
+template <class TS, class = void>
+struct nt_last {
+  typedef typename TS::T4 T;
+};
+template <class TS>
+struct nt_last<TS, std::void_t<typename TS::T5>> {
+  typedef typename TS::T5 T;
+};
+// A product by the shapes of TS (T0 .. T4, or to T5, and their `shapes`)
 template <class TS, class EPI>
 hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, float out_bytes, const EPI &epi, hipStream_t s) {
   const NtPlan p = nt_plan<TS>(M, N, g.chunks, batch, g.tri, out_bytes);
@@ -842,6 +853,9 @@ hipError_t launch_nt_plan(const NtArgs &g, int64_t M, int64_t N, int64_t batch, 
       case 1: return launch_nt<typename TS::T1>(g, M, N, bm, bn, first, count, 1, epi, s);
       case 2: return launch_nt<typename TS::T2>(g, M, N, bm, bn, first, count, 1, epi, s);
       case 3: return launch_nt<typename TS::T3>(g, M, N, bm, bn, first, count, 1, epi, s);
+      case 5:
+        if constexpr (nt_shapes<TS> > 5) return launch_nt<typename TS::T5>(g, M, N, bm, bn, first, count, 1, epi, s);
+        [[fallthrough]];
       default: return launch_nt<typename TS::T4>(g, M, N, bm, bn, first, count, 1, epi, s);
     }
   };
@@ -904,6 +918,18 @@ struct NtTiles<3, 3, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 1, 1, 4, 1, 3, 3, 1, 4> T3;
   typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T4;
   static constexpr NtShape shapes[] = {{128, 128, 1.f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
+};
+// (with 96 x 128: 2001 x 1500 outputs are 252 of them, one round, where of 128 x 128 a quarter of the compute units has none and of 64 x 128 it
+// takes one and a half: 43 us, 47 without)
+template <>
+struct NtTiles<3, 3, NT_BF16_DENSE> {
+  typedef NtTile<NT_BF16, 4, 2, 2, 4, 1, 3, 3, 1, 3> T0;
+  typedef NtTile<NT_BF16, 3, 2, 2, 4, 1, 3, 3, 1, 3> T1;
+  typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 3, 3, 2, 2> T2;
+  typedef NtTile<NT_BF16, 2, 2, 2, 2, 1, 3, 3, 1, 3> T3;
+  typedef NtTile<NT_BF16, 2, 1, 1, 4, 1, 3, 3, 1, 4> T4;
+  typedef NtTile<NT_BF16, 2, 2, 1, 1, 4, 3, 3, 4, 3> T5;
+  static constexpr NtShape shapes[] = {{128, 128, 1.f, 0.f}, {96, 128, .77f, 0.f}, {64, 128, .546f, 0.f}, {64, 64, .342f, .595f}, {32, 64, .214f, .413f}, {32, 32, .138f, 0.f}};
 };
 template <>
 struct NtTiles<1, 1, NT_MIXED> {

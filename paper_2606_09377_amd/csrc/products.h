@@ -73,7 +73,7 @@ static hipError_t nt_product(const NtArgs &g, const OUT &o, float *part, hipStre
   if (parts == 1) return launch_nt_plan<TS>(g, o.rows, o.cols, 1, o.bytes(), EpiOut<OUT>{o}, s);
   const int64_t ld = blocks_of(o.cols, 4) * 4;
   const NtShape &x = TS::shapes[nt_shapes<TS> - 1];
-  const hipError_t e = launch_nt<typename TS::T4>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,
+  const hipError_t e = launch_nt<typename nt_last<TS>::T>(g, o.rows, o.cols, x.bm, x.bn, 0, nt_tiles(o.rows, o.cols, x.bm, x.bn, false), parts,
                                                   EpiPart{part, o.rows, ld}, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_join<OUT>), dim3((unsigned)blocks_of(o.rows * (ld / 4), 256)), dim3(256), 0, s, part, parts, o.rows, ld, o);
