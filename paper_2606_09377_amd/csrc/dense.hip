@@ -171,6 +171,23 @@ static hipError_t launch_dense_planes(const PlanesArgs *a, const PlanesArgs *b, 
   });
 }
 
+// parts_of<3> of eight values: whether any of them needs more than the plain split is asked once (asked for every pair, the code of
+// 64 rows outgrew the instruction cache: 64 x 1024 x 1024 took 16 us)
+__device__ __forceinline__ void parts8(const float (&v)[8], bf16x8 (&out)[3]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+  uint32_t w[4][3];
+  if (__builtin_expect(__any(top >= 0x7f7f8000u), 0)) {   // rounds to infinity, is infinite or NaN
+#pragma unroll
+    for (int i = 0; i < 4; ++i) parts_of<3>(v[2 * i], v[2 * i + 1], w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_pair(v[2 * i], v[2 * i + 1], w[i][0], w[i][1], w[i][2]);
+  }
+#pragma unroll
+  for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]));
+}
 // db = factor times the sums of the columns' groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
 struct ColumnSums {
   const float *sums;
@@ -206,6 +223,118 @@ __global__ __launch_bounds__(TA::T, 2) void k_dense_pair(const NtArgs ga, const 
   else if (id < na + nb) nt_run<TB>(gb, eb, lds, id - na, nb, 0);
   else column_sums(sums, id - na - nb, reinterpret_cast<float *>(lds));
 }
+// dx of up to 64 float32 rows (MT row blocks) from g's rows as an operand and w as it is stored: laid out for the tiles, w would be moved four times.  A
+// workgroup takes 32 columns of w and all its rows, its 4 waves chunks of 32 rows in turn, each with the next one's loads in flight.  A lane has two
+// columns of eight rows, which are the even and the odd columns of two blocks of the matrix instruction: it reads them
+// across the rows, 128 bytes of each together, and splits them in registers.  Sums of the waves are added in LDS, in order.
+template <int MT>
+__device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat &w, const DenseOut &o, uint8_t *lds, int64_t block) {
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t k0 = block * 32, N = w.rows;
+  const int K = (int)w.cols;
+  const bool inside = k0 + 32 <= K;   // uniform
+  const float *wp = static_cast<const float *>(w.p) + k0 + 2 * r16;
+  struct Chunk {
+    float w[8][2];
+    bf16x8 a[MT][3];
+  };
+  auto load = [&](Chunk &q, int ch) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t n = (int64_t)ch * 32 + 8 * g4 + e;
+      if (inside && (int64_t)ch * 32 + 32 <= N) {   // uniform
+        __builtin_memcpy(q.w[e], __builtin_assume_aligned(wp + n * w.ld, 4), 8);
+      } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) q.w[e][b] = n < N && k0 + 2 * r16 + b < K ? wp[n * w.ld + b] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int p = 0; p < 3; ++p) q.a[t][p] = *reinterpret_cast<const bf16x8 *>(gp + (((int64_t)t * nch + ch) * 3 + p) * FRAG + lane * 16);
+  };
+  f32v4 hi[MT][2], lo[MT][2];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) hi[t][b] = lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+  auto use = [&](const Chunk &q) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float c[8] = {q.w[0][b], q.w[1][b], q.w[2][b], q.w[3][b], q.w[4][b], q.w[5][b], q.w[6][b], q.w[7][b]};
+      bf16x8 v[3];
+      parts8(c, v);
+      constexpr int pa[5] = {0, 2, 1, 0, 1}, pb[5] = {2, 0, 1, 1, 0};   // (nt.h)
+#pragma unroll
+      for (int p = 0; p < 5; ++p)   // (the row blocks' sums in turn: one's would wait for each other)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) lo[t][b] = mfma_bf16(v[pb[p]], q.a[t][pa[p]], lo[t][b]);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) hi[t][b] = mfma_bf16(v[0], q.a[t][0], hi[t][b]);
+    }
+  };
+  Chunk q[2];
+  int ch = wave;
+  if (ch < nch) load(q[0], ch);
+  for (; ch < nch; ch += 8) {
+    if (ch + 4 < nch) load(q[1], ch + 4);
+    use(q[0]);
+    if (ch + 8 < nch) load(q[0], ch + 8);
+    if (ch + 4 < nch) use(q[1]);
+  }
+  f32v4 *red = reinterpret_cast<f32v4 *>(lds);   // [wave][row block][block][lane]
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32v4 v = hi[t][b];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < __builtin_huge_valf() ? v[i] + lo[t][b][i] : v[i];
+      red[((wave * MT + t) * 2 + b) * 64 + lane] = v;
+    }
+  __syncthreads();
+  for (int it = threadIdx.x; it < (int)o.rows * 4; it += 256) {
+    const int m = it >> 2, j = it & 3, at = (m >> 4) * 128 + (m & 15) + 16 * j;
+    f32v4 v[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      v[b] = red[at + 64 * b];
+#pragma unroll
+      for (int k = 1; k < 4; ++k) v[b] += red[k * MT * 128 + at + 64 * b];
+    }
+    float x[8] = {v[0][0], v[1][0], v[0][1], v[1][1], v[0][2], v[1][2], v[0][3], v[1][3]};
+    o.store8(m, k0 + 8 * j, x, o.col(k0 + 8 * j));
+  }
+}
+template <int MT>
+__global__ __launch_bounds__(256, 2) void k_dense_few(const uint8_t *gp, int nch, DevMat w, const DenseOut oa, int na, const NtArgs gb, const EpiOut<DenseOut> eb, int nb,
+                                                      ColumnSums sums) {
+  typedef NtTiles<3, 3, NT_BF16_DENSE>::T4 TB;
+  static_assert(TB::T == 256 && TB::LDS >= 4 * MT * 2 * 1024, "workgroups of both");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[TB::LDS];
+  const int id = blockIdx.x;
+  if (id < na) few_dx<MT>(gp, nch, w, oa, lds, id);
+  else if (id < na + nb) nt_run<TB>(gb, eb, lds, id - na, nb, 0);
+  else column_sums(sums, id - na - nb, reinterpret_cast<float *>(lds));
+}
+// b: dw's product, if it goes along (nb tiles)
+static hipError_t launch_few(const uint8_t *gp, int64_t nch, const DevMat &w, const DenseOut &a, NtArgs gb, const DenseOut &b, int64_t nb, const ColumnSums &sums,
+                             hipStream_t s) {
+  typedef NtTiles<3, 3, NT_BF16_DENSE>::T4 TB;
+  if (nb) {
+    const hipError_t e = nt_args<TB>(gb, b.rows, b.cols, 32, 64, 0, nb, 1);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t na = blocks_of(a.cols, 32), ns = sums.out ? blocks_of(sums.cols, 64) : 0;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(na + nb + ns)), dim3(256), 0, s, gp, (int)nch, w, a, (int)na, gb, EpiOut<DenseOut>{b}, (int)nb, sums);
+    return hipGetLastError();
+  };
+  return a.rows <= 16 ? go(k_dense_few<1>) : a.rows <= 32 ? go(k_dense_few<2>) : go(k_dense_few<4>);
+}
+
 template <int P, int KIND>
 struct PairTile {   // 32 x 64 outputs
   typedef typename NtTiles<P, P, KIND>::T4 T;
@@ -280,11 +409,7 @@ __device__ __forceinline__ Parts8<BF> raw_parts(const Raw8<BF> &r) {
     const float v[8] = {__builtin_bit_cast(float, r.q[0].x), __builtin_bit_cast(float, r.q[0].y), __builtin_bit_cast(float, r.q[0].z),
                         __builtin_bit_cast(float, r.q[0].w), __builtin_bit_cast(float, r.q[1].x), __builtin_bit_cast(float, r.q[1].y),
                         __builtin_bit_cast(float, r.q[1].z), __builtin_bit_cast(float, r.q[1].w)};
-    uint32_t w[4][3];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) parts_of<3>(v[2 * i], v[2 * i + 1], w[i]);
-#pragma unroll
-    for (int p = 0; p < 3; ++p) o.p[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]));
+    parts8(v, o.p);
   }
   return o;
 }
@@ -330,17 +455,15 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const Parts8<BF> v = raw_parts<BF>(rw[b]);
+      if constexpr (!BF) {   // (nt.h: the small products, in order of their size, in an accumulator of their own; the row blocks' in turn, since one's wait for each other)
+        constexpr int pa[5] = {0, 2, 1, 0, 1}, pb[5] = {2, 0, 1, 1, 0};
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        if constexpr (BF) {
-          hi[t][b] = mfma_bf16(v.p[0], a[t].p[0], hi[t][b]);
-        } else {   // (nt.h: the small products, in order of their size, in an accumulator of their own)
-          constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};
+        for (int p = 0; p < 5; ++p)
 #pragma unroll
-          for (int p = 0; p < 5; ++p) lo[t][b] = mfma_bf16(v.p[pb[p]], a[t].p[pa[p]], lo[t][b]);
-          hi[t][b] = mfma_bf16(v.p[0], a[t].p[0], hi[t][b]);
-        }
+          for (int t = 0; t < MT; ++t) lo[t][b] = mfma_bf16(v.p[pb[p]], a[t].p[pa[p]], lo[t][b]);
       }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) hi[t][b] = mfma_bf16(v.p[0], a[t].p[0], hi[t][b]);
     }
   };
   auto use = [&](const Group &q) {
@@ -654,7 +777,10 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;
   const int64_t nch = blocks_of(N, 32), mch = blocks_of(std::max<int64_t>(M, 1), 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16),
                 kb = blocks_of(K, 16), mg = blocks_of(M, 64);
-  const size_t b_g = has_dx ? (size_t)mb * nch * P * FRAG : 0, b_wt = has_dx ? (size_t)kb * nch * P * FRAG : 0;
+  const bool few = !bf16 && has_dx && M <= 64;
+  // (few_dx takes whole groups of row blocks)
+  const int64_t gmb = few ? M <= 16 ? 1 : M <= 32 ? 2 : 4 : mb;
+  const size_t b_g = has_dx ? (size_t)gmb * nch * P * FRAG : 0, b_wt = has_dx && !few ? (size_t)kb * nch * P * FRAG : 0;
   const size_t b_gt = dw ? (size_t)nb * mch * P * FRAG : 0, b_xt = dw ? (size_t)kb * mch * P * FRAG : 0;
   const size_t b_sums = db ? (size_t)mg * N * 4 : 0;
   const size_t b_part = std::max(has_dx ? room(bf16, M, K, nch) : 0, dw ? room(bf16, N, K, mch) : 0);
@@ -667,7 +793,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   gl.x = dev(dy);
   if (has_dx) {
     gl.rows = gp;
-    gl.row_blocks = mb;
+    gl.row_blocks = gmb;
     gl.row_chunks = nch;
     wl.x = dev(w);
     wl.cols = wt;
@@ -683,7 +809,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
     gl.col_chunks = xl.col_chunks = mch;
   }
   gl.sums = db && M > 0 ? sums : nullptr;
-  HIP_TRY(c, launch_dense_planes(&gl, dw ? &xl : nullptr, has_dx ? &wl : nullptr, GradSource{mat_ref(o.act != VCR_ACT_NONE ? o.z : nullptr), o.act, drop},
+  HIP_TRY(c, launch_dense_planes(&gl, dw ? &xl : nullptr, has_dx && !few ? &wl : nullptr, GradSource{mat_ref(o.act != VCR_ACT_NONE ? o.z : nullptr), o.act, drop},
                                  bf16, s));
   const ColumnSums cs{sums, mg, N, drop.factor, db};
   const DropDev none = drop_dev(nullptr);
@@ -700,6 +826,13 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
     b.B = NtOperand{xt, nullptr, (int32_t)kb, 0};
     b.chunks = (int32_t)mch;
     bo = DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none};
+  }
+  if (few) {
+    const int64_t nb = dw ? nt_tiles(N, K, 32, 64, false) : 0;
+    const bool along = nb <= 2048;
+    HIP_TRY(c, launch_few(gp, nch, dev(w), ao, b, bo, along ? nb : 0, cs, s));
+    if (!along) HIP_TRY(c, product(bf16, b, bo, part, s));
+    return op_end(c);
   }
   if (has_dx && dw && (bf16 ? pair_pays<1, NT_BF16, NT_BF16>(ao, nch, bo, mch) : pair_pays<3, NT_BF16_DENSE, NT_BF16_DENSE>(ao, nch, bo, mch))) {
     HIP_TRY(c, bf16 ? (launch_pair<1, NT_BF16, NT_BF16>(a, ao, b, bo, cs, s)) : (launch_pair<3, NT_BF16_DENSE, NT_BF16_DENSE>(a, ao, b, bo, cs, s)));
