@@ -591,8 +591,9 @@ class Ctx:
         """Dropout of x (rows, cols), a float32 or bfloat16 CUDA tensor with contiguous rows, plus `residual`: of x's type
         unless `dtype` says so.  drop: a Dropout.  The gradient by x is the same call on dy, without the residual.  `out`
         may be x or the residual."""
+        import torch
         m = _mat(x)
-        y = x.new_empty(x.shape, dtype=dtype or x.dtype) if out is None else out
+        y = torch.empty_like(x, dtype=dtype) if out is None else out
         self._here(x, residual, y, drop.step)
         self._current_stream()
         self._check(self.lib.vcr_dropout(self.h, m, drop._c, None if residual is None else _mat(residual), _mat(y)))
@@ -603,7 +604,10 @@ class Ctx:
         type with contiguous rows, bias float32, act one of "none", "relu", "gelu", "silu".  Of x's type unless `dtype` says so.
         With keep_z (y, z), z as the gradient takes it, of x's type.  `out` may be the residual."""
         xm, wm = _mat(x), _mat(w)
-        y = x.new_empty((x.shape[0], w.shape[0]), dtype=dtype or x.dtype) if out is None else out
+        if out is not None:
+            y = out
+        else:   # (a dtype given costs a microsecond)
+            y = x.new_empty((x.shape[0], w.shape[0])) if dtype is None else x.new_empty((x.shape[0], w.shape[0]), dtype=dtype)
         z = x.new_empty(y.shape) if keep_z else None
         self._here(x, w, bias, residual, y, None if dropout is None else dropout.step)
         o, keep = _linear_opts(_bias(bias, w.shape[0]), act, dropout, residual, z)
@@ -616,11 +620,14 @@ class Ctx:
         """(dx, dw, db) of linear from dy (rows, n), all of one type: dx (rows, k), plus `add`, and dw (n, k) of that type (dw: of
         `dw_dtype`), db (n) float32; None where `need` says so.  z: linear's, for an activation (with "relu" and no
         residual its result will do); act and dropout as they were.  The gradient by the residual is dy."""
+        import torch
         g = _mat(dy)
         rows, n = dy.shape
         dx = dy.new_empty((rows, w.shape[1])) if need[0] else None
-        dw = dy.new_empty((n, x.shape[1]), dtype=dw_dtype or dy.dtype) if need[1] else None
-        db = dy.new_empty((n,), dtype=_f32()) if need[2] else None
+        dw = None
+        if need[1]:
+            dw = dy.new_empty((n, x.shape[1])) if dw_dtype is None else dy.new_empty((n, x.shape[1]), dtype=dw_dtype)
+        db = dy.new_empty((n,), dtype=torch.float32) if need[2] else None
         self._here(dy, x, w, z, add, None if dropout is None else dropout.step)
         o, keep = _linear_opts(None, act, dropout, None, z)
         self._current_stream()
@@ -736,11 +743,6 @@ def _bias(b, n):
     if not (isinstance(b, torch.Tensor) and b.dtype == torch.float32 and b.is_cuda and b.shape == (n,) and b.is_contiguous()):
         raise ValueError(f"expected a contiguous float32 CUDA tensor of shape ({n},)")
     return b.data_ptr()
-
-
-def _f32():
-    import torch
-    return torch.float32
 
 
 def _at(packed):
