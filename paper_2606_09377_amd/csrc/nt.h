@@ -267,9 +267,9 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
     int at4, over;   // over: chunks of the stage beyond the contraction
     int first;       // as a program has them: its first place in the contraction
   };
-  auto stage = [&](int kt, int buf) {
+  auto stage = [&](int kt, uint32_t at) {   // at: its place in LDS
     return Stage{a_base + kt * (T::AT ? 32 * KS * g.A.pitch : (int64_t)(T::ROWS ? KS * 64 : KS * PA * FRAG)),
-                 b_base + kt * (T::BT ? 32 * KS * g.B.pitch : (int64_t)(T::ROWS ? KS * 64 : T::BF * FRAG)), lds0 + buf * T::STAGE,
+                 b_base + kt * (T::BT ? 32 * KS * g.B.pitch : (int64_t)(T::ROWS ? KS * 64 : T::BF * FRAG)), lds0 + at,
                  (T::MIXED ? bk0 + kt : kc0 + kt * KS) / 4 * 256, KS - (kc1 - kc0 - kt * KS), (kc0 + kt * KS) * 32};
   };
   auto load = [&](const Stage &s, int q, auto last) {   // load q < LOADS of this wave
@@ -304,7 +304,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
     }
   };
   auto issue = [&](int kt, int buf) {
-    const Stage s = stage(kt, buf);
+    const Stage s = stage(kt, buf * T::STAGE);
     if (!T::ROWS && (KS == 1 || T::MIXED || s.over <= 0)) {
 #pragma unroll
       for (int q = 0; q < T::LOADS; ++q) load(s, q, std::false_type{});
@@ -433,8 +433,14 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
   constexpr int KW = T::KW, AREADS = MB * PA, BREADS = T::MIXED ? 0 : NB * PB, GROUPS = MB * T::PRODUCTS;
   Chunk set[2];
   Codes codes[T::MIXED ? 2 : 1];
-  auto read = [&](Chunk &c, Codes &q, int kt, int k, int n) {   // read n of chunk k of stage kt, and of a stage's codes with its first
-    const uint8_t *st = lds + kt % NS * T::STAGE;
+  // Where stage kt lies in LDS, as one number: taken apart by the compiler, every address of a loop of two stages has a sum of its own (five
+  // updates of 1024 x 1024, whose tiles have three stages, 733 us and 720; of two stages the loop knows the places, and keeps them).
+  auto stage_at = [&](int kt) {
+    uint32_t at = kt % NS * T::STAGE;
+    if constexpr (NS > 2) asm("" : "+s"(at));
+    return at;
+  };
+  auto read = [&](Chunk &c, Codes &q, int kt, const uint8_t *st, int k, int n) {   // read n of chunk k of stage kt (at st), and of a stage's codes with its first
     if (n < BREADS) read_b(c, kt, st, k * T::WK + wk, n / PB, n % PB);
     else if (n < BREADS + AREADS) read_a(c, kt, st, k * T::WK + wk, (n - BREADS) / PA, (n - BREADS) % PA);
     else if constexpr (T::MIXED) read_codes(q, kt, st, n - BREADS - AREADS);
@@ -489,6 +495,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
       Chunk &next = set[(SP * KW + k + 1) & 1];
       const int nk = k + 1 < KW ? k + 1 : 0, nkt = k + 1 < KW ? kt : kt + 1;
       Codes &ncodes = codes[T::MIXED ? SP ^ 1 : 0];   // (read with a stage's first chunk)
+      const uint8_t *nst = lds + stage_at(nkt);
       arrived();
       turned_anew();
       Stage ns{};
@@ -497,7 +504,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
         else landed(nkt, NS - 2);
         barrier_only();
         if constexpr (LOAD) {
-          ns = stage(kt + NS, kt % NS);
+          ns = stage(kt + NS, stage_at(kt));
         } else {
           if (kt + NS < KT) issue(kt + NS, kt % NS);
           if (nkt + 1 == KT && !whole) zero_beyond(nkt);
@@ -517,7 +524,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
         }
         if (k + 1 < KW || NEXT) {
 #pragma unroll
-          for (int q = n * reads(nk) / GROUPS; q < (n + 1) * reads(nk) / GROUPS; ++q) read(next, ncodes, nkt, nk, q);
+          for (int q = n * reads(nk) / GROUPS; q < (n + 1) * reads(nk) / GROUPS; ++q) read(next, ncodes, nkt, nst, nk, q);
         }
         if (T::MIXED && k + 1 < KW) {
 #pragma unroll
@@ -545,7 +552,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
       }
       if (nkt < KT) {
 #pragma unroll
-        for (int n = 0; n < reads(nk); ++n) read(next, codes[T::MIXED ? SP ^ 1 : 0], nkt, nk, n);
+        for (int n = 0; n < reads(nk); ++n) read(next, codes[T::MIXED ? SP ^ 1 : 0], nkt, lds + nkt % NS * T::STAGE, nk, n);
       }
       if (k * T::WK + wk < left) {   // wave-uniform
         if constexpr (T::MIXED) {
@@ -575,7 +582,7 @@ __device__ __forceinline__ void nt_run(const NtArgs &g, const EPI &epi, uint8_t 
       if (KT == 1 && !whole) zero_beyond(0);
     }
 #pragma unroll
-    for (int n = 0; n < reads(0); ++n) read(set[0], codes[0], 0, 0, n);
+    for (int n = 0; n < reads(0); ++n) read(set[0], codes[0], 0, lds, 0, n);
   }
   int kt = 0;
   if constexpr (T::ROWS) {
