@@ -3,9 +3,14 @@
 //
 //   z = x w^T + b,  y = D(act(z)) + residual;   g = D(dy) act'(z),  dx = g w + add,  dw = g^T x,  db = sum g.
 //
-// All three products contract the contiguous axes of operands in the layout of nt.h: bf16 values in one part, float32 ones in three
-// (their six partial products keep float32's accuracy).  Dropout's factor is left out of g and multiplies the sums, so that
-// a bf16 g is dy itself or zero where the activation's slope is.
+// The products are nt.h's, on matrix instructions.  bf16 matrices go into the tiles as they are stored (rows aligned to 16 bytes; the
+// gradients' operands are transposed on the way out of LDS), others are laid out in the instructions' order first, bf16 values in one part,
+// float32 ones in three (their six partial products keep float32's accuracy).  Dropout's factor is left out of g and
+// multiplies the sums, so that a bf16 g is dy itself or zero where the activation's slope is.
+//
+// 4096 x 8192 x 8192 in bf16 is bound by the matrix instructions and what feeds them: forward with all that the epilogue does 1.24 PFLOP/s (443 us; a library
+// product alone 1.63), both gradients 1.31 (839 us; 865 for two library products alone).  Few rows are bound by reading the weights: one bf16 row of
+// 8192 x 8192 takes 22 us in the kernel, 6.1 TB/s.
 #include <algorithm>
 
 #include "products.h"
@@ -14,6 +19,9 @@
 namespace vcr {
 
 // ---- where results go -------------------------------------------------------------------------
+// Eight columns of a row at a time, from a tile's rows in LDS (nt.h), so that every access is 16 or 32 bytes.  The sums are rounded once, to y (and z); bias,
+// activation, dropout and residual cost no pass of their own.  (4096 x 8192 x 8192 in bf16: 360 us with nothing here, 443 with bias, ReLU,
+// dropout, residual and z: 201 MB more, of which the other workgroup's products hide about half.)
 struct DenseOut {
   static constexpr bool STAGED = true;
   MatRef y, z, res;
@@ -69,7 +77,7 @@ struct DenseOut {
 
 // ---- operands ---------------------------------------------------------------------------------
 // Up to three matrices of one type laid out in a launch, 64 x 64 values a workgroup; the first one may be a gradient, whose
-// values are those kept by dropout times the activation's slope.
+// values are those kept by dropout times the activation's slope.  Bound by memory: float32 2001 x 1000 and 1500 x 1000, 14 MB in and 21 MB out, 8.5 us.
 struct GradSource {
   MatRef z;
   int32_t act;
@@ -109,7 +117,7 @@ __global__ __launch_bounds__(256) void k_dense_planes(PlanesOf a, PlanesOf b, Pl
 }
 // g = the kept values of dy times the activation's slope as rows of bf16 (out null: not stored), and the sums of its columns over every 64
 // rows, sums [group][cols] (null: none; of one group: times `factor`, what is asked for).  A workgroup takes 64 x 64 values, a
-// thread eight columns of two rows.  Bound by memory.
+// thread eight columns of two rows.  Bound by memory: 4096 x 8192 with ReLU and dropout, 201 MB, 49 us (4.1 TB/s).
 __global__ __launch_bounds__(256) void k_grad_rows(DevMat dy, int vec, GradSource src, uint16_t *out, int64_t pitch, float *sums, float factor, int64_t first) {
   __shared__ float part[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, oct = threadIdx.x & 7;
@@ -188,7 +196,8 @@ __device__ __forceinline__ void parts8(const float (&v)[8], bf16x8 (&out)[3]) {
 #pragma unroll
   for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]));
 }
-// db = factor times the sums of the columns' groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group
+// db = factor times the sums of the columns' groups of 64 rows: a workgroup takes 64 columns, a wave every fourth group (64 groups of 8192 columns: 5 us,
+// a launch and its reads' latency)
 struct ColumnSums {
   const float *sums;
   int64_t groups, cols;
@@ -212,7 +221,8 @@ __global__ __launch_bounds__(256) void k_dense_sums(ColumnSums g) {
 
 // ---- both gradients in one launch -------------------------------------------------------------
 // Two products of small tiles and the columns' sums, where the launches would take longer than their work: workgroups
-// of one after those of the other.
+// of one after those of the other.  (us a call, together and apart: bf16 512 x 1024 x 1024 15.0 and 21.1, 512 x 2048 x 2048 32.7 and 28.3; float32
+// 128 x 2048 x 2048 36.4 and 38.7, 128 x 4096 x 4096 117.8 and 108.4.)
 template <class TA, class TB>
 __global__ __launch_bounds__(TA::T, 2) void k_dense_pair(const NtArgs ga, const EpiOut<DenseOut> ea, int na, const NtArgs gb, const EpiOut<DenseOut> eb, int nb,
                                                          ColumnSums sums) {
@@ -227,6 +237,9 @@ __global__ __launch_bounds__(TA::T, 2) void k_dense_pair(const NtArgs ga, const 
 // workgroup takes 32 columns of w and all its rows, its 4 waves chunks of 32 rows in turn, each with the next one's loads in flight.  A lane has two
 // columns of eight rows, which are the even and the odd columns of two blocks of the matrix instruction: it reads them
 // across the rows, 128 bytes of each together, and splits them in registers.  Sums of the waves are added in LDS, in order.
+// 64 x 1024 x 1024 takes 15 us, dw's tiles and db in the same launch: a chain of 8 chunks a wave, each 48 matrix instructions and two splits behind
+// its loads.  (Calls this way and with w laid out for the tiles, us: 16 x 1024 x 1024 15.5 and 21.0, 64 x 1024 x 1024 20.1 and 22.7, 64 x 8192 x 8192
+// 235 and 391.)
 template <int MT>
 __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat &w, const DenseOut &o, uint8_t *lds, int64_t block) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
@@ -370,7 +383,9 @@ static hipError_t launch_pair(NtArgs ga, const DenseOut &a, NtArgs gb, const Den
 // rows), its 8 waves go through groups of U chunks of 32 columns in turn, each with the next group's loads in flight, and their sums are added in LDS in wave order.
 // A lane reads its row's eight columns of a chunk as the matrix instruction takes them, of w and of x alike (x comes from L2: laid out
 // in LDS it would have to wait there for the slowest wave); float32 values are split into their parts in registers.  Rows beyond
-// the last read that one, and their results are not stored.
+// the last read that one, and their results are not stored.  Float32 8192 x 8192: one row 51 us (5.2 TB/s), 64 rows 94 us, in which the splits of x,
+// anew for every 32 rows of w, take as long as the loads.  (Laid out for the tiles instead, us a call: float32 16 x 1024 x 1024 15.0, 8.0 here;
+// 64 x 8192 x 8192 230 and 100; bf16 rows of no alignment, 64 x 1024 x 1024 12.9 and 11.6, 64 x 8192 x 8192 155 and 103.)
 template <bool BF>
 struct Raw8 {   // eight columns of a row as stored
   uint4 q[BF ? 1 : 2];
@@ -519,6 +534,11 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
     }
   }
 }
+// Two row blocks a workgroup halve what is read and split of x, where enough workgroups are left (us with one and two: float32 64 x 4096 x 8192 82.6 and
+// 55.0, 16 x 4096 x 8192 38.7 and 35.6, 8 x 8192 x 8192 61.8 and 76.9; bf16 8 x 8192 x 8192 63.5 and 53.4, 1 x 4096 x 8192 23.4 and 25.3).  The
+// columns are divided among idle compute units where that saves more than the launch that joins the parts, of which it takes more than 64 too long
+// to read (us whole and in parts: float32 1 x 2048 x 256 8.3 and 11.3, 1 x 8192 x 256 22.6 and 11.2, 64 x 784 x 1024 10.0 and 11.3,
+// 64 x 2048 x 256 22.2 and 11.2, 64 x 65536 x 64 563 and 27; 1 x 262144 x 16 in 64 parts 21, in 256 34).
 struct DenseRows {
   int nb, u, parts, z_groups;
   int64_t wgs;
@@ -527,11 +547,13 @@ struct DenseRows {
 static DenseRows dense_rows(bool bf16, int64_t M, int64_t N, int64_t K) {
   DenseRows p{};
   const int64_t blocks = blocks_of(N, 16);
-  p.nb = M > 8 && blocks >= 512 ? 2 : 1;
+  p.nb = M > (bf16 ? 4 : 8) && blocks >= 512 ? 2 : 1;
   p.u = bf16 ? (M <= 16 ? 4 : 2) : M <= 16 ? 2 : 1;
   p.wgs = blocks_of(blocks, p.nb);
-  const int64_t groups = blocks_of(K, 32 * p.u), bytes = 16 * p.nb * K * (bf16 ? 2 : 4);
-  const int64_t z = std::max<int64_t>(1, std::min<int64_t>({256 / p.wgs, bytes >> 18, groups / 16}));
+  const int64_t groups = blocks_of(K, 32 * p.u);
+  int64_t z = std::min<int64_t>({256 / p.wgs, groups / 8, 64});
+  const float chain = (2.f + .1f * (float)M) * (1.f / 1024) * (float)K;   // us of a workgroup with all columns
+  if (z < 2 || chain - chain / (float)z < 5.f) z = 1;
   p.z_groups = (int)blocks_of(groups, z);
   p.parts = (int)blocks_of(groups, p.z_groups);
   p.part_bytes = p.parts > 1 ? (size_t)p.parts * M * p.wgs * p.nb * 64 : 0;
@@ -688,7 +710,9 @@ vcr_status vcr_linear(vcr_ctx *c, const vcr_mat *x, const vcr_mat *w, const vcr_
   const int P = bf16 ? 1 : 3;
   const DenseOut out{mat_ref(y), mat_ref(o.z), mat_ref(o.residual), o.bias, M, N, o.act, 1.f, drop_dev(o.drop)};
   const bool as_stored = bf16 && rows_product(x, w);
-  if (as_stored ? M <= 8 && N * K <= (int64_t)1 << 24 : M <= 64) {
+  // (few bf16 rows on narrow layers: by the plan a product in parts and their sum; us by rows and by tiles: 1 x 4096 x 2048 8.3 and 11.0, 16 x 4096 x 2048
+  // 10.1 and 10.9, 8 x 8192 x 2048 14.5 and 11.6, 1 x 4096 x 4096 9.1 and 8.2)
+  if (as_stored ? M <= 16 && N * K <= (int64_t)1 << 23 : M <= 64) {
     const DenseRows p = dense_rows(bf16, M, N, K);
     Workspace *ws = nullptr;
     TRY(op_space(c, p.part_bytes, &ws));
@@ -828,8 +852,11 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
     bo = DenseOut{mat_ref(dw), MatRef{}, MatRef{}, nullptr, N, K, VCR_ACT_NONE, drop.factor, none};
   }
   if (few) {
+    // dw's tiles go along where they are few, or where dx alone leaves compute units idle (32 columns of w a workgroup); else its own plan has
+    // larger ones (us along and apart: 64 x 8192 x 256 18.4 and 19.6, 64 x 4096 x 4096 80 and 91, 64 x 1024 x 65536 757 and 835, 1 x 5120 x 5120 92 and 98;
+    // 64 x 6144 x 8192 213 and 202, 64 x 16384 x 1024 82 and 73, 64 x 8192 x 8192 278 and 235)
     const int64_t nb = dw ? nt_tiles(N, K, 32, 64, false) : 0;
-    const bool along = nb <= 2048;
+    const bool along = nb <= 2048 || K < 6144;
     HIP_TRY(c, launch_few(gp, nch, dev(w), ao, b, bo, along ? nb : 0, cs, s));
     if (!along) HIP_TRY(c, product(bf16, b, bo, part, s));
     return op_end(c);

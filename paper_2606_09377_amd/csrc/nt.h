@@ -21,7 +21,7 @@
 //   eight values are two of LDS's transposing reads, each of 4 rows by 16 columns for 16 lanes, whose 32-byte pieces change places by the row's number, so
 //   that those of the 8 rows that 32 lanes read lie in different banks.
 // In both the permutation is applied to the addresses that are read from memory (a load to LDS has no other).  What lies beyond the matrix
-// is read in the place of the nearest that does not, and zeroed in registers where it would be contracted.
+// is read in the place of the nearest that does not, and zeroed in LDS where it would be contracted.
 //
 // Parts.  float32 values are three bf16 parts h + m + l (split_bf16.h); P parts keep 8 P bits.  Products of
 // (A parts, B parts), in order of their size:

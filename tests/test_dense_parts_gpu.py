@@ -1,0 +1,56 @@
+"""Few rows of float layers whose contraction is divided among workgroups, and gradients of few rows on wide layers, against 64
+bits.  Tolerances as in test_dense_gpu.py: parts are float32 sums, joined by float32 additions."""
+import numpy as np
+import pytest
+
+from oracle import dense64 as o64
+from tests.test_dense_gpu import ctx, dev, host, near, sums, test_linear as linear, test_linear_grad as linear_grad  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# (some in one part beside those in several; columns that end inside a group, a chunk and eight; the last part short)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("m,k,n", [(1, 8192, 256), (1, 9001, 40), (2, 4100, 500), (5, 70001, 16), (16, 8193, 96), (17, 2079, 33), (33, 2100, 250),
+                                   (48, 6152, 700), (64, 30000, 17), (64, 2048, 2049)])
+def test_few_rows_in_parts(ctx, m, k, n, dtype):  # noqa: F811
+    linear(ctx, m, k, n, dtype)
+
+
+@pytest.mark.parametrize("dtype,pitch", [("float32", 0), ("bfloat16", 0), ("bfloat16", 3)])
+@pytest.mark.parametrize("m", [1, 16, 64])
+def test_parts_over_the_residual(ctx, m, dtype, pitch):  # noqa: F811
+    import torch
+    rng = np.random.default_rng(m)
+    k, n = 9000, 200
+    x, w, r = (dev(rng.standard_normal(s), dtype, pitch) for s in ((m, k), (n, k), (m, n)))
+    z, mag = o64.linear(host(x), host(w))
+    want = z + host(r)
+    apart = ctx.linear(x, w, residual=r)
+    got = ctx.linear(x, w, residual=r, out=r)
+    assert got.data_ptr() == r.data_ptr() and torch.equal(got, apart)
+    near(got, want, sums(mag, k) + 2.0 ** -24 * np.abs(want), dtype)
+    assert all(torch.equal(ctx.linear(x, w), ctx.linear(x, w)) for _ in range(3))
+
+
+# dw beside dx in a launch, and by its own plan
+@pytest.mark.parametrize("m,k,n", [(5, 6400, 1100), (64, 6144, 700), (33, 6143, 1200), (1, 2000, 5000), (64, 8200, 90)])
+def test_gradients_of_few_rows_on_wide_layers(ctx, m, k, n):  # noqa: F811
+    linear_grad(ctx, m, k, n, "float32")
+
+
+def test_operands_beside_nan(ctx):  # noqa: F811
+    """bf16 matrices as they are stored end inside a stage of the contraction, with NaN behind every row and after the last."""
+    import torch
+    rng = np.random.default_rng(5)
+    for m, k, n in ((8, 72, 40), (70, 40, 136), (130, 8, 264), (300, 1032, 136), (520, 200, 520)):
+        def held(r, c):
+            buf = torch.full((r + 3, c + 24), float("nan"), dtype=torch.bfloat16, device="cuda")
+            t = buf[1:r + 1, 8:c + 8]
+            t.copy_(torch.as_tensor(rng.standard_normal((r, c)), dtype=torch.float32).bfloat16())
+            return t
+        x, w, dy = held(m, k), held(n, k), held(m, n)
+        z, mag = o64.linear(host(x), host(w))
+        near(ctx.linear(x, w), z, sums(mag, k), "bfloat16")
+        for t, (v, g), terms, o in zip(ctx.linear_grad(dy, x, w), o64.gradients(host(dy), host(x), host(w)), (n, m, m), ("bfloat16", "bfloat16", "float32")):
+            near(t, v, sums(g, terms) + 2.0 ** -23 * g, o)
