@@ -8,8 +8,8 @@
 // float32 ones in three (their six partial products keep float32's accuracy).  Dropout's factor is left out of g and
 // multiplies the sums, so that a bf16 g is dy itself or zero where the activation's slope is.
 //
-// 4096 x 8192 x 8192 in bf16 is bound by the matrix instructions and what feeds them: forward with all that the epilogue does 1.24 PFLOP/s (443 us; a library
-// product alone 1.63), both gradients 1.31 (839 us; 865 for two library products alone).  Few rows are bound by reading the weights: one bf16 row of
+// 4096 x 8192 x 8192 in bf16 is bound by the matrix instructions and what feeds them: y alone 364 us (1.51 PFLOP/s; a library product 345), with all that the
+// epilogue does 434; dx 371 and dw 399 (library 396 and 471), both with db behind ReLU and dropout 826.  Few rows are bound by reading the weights: one bf16 row of
 // 8192 x 8192 takes 22 us in the kernel, 6.1 TB/s.
 #include <algorithm>
 
@@ -20,8 +20,9 @@ namespace vcr {
 
 // ---- where results go -------------------------------------------------------------------------
 // Eight columns of a row at a time, from a tile's rows in LDS (nt.h), so that every access is 16 or 32 bytes.  The sums are rounded once, to y (and z); bias,
-// activation, dropout and residual cost no pass of their own.  (4096 x 8192 x 8192 in bf16: 360 us with nothing here, 443 with bias, ReLU,
-// dropout, residual and z: 201 MB more, of which the other workgroup's products hide about half.)
+// activation, dropout and residual cost no pass of their own.  (4096 x 8192 x 8192 in bf16: 364 us with nothing here, 370 with bias and ReLU, 406 with
+// bias and GELU, whose error function no product hides, since a large tile has its compute unit to itself; 434 with bias, ReLU, dropout,
+// residual and z, 134 MB more and 4 M Philox outputs.)
 struct DenseOut {
   static constexpr bool STAGED = true;
   MatRef y, z, res;

@@ -892,6 +892,8 @@ struct NtTiles<1, 1, NT_BF16> {
   typedef NtTile<NT_BF16, 2, 4, 1, 1, 4, 1, 1, 4, 3> T4;
   static constexpr NtShape shapes[] = {{256, 256, .68f, 0.f}, {128, 128, .242f, .41f}, {64, 128, .147f, 0.f}, {64, 64, .087f, .182f}, {32, 64, .058f, .143f}};
 };
+// Operands as a program has them: two chunks a stage, so that wave-wide loads read whole lines of 128 bytes, and two stages for the large tiles (128 KB of
+// LDS; four of one chunk read half lines).  4096 x 8192 x 8192: NT_ROWS 364 us (1.51 PFLOP/s), NT_RT 371, NT_TT 399 with the writes of 8192 x 8192 results.
 template <int KIND>
 struct NtTilesOfRows {
   typedef NtTile<KIND, 8, 4, 2, 4, 1, 1, 1, 2, 2> T0;
