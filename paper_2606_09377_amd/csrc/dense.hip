@@ -796,7 +796,8 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   TRY(op_begin(c));
   const bool bf16 = dy->type == VCR_BF16, has_dx = dx && M > 0;
   if (!has_dx && !dw && !db) return VCR_OK;
-  if (bf16 && M > 0 && (!dx || rows_operand(w)) && (!dw || rows_operand(x))) return grad_of_rows(c, dy, x, w, o, add, dx, dw, db);
+  // (g's rows, where they are written out, have offsets of the tiles' 32 bits up to 2^22 columns, as rows_operand asks of the others)
+  if (bf16 && M > 0 && N < (int64_t)1 << 22 && (!dx || rows_operand(w)) && (!dw || rows_operand(x))) return grad_of_rows(c, dy, x, w, o, add, dx, dw, db);
   const int P = bf16 ? 1 : 3;
   const hipStream_t s = c->stream;
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;
@@ -857,7 +858,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
     // larger ones (us along and apart: 64 x 8192 x 256 18.4 and 19.6, 64 x 4096 x 4096 80 and 91, 64 x 1024 x 65536 757 and 835, 1 x 5120 x 5120 92 and 98;
     // 64 x 6144 x 8192 213 and 202, 64 x 16384 x 1024 82 and 73, 64 x 8192 x 8192 278 and 235)
     const int64_t nb = dw ? nt_tiles(N, K, 32, 64, false) : 0;
-    const bool along = nb <= 2048 || K < 6144;
+    const bool along = nb <= 2048 || (K < 6144 && nb <= 1 << 20);   // (a launch takes less than 2^32 threads)
     HIP_TRY(c, launch_few(gp, nch, dev(w), ao, b, bo, along ? nb : 0, cs, s));
     if (!along) HIP_TRY(c, product(bf16, b, bo, part, s));
     return op_end(c);

@@ -260,7 +260,7 @@ class Dropout:
     """Which values dropout keeps (vcr_drop): each with probability 1 - p, in steps of 2^-16, by random bits that seed, offset
     + step and a value's place give.  `step`: an int64 CUDA tensor of one element, read when a call's work runs (so that replays of
     a recorded call take new masks), or None.  The same seed, offset and step give the same mask: a gradient takes the object
-    of its call, another call an offset of its own."""
+    of its call, another call an offset of its own.  A Dropout does not change: it is kept as the library reads it."""
 
     __slots__ = ("p", "seed", "offset", "step", "_c")
 
@@ -269,8 +269,12 @@ class Dropout:
             import torch
             if not (isinstance(step, torch.Tensor) and step.dtype == torch.int64 and step.is_cuda and step.numel() == 1):
                 raise ValueError("expected an int64 CUDA tensor of one element")
-        self.p, self.seed, self.offset, self.step = p, seed, offset, step
-        self._c = _DROP.pack(p, seed & (2 ** 64 - 1), offset & (2 ** 64 - 1), 0 if step is None else step.data_ptr())
+        for name, value in (("p", p), ("seed", seed), ("offset", offset), ("step", step),
+                            ("_c", _DROP.pack(p, seed & (2 ** 64 - 1), offset & (2 ** 64 - 1), 0 if step is None else step.data_ptr()))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a Dropout does not change: make another one")
 
 
 def _net_nodes(net):

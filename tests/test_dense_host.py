@@ -193,3 +193,12 @@ def test_oracle_loss_gradient_is_the_differences(smoothing, lse2):
             e[r, c] = h
             diff = (o64.cross_entropy(x + e, t, smoothing, lse2)[0] - o64.cross_entropy(x - e, t, smoothing, lse2)[0]) / (2 * h)
             assert abs(diff - d[r, c]) < 1e-8
+
+
+def test_a_dropout_does_not_change(vc):
+    d = vc.Dropout(0.25, 7, 9)
+    packed = d._c
+    for name, value in (("p", 0.5), ("seed", 8), ("offset", 10), ("step", None)):
+        with pytest.raises(AttributeError):
+            setattr(d, name, value)
+    assert (d.p, d.seed, d.offset, d.step) == (0.25, 7, 9, None) and d._c == packed

@@ -54,3 +54,17 @@ def test_operands_beside_nan(ctx):  # noqa: F811
         near(ctx.linear(x, w), z, sums(mag, k), "bfloat16")
         for t, (v, g), terms, o in zip(ctx.linear_grad(dy, x, w), o64.gradients(host(dy), host(x), host(w)), (n, m, m), ("bfloat16", "bfloat16", "float32")):
             near(t, v, sums(g, terms) + 2.0 ** -23 * g, o)
+
+
+@pytest.mark.parametrize("n", [(1 << 22) - 8, (1 << 22) + 16])
+def test_gradients_of_very_many_outputs(ctx, n):  # noqa: F811
+    """g's rows written out for the tiles reach their offsets' 32 bits at 2^22 columns."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(3)
+    m, k = 3, 8
+    x, dy, z = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, k), (m, n), (m, n)))
+    _, dw, db = ctx.linear_grad(dy, x, None, z=z, act="relu", need=(False, True, True))
+    at = torch.cat([torch.arange(40), torch.arange(n // 2, n // 2 + 40), torch.arange(n - 40, n)]).cuda()
+    (_, (want, mag), (b, b_mag)) = o64.gradients(host(dy[:, at]) * (host(z[:, at]) > 0), host(x), np.zeros((len(at), k)))
+    near(dw[at], want, sums(mag, m), "bfloat16")
+    near(db[at], b, sums(b_mag, m))
