@@ -180,19 +180,22 @@ static hipError_t launch_dense_planes(const PlanesArgs *a, const PlanesArgs *b, 
   });
 }
 
-// parts_of<3> of eight values: whether any of them needs more than the plain split is asked once (asked for every pair, the code of
-// 64 rows outgrew the instruction cache: 64 x 1024 x 1024 took 16 us)
-__device__ __forceinline__ void parts8(const float (&v)[8], bf16x8 (&out)[3]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+// Three parts of eight values, plainly split; `top` is raised to their largest magnitude.  The plain split is wrong where a finite value rounds to
+// infinity alone (an infinite or NaN one makes its small products NaN, and the large one, which is then infinite or NaN, is the result):
+// a wave that finds `top` so large takes its sums again with ANY, parts_of<3>.  (A question with every eight values, and the other way's code beside each,
+// outgrew the instruction cache: 64 x 1024 x 1024 took 16 us asked for every pair, its dx 14.5 asked for every eight.)
+constexpr float PLAIN_SPLIT = 0x1.ffp127f;   // below
+template <bool ANY>
+__device__ __forceinline__ void parts8(const float (&v)[8], bf16x8 (&out)[3], float &top) {
   uint32_t w[4][3];
-  if (__builtin_expect(__any(top >= 0x7f7f8000u), 0)) {   // rounds to infinity, is infinite or NaN
 #pragma unroll
-    for (int i = 0; i < 4; ++i) parts_of<3>(v[2 * i], v[2 * i + 1], w[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) split_pair(v[2 * i], v[2 * i + 1], w[i][0], w[i][1], w[i][2]);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (ANY) {
+      parts_of<3>(v[2 * i], v[2 * i + 1], w[i]);
+    } else {
+      top = fmaxf(fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])), top);
+      split_pair(v[2 * i], v[2 * i + 1], w[i][0], w[i][1], w[i][2]);
+    }
   }
 #pragma unroll
   for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]));
@@ -245,25 +248,17 @@ template <int MT>
 __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat &w, const DenseOut &o, uint8_t *lds, int64_t block) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t k0 = block * 32, N = w.rows;
-  const int K = (int)w.cols;
-  const bool inside = k0 + 32 <= K;   // uniform
-  const float *wp = static_cast<const float *>(w.p) + k0 + 2 * r16;
+  // (two columns or more: vcr_linear_grad.  Columns beyond the last lie where they are read without a branch and are not stored)
+  const int K = (int)w.cols, N = (int)w.rows, k0 = (int)block * 32, kc = min(k0 + 2 * r16, K - 2);
+  const bool second = k0 + 2 * r16 == K - 1;   // the first of the lane's columns is the second one read
+  const float *wp = static_cast<const float *>(w.p) + kc;
   struct Chunk {
     float w[8][2];
     bf16x8 a[MT][3];
   };
   auto load = [&](Chunk &q, int ch) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int64_t n = (int64_t)ch * 32 + 8 * g4 + e;
-      if (inside && (int64_t)ch * 32 + 32 <= N) {   // uniform
-        __builtin_memcpy(q.w[e], __builtin_assume_aligned(wp + n * w.ld, 4), 8);
-      } else {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) q.w[e][b] = n < N && k0 + 2 * r16 + b < K ? wp[n * w.ld + b] : 0.f;
-      }
-    }
+    for (int e = 0; e < 8; ++e) __builtin_memcpy(q.w[e], __builtin_assume_aligned(wp + min(ch * 32 + 8 * g4 + e, N - 1) * w.ld, 4), 8);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -274,12 +269,16 @@ __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat 
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int b = 0; b < 2; ++b) hi[t][b] = lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
-  auto use = [&](const Chunk &q) {
+  float top = 0.f;
+  auto use = [&](const Chunk &q, int ch, auto any) {
+    const int left = N - ch * 32 - 8 * g4;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const float c[8] = {q.w[0][b], q.w[1][b], q.w[2][b], q.w[3][b], q.w[4][b], q.w[5][b], q.w[6][b], q.w[7][b]};
+      float c[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = e < left ? b == 0 && !second ? q.w[e][0] : q.w[e][1] : 0.f;
       bf16x8 v[3];
-      parts8(c, v);
+      parts8<decltype(any)::value>(c, v, top);
       constexpr int pa[5] = {0, 2, 1, 0, 1}, pb[5] = {2, 0, 1, 1, 0};   // (nt.h)
 #pragma unroll
       for (int p = 0; p < 5; ++p)   // (the row blocks' sums in turn: one's would wait for each other)
@@ -289,14 +288,26 @@ __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat 
       for (int t = 0; t < MT; ++t) hi[t][b] = mfma_bf16(v[0], q.a[t][0], hi[t][b]);
     }
   };
+  const std::false_type plain{};
   Chunk q[2];
   int ch = wave;
   if (ch < nch) load(q[0], ch);
   for (; ch < nch; ch += 8) {
     if (ch + 4 < nch) load(q[1], ch + 4);
-    use(q[0]);
+    use(q[0], ch, plain);
     if (ch + 8 < nch) load(q[0], ch + 8);
-    if (ch + 4 < nch) use(q[1]);
+    if (ch + 4 < nch) use(q[1], ch + 4, plain);
+  }
+  if (__builtin_expect(__any(top >= PLAIN_SPLIT), 0)) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) hi[t][b] = lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (ch = wave; ch < nch; ch += 4) {
+      load(q[0], ch);
+      use(q[0], ch, std::true_type{});
+    }
   }
   f32v4 *red = reinterpret_cast<f32v4 *>(lds);   // [wave][row block][block][lane]
 #pragma unroll
@@ -416,8 +427,8 @@ template <bool BF>
 struct Parts8 {
   bf16x8 p[BF ? 1 : 3];
 };
-template <bool BF>
-__device__ __forceinline__ Parts8<BF> raw_parts(const Raw8<BF> &r) {
+template <bool BF, bool ANY>
+__device__ __forceinline__ Parts8<BF> raw_parts(const Raw8<BF> &r, float &top) {
   Parts8<BF> o;
   if constexpr (BF) {
     o.p[0] = __builtin_bit_cast(bf16x8, r.q[0]);
@@ -425,7 +436,7 @@ __device__ __forceinline__ Parts8<BF> raw_parts(const Raw8<BF> &r) {
     const float v[8] = {__builtin_bit_cast(float, r.q[0].x), __builtin_bit_cast(float, r.q[0].y), __builtin_bit_cast(float, r.q[0].z),
                         __builtin_bit_cast(float, r.q[0].w), __builtin_bit_cast(float, r.q[1].x), __builtin_bit_cast(float, r.q[1].y),
                         __builtin_bit_cast(float, r.q[1].z), __builtin_bit_cast(float, r.q[1].w)};
-    parts8(v, o.p);
+    parts8<ANY>(v, o.p, top);
   }
   return o;
 }
@@ -457,20 +468,26 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
     }
   };
   f32v4 hi[MT][NB], lo[BF ? 1 : MT][BF ? 1 : NB];
+  auto clear = [&] {
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      hi[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (!BF) lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
-    }
-  auto multiply = [&](const Raw8<BF> (&rw)[NB], const Raw8<BF> (&rx)[MT]) {
+      for (int b = 0; b < NB; ++b) {
+        hi[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!BF) lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
+      }
+  };
+  clear();
+  float top = 0.f;
+  const std::false_type plain{};
+  auto multiply = [&](const Raw8<BF> (&rw)[NB], const Raw8<BF> (&rx)[MT], auto any) {
+    constexpr bool ANY = decltype(any)::value;
     Parts8<BF> a[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) a[t] = raw_parts<BF>(rx[t]);
+    for (int t = 0; t < MT; ++t) a[t] = raw_parts<BF, ANY>(rx[t], top);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const Parts8<BF> v = raw_parts<BF>(rw[b]);
+      const Parts8<BF> v = raw_parts<BF, ANY>(rw[b], top);
       if constexpr (!BF) {   // (nt.h: the small products, in order of their size, in an accumulator of their own; the row blocks' in turn, since one's wait for each other)
         constexpr int pa[5] = {0, 2, 1, 0, 1}, pb[5] = {2, 0, 1, 1, 0};
 #pragma unroll
@@ -484,7 +501,7 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
   };
   auto use = [&](const Group &q) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) multiply(q.w[u], q.x[u]);
+    for (int u = 0; u < U; ++u) multiply(q.w[u], q.x[u], plain);
   };
   Group q[2];
   int gi = g0 + wave;
@@ -495,16 +512,27 @@ __global__ __launch_bounds__(512) void k_dense_rows(DevMat x, DevMat w, DenseOut
     if (gi + 16 < gw) load(q[0], gi + 16);
     if (gi + 8 < gw) use(q[1]);
   }
+  auto chunk = [&](int c, auto any) {   // one that may lie beyond the columns in part
+    const int n = max(0, min(8, K - 32 * c - 8 * g4));
+    const int64_t at = (int64_t)c * (32 * ES);
+    Raw8<BF> ew[NB], ex[MT];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) ew[b] = raw_edge<BF>(wp[b] + at, n);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) ex[t] = raw_edge<BF>(xp[t] + at, n);
+    multiply(ew, ex, any);
+  };
   if (groups > whole && g1 == groups && wave == (whole - g0) % 8) {   // the columns beyond whole groups
-    for (int c = whole * U; c * 32 < K; ++c) {
-      const int n = max(0, min(8, K - 32 * c - 8 * g4));
-      const int64_t at = (int64_t)c * (32 * ES);
-      Raw8<BF> ew[NB], ex[MT];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) ew[b] = raw_edge<BF>(wp[b] + at, n);
-#pragma unroll
-      for (int t = 0; t < MT; ++t) ex[t] = raw_edge<BF>(xp[t] + at, n);
-      multiply(ew, ex);
+#pragma unroll 1
+    for (int c = whole * U; c * 32 < K; ++c) chunk(c, plain);
+  }
+  if constexpr (!BF) {
+    if (__builtin_expect(__any(top >= PLAIN_SPLIT), 0)) {   // (groups of this wave, as above)
+      clear();
+#pragma unroll 1
+      for (gi = g0 + wave; gi < g1; gi += 8)
+#pragma unroll 1
+        for (int c = gi * U; c < (gi + 1) * U && c * 32 < K; ++c) chunk(c, std::true_type{});
     }
   }
 #pragma unroll
@@ -803,7 +831,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;
   const int64_t nch = blocks_of(N, 32), mch = blocks_of(std::max<int64_t>(M, 1), 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16),
                 kb = blocks_of(K, 16), mg = blocks_of(M, 64);
-  const bool few = !bf16 && has_dx && M <= 64;
+  const bool few = !bf16 && has_dx && M <= 64 && K > 1;
   // (few_dx takes whole groups of row blocks)
   const int64_t gmb = few ? M <= 16 ? 1 : M <= 32 ? 2 : 4 : mb;
   const size_t b_g = has_dx ? (size_t)gmb * nch * P * FRAG : 0, b_wt = has_dx && !few ? (size_t)kb * nch * P * FRAG : 0;

@@ -68,3 +68,31 @@ def test_gradients_of_very_many_outputs(ctx, n):  # noqa: F811
     (_, (want, mag), (b, b_mag)) = o64.gradients(host(dy[:, at]) * (host(z[:, at]) > 0), host(x), np.zeros((len(at), k)))
     near(dw[at], want, sums(mag, m), "bfloat16")
     near(db[at], b, sums(b_mag, m))
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 200, 48), (5, 9000, 40), (16, 300, 96), (33, 130, 70), (64, 2500, 33), (300, 200, 100)])
+def test_values_that_round_to_infinity_in_bf16(ctx, m, k, n):  # noqa: F811
+    """Finite float32 values of more than bf16's largest take part with all their bits, beside infinite ones that reach their own results alone."""
+    rng = np.random.default_rng(k)
+    x, w, dy = rng.standard_normal((m, k)), 1e-20 * rng.standard_normal((n, k)), 1e-20 * rng.standard_normal((m, n))
+    x[0, 3], x[m - 1, k - 1], x[m // 2, k // 2] = 3.4e38, -3.396e38, 3.4028234e38
+    tx, tw = dev(x), dev(w)
+    z, mag = o64.linear(host(tx), host(tw))
+    near(ctx.linear(tx, tw), z, sums(mag, k))
+    w = rng.standard_normal((n, k))
+    w[0, 3], w[n - 1, k - 1], w[n // 2, k // 2] = 3.4e38, -3.396e38, 3.4028234e38
+    tw, tg = dev(w), dev(dy)
+    (want, mag), _, _ = o64.gradients(host(tg), host(tx), host(tw))
+    near(ctx.linear_grad(tg, None, tw, need=(True, False, False))[0], want, sums(mag, n))
+    w[n // 3, 7] = np.inf
+    tw = dev(w)
+    got = host(ctx.linear_grad(tg, None, tw, need=(True, False, False))[0])
+    assert np.array_equal(got[:, 7], np.sign(dy[:, n // 3]) * np.inf)
+    rest = np.arange(k) != 7
+    assert (np.abs(got - want)[:, rest] <= (sums(mag, n) + 2.0 ** -24 * (np.abs(want) + sums(mag, n)))[:, rest]).all()
+
+
+# an odd last column, one column alone, and contractions that end inside a chunk
+@pytest.mark.parametrize("m,k,n", [(3, 1, 70), (3, 2, 33), (20, 3, 31), (64, 33, 1), (64, 65, 45), (7, 95, 130)])
+def test_gradients_of_few_rows_of_odd_widths(ctx, m, k, n):  # noqa: F811
+    linear_grad(ctx, m, k, n, "float32")
