@@ -9,7 +9,7 @@
 // multiplies the sums, so that a bf16 g is dy itself or zero where the activation's slope is.
 //
 // 4096 x 8192 x 8192 in bf16 is bound by the matrix instructions and what feeds them: y alone 364 us (1.51 PFLOP/s; a library product 345), with all that the
-// epilogue does 434; dx 371 and dw 399 (library 396 and 471), both with db behind ReLU and dropout 826.  Few rows are bound by reading the weights: one bf16 row of
+// epilogue does 434; dx 371 and dw 399 (library 396 and 471), both with db behind ReLU and dropout 818.  Few rows are bound by reading the weights: one bf16 row of
 // 8192 x 8192 takes 22 us in the kernel, 6.1 TB/s.
 #include <algorithm>
 
@@ -208,13 +208,15 @@ struct ColumnSums {
   float factor;
   float *out;   // or null
 };
-__device__ __forceinline__ void column_sums(const ColumnSums &g, int64_t block, float *lds) {   // lds: 256 floats
+__device__ __forceinline__ void column_sums(const ColumnSums &g, int64_t block, float *lds) {   // lds: 256 floats (waves beyond four have nothing to do)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = block * 64 + lane;
   float s = 0.f;
+  if (wave < 4) {
 #pragma unroll 8
-  for (int64_t p = wave; p < g.groups; p += 4) s += c < g.cols ? g.sums[p * g.cols + c] : 0.f;
-  lds[threadIdx.x] = s;
+    for (int64_t p = wave; p < g.groups; p += 4) s += c < g.cols ? g.sums[p * g.cols + c] : 0.f;
+    lds[threadIdx.x] = s;
+  }
   __syncthreads();
   if (wave == 0 && c < g.cols) g.out[c] = g.factor * ((lds[lane] + lds[64 + lane]) + (lds[128 + lane] + lds[192 + lane]));
 }
@@ -238,12 +240,11 @@ __global__ __launch_bounds__(TA::T, 2) void k_dense_pair(const NtArgs ga, const 
   else column_sums(sums, id - na - nb, reinterpret_cast<float *>(lds));
 }
 // dx of up to 64 float32 rows (MT row blocks) from g's rows as an operand and w as it is stored: laid out for the tiles, w would be moved four times.  A
-// workgroup takes 32 columns of w and all its rows, its 4 waves chunks of 32 rows in turn, each with the next one's loads in flight.  A lane has two
+// workgroup takes 32 columns of w and all its rows, its 8 waves chunks of 32 rows in turn, each with the next one's loads in flight.  A lane has two
 // columns of eight rows, which are the even and the odd columns of two blocks of the matrix instruction: it reads them
 // across the rows, 128 bytes of each together, and splits them in registers.  Sums of the waves are added in LDS, in order.
-// 64 x 1024 x 1024 takes 15 us, dw's tiles and db in the same launch: a chain of 8 chunks a wave, each 48 matrix instructions and two splits behind
-// its loads.  (Calls this way and with w laid out for the tiles, us: 16 x 1024 x 1024 15.5 and 21.0, 64 x 1024 x 1024 20.1 and 22.7, 64 x 8192 x 8192
-// 235 and 391.)
+// 64 x 1024 x 1024 takes 11.4 us, dw's tiles and db in the same launch (12.3 with 4 waves): a wave's chunks one after another, each 48
+// matrix instructions and two splits behind its loads.
 template <int MT>
 __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat &w, const DenseOut &o, uint8_t *lds, int64_t block) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
@@ -292,11 +293,11 @@ __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat 
   Chunk q[2];
   int ch = wave;
   if (ch < nch) load(q[0], ch);
-  for (; ch < nch; ch += 8) {
-    if (ch + 4 < nch) load(q[1], ch + 4);
+  for (; ch < nch; ch += 16) {
+    if (ch + 8 < nch) load(q[1], ch + 8);
     use(q[0], ch, plain);
-    if (ch + 8 < nch) load(q[0], ch + 8);
-    if (ch + 4 < nch) use(q[1], ch + 4, plain);
+    if (ch + 16 < nch) load(q[0], ch + 16);
+    if (ch + 8 < nch) use(q[1], ch + 8, plain);
   }
   if (__builtin_expect(__any(top >= PLAIN_SPLIT), 0)) {
 #pragma unroll
@@ -304,7 +305,7 @@ __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat 
 #pragma unroll
       for (int b = 0; b < 2; ++b) hi[t][b] = lo[t][b] = f32v4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (ch = wave; ch < nch; ch += 4) {
+    for (ch = wave; ch < nch; ch += 8) {
       load(q[0], ch);
       use(q[0], ch, std::true_type{});
     }
@@ -320,24 +321,26 @@ __device__ __forceinline__ void few_dx(const uint8_t *gp, int nch, const DevMat 
       red[((wave * MT + t) * 2 + b) * 64 + lane] = v;
     }
   __syncthreads();
-  for (int it = threadIdx.x; it < (int)o.rows * 4; it += 256) {
+  for (int it = threadIdx.x; it < (int)o.rows * 4; it += 512) {
     const int m = it >> 2, j = it & 3, at = (m >> 4) * 128 + (m & 15) + 16 * j;
     f32v4 v[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       v[b] = red[at + 64 * b];
 #pragma unroll
-      for (int k = 1; k < 4; ++k) v[b] += red[k * MT * 128 + at + 64 * b];
+      for (int k = 1; k < 8; ++k) v[b] += red[k * MT * 128 + at + 64 * b];
     }
     float x[8] = {v[0][0], v[1][0], v[0][1], v[1][1], v[0][2], v[1][2], v[0][3], v[1][3]};
     o.store8(m, k0 + 8 * j, x, o.col(k0 + 8 * j));
   }
 }
+// dw's tiles beside it: at most two chunks
+typedef NtTile<NT_BF16, 2, 2, 2, 4, 1, 3, 3, 1, 2> FewTile;
 template <int MT>
-__global__ __launch_bounds__(256, 2) void k_dense_few(const uint8_t *gp, int nch, DevMat w, const DenseOut oa, int na, const NtArgs gb, const EpiOut<DenseOut> eb, int nb,
+__global__ __launch_bounds__(512) void k_dense_few(const uint8_t *gp, int nch, DevMat w, const DenseOut oa, int na, const NtArgs gb, const EpiOut<DenseOut> eb, int nb,
                                                       ColumnSums sums) {
-  typedef NtTiles<3, 3, NT_BF16_DENSE>::T4 TB;
-  static_assert(TB::T == 256 && TB::LDS >= 4 * MT * 2 * 1024, "workgroups of both");
+  typedef FewTile TB;
+  static_assert(TB::T == 512 && TB::LDS >= 8 * MT * 2 * 1024, "workgroups of both");
   __shared__ __attribute__((aligned(16))) uint8_t lds[TB::LDS];
   const int id = blockIdx.x;
   if (id < na) few_dx<MT>(gp, nch, w, oa, lds, id);
@@ -347,17 +350,23 @@ __global__ __launch_bounds__(256, 2) void k_dense_few(const uint8_t *gp, int nch
 // b: dw's product, if it goes along (nb tiles)
 static hipError_t launch_few(const uint8_t *gp, int64_t nch, const DevMat &w, const DenseOut &a, NtArgs gb, const DenseOut &b, int64_t nb, const ColumnSums &sums,
                              hipStream_t s) {
-  typedef NtTiles<3, 3, NT_BF16_DENSE>::T4 TB;
   if (nb) {
-    const hipError_t e = nt_args<TB>(gb, b.rows, b.cols, 32, 64, 0, nb, 1);
+    const hipError_t e = nt_args<FewTile>(gb, b.rows, b.cols, FewTile::BM, FewTile::BN, 0, nb, 1);
     if (e != hipSuccess) return e;
   }
   const int64_t na = blocks_of(a.cols, 32), ns = sums.out ? blocks_of(sums.cols, 64) : 0;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(na + nb + ns)), dim3(256), 0, s, gp, (int)nch, w, a, (int)na, gb, EpiOut<DenseOut>{b}, (int)nb, sums);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(na + nb + ns)), dim3(512), 0, s, gp, (int)nch, w, a, (int)na, gb, EpiOut<DenseOut>{b}, (int)nb, sums);
     return hipGetLastError();
   };
   return a.rows <= 16 ? go(k_dense_few<1>) : a.rows <= 32 ? go(k_dense_few<2>) : go(k_dense_few<4>);
+}
+
+// Whether that pays: on narrow layers few workgroups go through a long chain of chunks (us, left), where the other way moves w four times.  (us a call
+// this way and by tiles: 16 x 1024 x 1024 15.0 and 21.1, 64 x 1024 x 1024 17.2 and 22.7, 32 x 256 x 2048 17.3 and 23.0, 32 x 2048 x 8192 77 and 86,
+// 64 x 8192 x 8192 229 and 394; 64 x 256 x 8192 58.7 and 33.7, 1 x 1024 x 8192 58.7 and 53.6, 64 x 512 x 65536 628 and 233.)
+static bool few_pays(int64_t M, int64_t N, int64_t K) {
+  return K > 1 && M <= 64 && (float)blocks_of(N, 256) * (.8f + .013f * (float)M) < 10.f + 1.8e-6f * (float)N * (float)K;
 }
 
 template <int P, int KIND>
@@ -395,7 +404,7 @@ static hipError_t launch_pair(NtArgs ga, const DenseOut &a, NtArgs gb, const Den
 // rows), its 8 waves go through groups of U chunks of 32 columns in turn, each with the next group's loads in flight, and their sums are added in LDS in wave order.
 // A lane reads its row's eight columns of a chunk as the matrix instruction takes them, of w and of x alike (x comes from L2: laid out
 // in LDS it would have to wait there for the slowest wave); float32 values are split into their parts in registers.  Rows beyond
-// the last read that one, and their results are not stored.  Float32 8192 x 8192: one row 51 us (5.2 TB/s), 64 rows 94 us, in which the splits of x,
+// the last read that one, and their results are not stored.  Float32 8192 x 8192: one row 51 us (5.2 TB/s), 64 rows 98 us, in which the splits of x,
 // anew for every 32 rows of w, take as long as the loads.  (Laid out for the tiles instead, us a call: float32 16 x 1024 x 1024 15.0, 8.0 here;
 // 64 x 8192 x 8192 230 and 100; bf16 rows of no alignment, 64 x 1024 x 1024 12.9 and 11.6, 64 x 8192 x 8192 155 and 103.)
 template <bool BF>
@@ -831,7 +840,7 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   const int64_t K = has_dx ? w->cols : dw ? x->cols : 1;
   const int64_t nch = blocks_of(N, 32), mch = blocks_of(std::max<int64_t>(M, 1), 32), mb = blocks_of(M, 16), nb = blocks_of(N, 16),
                 kb = blocks_of(K, 16), mg = blocks_of(M, 64);
-  const bool few = !bf16 && has_dx && M <= 64 && K > 1;
+  const bool few = !bf16 && has_dx && few_pays(M, N, K);
   // (few_dx takes whole groups of row blocks)
   const int64_t gmb = few ? M <= 16 ? 1 : M <= 32 ? 2 : 4 : mb;
   const size_t b_g = has_dx ? (size_t)gmb * nch * P * FRAG : 0, b_wt = has_dx && !few ? (size_t)kb * nch * P * FRAG : 0;
@@ -883,10 +892,10 @@ vcr_status vcr_linear_grad(vcr_ctx *c, const vcr_mat *dy, const vcr_mat *x, cons
   }
   if (few) {
     // dw's tiles go along where they are few, or where dx alone leaves compute units idle (32 columns of w a workgroup); else its own plan has
-    // larger ones (us along and apart: 64 x 8192 x 256 18.4 and 19.6, 64 x 4096 x 4096 80 and 91, 64 x 1024 x 65536 757 and 835, 1 x 5120 x 5120 92 and 98;
-    // 64 x 6144 x 8192 213 and 202, 64 x 16384 x 1024 82 and 73, 64 x 8192 x 8192 278 and 235)
-    const int64_t nb = dw ? nt_tiles(N, K, 32, 64, false) : 0;
-    const bool along = nb <= 2048 || (K < 6144 && nb <= 1 << 20);   // (a launch takes less than 2^32 threads)
+    // larger ones (us along and apart: 64 x 1024 x 1024 17.1 and 22.6, 64 x 8192 x 256 18.7 and 19.2, 64 x 4096 x 4096 72 and 86, 64 x 5120 x 5120 104 and 115,
+    // 64 x 6144 x 8192 192 and 195; 64 x 7000 x 2048 68.4 and 66.0, 64 x 16384 x 1024 78 and 74, 64 x 8192 x 8192 249 and 229)
+    const int64_t nb = dw ? nt_tiles(N, K, FewTile::BM, FewTile::BN, false) : 0;
+    const bool along = nb <= 512 || (K <= 6144 && nb <= 1 << 20);   // (a launch takes less than 2^32 threads)
     HIP_TRY(c, launch_few(gp, nch, dev(w), ao, b, bo, along ? nb : 0, cs, s));
     if (!along) HIP_TRY(c, product(bf16, b, bo, part, s));
     return op_end(c);

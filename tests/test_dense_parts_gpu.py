@@ -33,8 +33,8 @@ def test_parts_over_the_residual(ctx, m, dtype, pitch):  # noqa: F811
     assert all(torch.equal(ctx.linear(x, w), ctx.linear(x, w)) for _ in range(3))
 
 
-# dw beside dx in a launch, and by its own plan
-@pytest.mark.parametrize("m,k,n", [(5, 6400, 1100), (64, 6144, 700), (33, 6143, 1200), (1, 2000, 5000), (64, 8200, 90)])
+# dw beside dx in a launch, and by its own plan; narrow layers, whose dx is taken by tiles
+@pytest.mark.parametrize("m,k,n", [(5, 6400, 1100), (64, 6144, 700), (33, 6143, 1200), (1, 2000, 5000), (64, 8200, 90), (40, 96, 6000), (64, 300, 4100)])
 def test_gradients_of_few_rows_on_wide_layers(ctx, m, k, n):  # noqa: F811
     linear_grad(ctx, m, k, n, "float32")
 
