@@ -93,12 +93,16 @@ def cross_entropy(x, label, smoothing=0.0, lse2=0.0, mean=True, scale=1.0):
             if t >= n:
                 loss[r], d[r] = np.nan, np.nan
                 continue
+            # (by differences from the maximum: e - x_t would lose log sum beside a maximum of 2^53 or more)
             top = x[r].max()
-            e = top + np.log(np.exp(x[r] - (0.0 if top == -np.inf else top)).sum()) if np.isfinite(top) else np.nan
-            loss[r] = e + lse2 * e * e - ((1 - smoothing) * x[r, t] if smoothing < 1 else 0.0)
+            below = x[r] - top if np.isfinite(top) else np.full(n, np.nan)
+            p = np.exp(below)
+            log_sum = np.log(p.sum())
+            e = top + log_sum
+            loss[r] = log_sum + lse2 * e * e - ((1 - smoothing) * below[t] if smoothing < 1 else 0.0)
             if smoothing > 0:
-                loss[r] -= smoothing * x[r].mean()
-            q = (1 + 2 * lse2 * e) * np.exp(x[r] - e) - smoothing / n
+                loss[r] -= smoothing * below.mean()
+            q = (1 + 2 * lse2 * e) * p / p.sum() - smoothing / n
             q[t] -= 1 - smoothing
             d[r] = scale * q / count
     return loss.sum() / count, loss, d

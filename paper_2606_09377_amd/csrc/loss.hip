@@ -32,12 +32,13 @@ __device__ __forceinline__ RowSum joined(const RowSum &a, const RowSum &b) {
   const float top = fmaxf(a.top, b.top), base = base_of(top);
   return RowSum{top, a.sum * exp_less(a.top, base) + b.sum * exp_less(b.top, base), a.mean + b.mean};
 }
-// Of many values: 2^(x L - base L), a multiply-add less than exp_less, and what base L was rounded by as a factor of them all.
-// Where base L overflows (a mask of the type's lowest value that left nothing else) or base is infinite or NaN: exp_less.
+// Of many values: 2^(x L - base L), a multiply-add less than exp_less, and what base L was rounded by as a factor of them all.  That is half a
+// unit of base L's last place: below 2^24 the factor lies between 1/2 and 2 (at 2^30 it may be 2^64, from 1.5e9 on infinite or 0, and NaN with the values'
+// opposite).  Beyond, or where base is infinite or NaN: exp_less.  (A thread's base is the maximum of its own values so far, which may all be masked.)
 struct ExpLess {
   float base, scaled, factor;
   bool fast;
-  __device__ __forceinline__ explicit ExpLess(float b) : base(b), scaled(b * LOG2E), factor(1.f), fast(fabsf(b) < 1e37f) {
+  __device__ __forceinline__ explicit ExpLess(float b) : base(b), scaled(b * LOG2E), factor(1.f), fast(fabsf(b) < 0x1p24f) {
     if (fast) factor = __builtin_amdgcn_exp2f(-fmaf(b, LOG2E, -scaled));
   }
   template <bool FAST>
