@@ -833,12 +833,19 @@ hipError_t nt_args(NtArgs &g, int64_t M, int64_t N, int bm, int bn, int64_t firs
   g.z_chunks = (kt + parts - 1) / parts * T::KS;
   return hipSuccess;
 }
+// (in launches of what each can count, 32 bits of threads)
 template <class T, class EPI>
 hipError_t launch_nt(NtArgs g, int64_t M, int64_t N, int bm, int bn, int64_t first, int64_t count, int parts, const EPI &epi, hipStream_t s) {
-  const hipError_t e = nt_args<T>(g, M, N, bm, bn, first, count, parts);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)(count * g.sub_m * g.sub_n), (unsigned)parts), dim3(T::T), 0, s, g, epi);
-  return hipGetLastError();
+  const int64_t subs = (int64_t)(bm / T::BM) * (bn / T::BN), most = std::max<int64_t>(1, 0xffffffffll / T::T / std::max<int64_t>(1, subs));
+  for (int64_t at = first; at < first + count || at == first; at += most) {
+    const int64_t n = std::min(most, first + count - at);
+    hipError_t e = nt_args<T>(g, M, N, bm, bn, at, n, parts);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_nt<T, EPI>), dim3((unsigned)(n * subs), (unsigned)parts), dim3(T::T), 0, s, g, epi);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 // The smallest shape
 template <class TS, class = void>
