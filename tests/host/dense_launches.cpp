@@ -5,8 +5,8 @@
 // arguments say is written lies inside the call's workspace, no two buffers over each other.
 //
 //   dense_launches            reads calls, one a line, and prints each one's launches
-//     linear rows k n bf16 pitch act drop residual z other     grad rows k n bf16 pitch act drop need (1 dx, 2 dw, 4 db) other     loss rows n bf16 pitch
-//     other: results (y, dw) of the other type
+//     linear rows k n bf16 pitch act drop residual z other     grad rows k n bf16 pitch act drop need (1 dx, 2 dw, 4 db) other     loss rows n bf16 pitch other
+//     other: results (y, dw, dlogits) of the other type
 //   dense_launches random N   makes N calls of legal sizes, the smallest and the largest among them
 #include <cxxabi.h>
 #include <dlfcn.h>
@@ -116,7 +116,7 @@ static void note(const vcr::NtArgs &g, dim3 grid, int parts) {
   operand(g.B, g.chunks, parts);
   if ((int64_t)g.z_chunks * grid.y < g.chunks) wrong("parts do not cover the contraction");
   notes += (int64_t)g.z_chunks * (grid.y - 1) >= g.chunks ? " empty" : "";   // (a part without a share: its sums are zeros)
-  notes += " chunks=" + std::to_string(g.chunks) + " z=" + std::to_string(g.z_chunks) + " cols=" + std::to_string(g.cols);
+  notes += " chunks=" + std::to_string(g.chunks) + " z=" + std::to_string(g.z_chunks) + " cols=" + std::to_string(g.cols) + " first=" + std::to_string(g.first);
 }
 static void epilogue(const vcr::EpiPart &e, dim3 grid) { span(e.p, (uint64_t)grid.y * e.rows * e.ld * 4); }
 static void epilogue(const vcr::EpiOut<DenseOut> &, dim3) {}
@@ -282,7 +282,7 @@ static vcr_status make(const Call &c) {
     const vcr_mat x = mat(0, c.m, c.n, c), r = mat(1, c.m, c.n, c), y = mat(2, c.m, c.n, c);
     st = vcr_dropout(ctx, &x, &drop, c.residual ? &r : nullptr, &y);
   } else {   // need: 1 dlogits, 2 losses, 4 total
-    const vcr_mat x = mat(0, c.m, c.n, c), d = mat(1, c.m, c.n, c);
+    const vcr_mat x = mat(0, c.m, c.n, c), d = mat(1, c.m, c.n, c, c.bf16 ^ c.other);
     const vcr_loss_opts o{.1f, 0.f, 1, 1.f};
     st = vcr_cross_entropy(ctx, &x, reinterpret_cast<int64_t *>(vec), &o, c.need & 2 ? vec : nullptr, c.need & 4 ? vec : nullptr, c.need & 1 ? &d : nullptr);
   }
@@ -338,7 +338,7 @@ int main(int argc, char **argv) {
     bool good;
     if (q.kind == "linear") good = scanf("%" SCNd64 " %" SCNd64 " %" SCNd64 " %d %" SCNd64 " %d %d %d %d %d", &q.m, &q.k, &q.n, &q.bf16, &q.pitch, &q.act, &q.drop, &q.residual, &q.z, &q.other) == 10;
     else if (q.kind == "grad") good = scanf("%" SCNd64 " %" SCNd64 " %" SCNd64 " %d %" SCNd64 " %d %d %d %d", &q.m, &q.k, &q.n, &q.bf16, &q.pitch, &q.act, &q.drop, &q.need, &q.other) == 9;
-    else good = scanf("%" SCNd64 " %" SCNd64 " %d %" SCNd64, &q.m, &q.n, &q.bf16, &q.pitch) == 4;
+    else good = scanf("%" SCNd64 " %" SCNd64 " %d %" SCNd64 " %d", &q.m, &q.n, &q.bf16, &q.pitch, &q.other) == 5;
     if (!good) return 2;
     const vcr_status st = make(q);
     printf("%d%s\n", (int)st, text.c_str());

@@ -59,7 +59,7 @@ def check(ctx, x, label, dtype, shift=0, lse2=0.0, mean=True):
 
 
 # one workgroup for everything (8 lanes a row, a wave a row), waves, workgroups of 256, 512 and 1024, rows beyond the registers, rows divided
-PLANS = [(30, 60), (9, 200), (32, 1000), (300, 200), (40, 1000), (40, 4000), (40, 8000), (40, 16000), (40, 32000), (70, 140000), (3, 100001)]
+PLANS = [(200, 30), (30, 60), (9, 200), (32, 1000), (300, 200), (40, 1000), (40, 4000), (40, 8000), (40, 16000), (40, 32000), (40, 50000), (70, 140000), (3, 100001)]
 MASKS = (-1e4, -16777216.0, -1.6e7, -1e9, -2e9, -5e9, -1e10, -1e20, -1e30, -1e36, -9.9e36, -1.1e37)
 
 
