@@ -492,7 +492,8 @@ typedef struct {
 
 /* z = x w^T + bias, y = D(act(z)) + residual, x (rows, k) and w (n, k) of one type, y (rows, n); z is written where it is
  * given.  opts may be NULL (y = x w^T); y may be the residual itself.  bf16 products are exact, float32 ones as under
- * "Arithmetic", x and w alike exact down to 2^-110 and below that each rounded by up to 2^-134; sums are float32, in an order that depends on the sizes, and each output is rounded once to its type. */
+ * "Arithmetic", x and w alike exact down to 2^-110 and each rounded by up to 2^-134 below that; sums are float32, in an
+ * order that depends on the sizes, and each output is rounded once to its type. */
 vcr_status vcr_linear(vcr_ctx *ctx, const vcr_mat *x, const vcr_mat *w, const vcr_linear_opts *opts, const vcr_mat *y);
 
 /* Gradients of vcr_linear from dy (rows, n): with g = D(dy) act'(z) (act'(0) = 0 for VCR_ACT_RELU),
@@ -519,8 +520,9 @@ typedef struct {
  * N the number of rows with a label of 0 or more (1 if there is none) with `mean`, else 1.  A row with a negative label does not
  * count: its loss and dlogits are 0, and its logits are not read.  One with a label of n or more has a loss and dlogits of NaN.  Logits of
  * -infinity have probability 0 (and make the loss infinite with smoothing); a row of nothing else, or with +infinity or
- * NaN, gives NaN; finite ones may be as large as float32 holds, so masks of any large negative number serve.  loss (rows), total (1) and dlogits may be NULL; dlogits may be logits itself.  Statistics are float32; sums are taken
- * in a fixed order. */
+ * NaN, gives NaN.  Finite ones may be as large as float32 holds: any large negative number masks a class.  loss (rows), total (1) and
+ * dlogits may be NULL; dlogits may be logits itself.  Statistics are float32 (exp(x_j - e) to about (|x_j - e| + 2) 2^-23 of itself); sums are
+ * taken in a fixed order. */
 vcr_status vcr_cross_entropy(vcr_ctx *ctx, const vcr_mat *logits, const int64_t *label, const vcr_loss_opts *opts, float *loss,
                              float *total, const vcr_mat *dlogits);
 

@@ -6,7 +6,9 @@
 // The products are nt.h's, on matrix instructions.  bf16 matrices go into the tiles as they are stored (rows aligned to 16 bytes; the
 // gradients' operands are transposed on the way out of LDS), others are laid out in the instructions' order first, bf16 values in one part,
 // float32 ones in three (their six partial products keep float32's accuracy).  Dropout's factor is left out of g and
-// multiplies the sums, so that a bf16 g is dy itself or zero where the activation's slope is.
+// multiplies the sums, so that a bf16 g is dy itself or zero behind ReLU.  Behind GELU and SiLU g = dy act'(z) has more bits than dy, and is rounded to bf16 for both
+// products, as dy was when its layer wrote it: results are then off by 2.3e-3 of themselves instead of the 1.7e-3 that their own rounding costs.  In two
+// parts it would double the products' instructions, which are what bounds them; float32 operands keep all bits.  db takes g unrounded.
 //
 // 4096 x 8192 x 8192 in bf16 is bound by the matrix instructions and what feeds them: y alone 364 us (1.51 PFLOP/s; a library product 345), with all that the
 // epilogue does 434; dx 371 and dw 399 (library 396 and 471), both with db behind ReLU and dropout 818.  Few rows are bound by reading the weights: one bf16 row of
@@ -404,8 +406,9 @@ static hipError_t launch_pair(NtArgs ga, const DenseOut &a, NtArgs gb, const Den
 // rows), its 8 waves go through groups of U chunks of 32 columns in turn, each with the next group's loads in flight, and their sums are added in LDS in wave order.
 // A lane reads its row's eight columns of a chunk as the matrix instruction takes them, of w and of x alike (x comes from L2: laid out
 // in LDS it would have to wait there for the slowest wave); float32 values are split into their parts in registers.  Rows beyond
-// the last read that one, and their results are not stored.  Float32 8192 x 8192: one row 51 us (5.2 TB/s), 64 rows 98 us, in which the splits of x,
-// anew for every 32 rows of w, take as long as the loads.  (Laid out for the tiles instead, us a call: float32 16 x 1024 x 1024 15.0, 8.0 here;
+// the last read that one, and their results are not stored.  Float32 8192 x 8192: one row 51 us (5.2 TB/s), 64 rows 98 to 104 us, in which the splits of x,
+// anew for every 32 rows of w, take as long as the loads (ten of that variant's registers wait in scratch memory outside the
+// loop, none is fetched in it).  (Laid out for the tiles instead, us a call: float32 16 x 1024 x 1024 15.0, 8.0 here;
 // 64 x 8192 x 8192 230 and 100; bf16 rows of no alignment, 64 x 1024 x 1024 12.9 and 11.6, 64 x 8192 x 8192 155 and 103.)
 template <bool BF>
 struct Raw8 {   // eight columns of a row as stored

@@ -1,8 +1,11 @@
 // Cross entropy with its gradient: vcr_cross_entropy of vcrown.h.
 //
 // With m = max x, S = sum exp(x - m), e = m + log S, a row's loss is (m - (1 - s) x_t - s mean x) + log S + c e^2 and its gradient
-// a multiple of exp(x - m) less a constant, and less another at the label.  exp(x - m) is 2^((x - m) L), L = log2 e.  (2^(x L - m L)
-// would take one instruction less, but m L overflows where all that a mask left is the type's lowest value.)
+// a multiple of exp(x - m) less a constant, and less another at the label.  exp(x - m) is 2^((x - m) L), L = log2 e, or where that is safe
+// 2^(x L - m L), an instruction less (ExpLess).  The exponent is rounded to float32, by up to 2^-24 of |x - m| L, as x - m is in a plain form; L itself is
+// rounded too, which makes it 2^-26 of that too small.  So exp(x - m) is off by about 2^-24 |x - m| of itself: 2e-7 at random where |x - m| is 2 to 8, 4e-7 at 16 to 40 (a
+// plain form 1.5e-7 and 6e-7 on float32 logits; nothing on those of few bits, whose differences are exact).  A second word of L would correct the 2^-26 alone, at
+// an instruction more for every value; half a unit of the sum's last place is what it amounts to.
 #include "training.h"
 
 namespace vcr {
@@ -479,7 +482,7 @@ __global__ __launch_bounds__(256) void k_loss_split(const LossArgs a, int per, i
 
 // One workgroup for everything saves a launch where it has few rows a group (us a call, this way and by rows: 64 x 10 10.0 and 13;
 // 256 x 60 11.0 and 13.5, 512 x 60 17 and 13; 32 x 1000 11.1 and 13.6, 48 x 1000 13.4 and 13.6).  Rows are divided where there are too few of them for the
-// chip and each takes long (this way and by rows: 1 x 30000 bf16 16 and 14, 5 x 100001 13.8 and 19, 64 x 100000 19 and 20, float32 64 x
+// chip and each takes long (this way and by rows: 1 x 30000 bf16 16 and 14, 5 x 100001 13.4 and 19, 64 x 100000 19 and 20, float32 64 x
 // 50000 18 and 14, bf16 64 x 262144 28 and 38, 128 x 262144 48 and 45).
 struct LossPlan {
   bool small;
